@@ -20,7 +20,8 @@
  *   UnBatch                                      -> nothing to do: block tables persist
  *
  * Geometry is fixed to the attention shape the kernels are written for:
- * 8 query heads sharing 1 KV head, head_dim 256, page size 16 tokens, bf16.
+ * 8 query heads sharing 1 KV head, head_dim 256, page size 16 tokens, bf16 (the cache: bf16 or,
+ * by request of the pool, 8 bits).
  *
  * Conventions
  *  - Every call returns 0 (OXY_OK) or a negative oxy_status; no C++ exception
@@ -62,6 +63,22 @@
  *   V page: chunk (w, c, gp, n), w<4, c<4, gp<2, n<16, at byte ((((w*4+c)*2+gp)*16)+n)*16
  *           holds V[4gp..4gp+3][d] followed by V[8+4gp..8+4gp+3][d], d = 64w+4n+c.
  * oxy_gather_kv reads tokens back in the natural [token][256] order.
+ *
+ * A pool in 8 bits (OXY_POOL_KV_FP8) holds a row x of 256 bf16 -- a token's key or value -- as 256
+ * e4m3 codes and one exponent byte b:
+ *   b = 127 + the smallest e >= -126 with max|x| <= 448 * 2^e    (over the finite elements)
+ *   code_i = x_i * 2^-e rounded to e4m3, to nearest even         (infinities and NaN: NaN)
+ *   value_i = code_i * 2^e            (a bf16 number; infinite where |x_i| >= 1.9375 * 2^127 makes it 2^128)
+ * Every call takes and returns bf16 as with a bf16 pool; the attention is that of the values, and
+ * oxy_gather_kv returns them.  What a row holds depends on that row alone, not on how a history was
+ * cut into calls, what else is in its page or what was there before.  About half the memory
+ * (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded up to 256): first
+ * the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.
+ *   K page: 16-byte chunk (jj, hf, g, k8), jj<4, hf<2, g<4, k8<8, at ((((jj*2+hf)*4+g)*8)+k8)*16
+ *           holds the codes of K[8hf+k8][64jj+16g .. +15].
+ *   V page: chunk (w, cp, gp, n), w<4, cp<2, gp<2, n<16, at ((((w*2+cp)*2+gp)*16)+n)*16 holds those of
+ *           V[4gp..4gp+3][d], V[8+4gp..8+4gp+3][d], then the same of d+1, d = 64w+4n+2cp.
+ *   exponents: K key k at 2*(k%8) + k/8; V key k at 16 + 8*((k/4)%2) + 4*(k/8) + k%4.
  */
 #ifndef OXY_H
 #define OXY_H
@@ -90,6 +107,7 @@ enum { OXY_KIND_ACTION = 0, OXY_KIND_DECODE = 1 };
 enum { OXY_POOL_HOST_ONLY = 1 }; /* metadata only: no device pointer is touched, no HIP call is
                                     made; append/attention/gather return OXY_ERR_INVALID_ARG.
                                     For indexing tests on machines without a GPU.              */
+enum { OXY_POOL_KV_FP8 = 2 };    /* keys and values are held in 8 bits (see above)             */
 /* batch flags */
 enum { OXY_BATCH_APPEND_ONLY = 1 }; /* lengths, blocks and slots only; no attention work list
                                        (used to load a history); oxy_mixed_attention on such a
@@ -238,6 +256,8 @@ int32_t oxy_mixed_attention_static(oxy_pool *pool, const oxy_batch *batch, int32
  * launch sequence is updated in place once eight are held).  Same kernels, same arguments,
  * same results bit for bit.  The pool keeps the recordings until it is destroyed; the pointers
  * must stay valid while steps of that form are replayed.  events must be NULL.
+ * On a pool in 8 bits OXY_STEP_FUSE_ACROSS_LAYERS and OXY_STEP_FOLD_APPEND are not covered and ignored:
+ * new rows are quantised by a launch of their own.
  * events: NULL, or HOST array of 4*(layer_end-layer_begin) entries, each a created hipEvent_t or
  * NULL; per layer they receive the begin and end timestamps of the work-item kernel and of the
  * merge kernel themselves (hipExtLaunchKernel start/stop events; a profiling hook).  A launch
@@ -264,6 +284,62 @@ int32_t oxy_batch_destroy(oxy_batch *batch);
  * k_out, v_out: DEVICE bf16 [n][256]. */
 int32_t oxy_gather_kv(oxy_pool *pool, int32_t layer, const int64_t *slots, int32_t n,
                       void *k_out, void *v_out, void *hip_stream);
+/* The same of layers [layer_begin, layer_end): layer l's rows go to k_out + (l - layer_begin) * layer_stride
+ * and v_out likewise (bytes, at least n * 512).  On a pool in 8 bits one launch serves all the layers. */
+int32_t oxy_gather_kv_layers(oxy_pool *pool, int32_t layer_begin, int32_t layer_end,
+                             const int64_t *slots, int32_t n, void *k_out, void *v_out,
+                             size_t layer_stride, void *hip_stream);
+
+/* --- rotary positions: what queries and keys carry when they meet in the cache --------- */
+/* Pair i of the first rot_dims dims of a row is turned by position * freqs[i]:
+ *   y1 = x1 c - x2 s, y2 = x2 c + x1 s,  c, s = amplitude * (cos, sin);
+ * the other dims are copied.  Angles are taken in 64 bits, products in 32, the result is rounded to
+ * bf16 once.  The gradient, or the way back (amplitude 1), is the call with negated positions. */
+enum { OXY_ROTARY_HALVES = 0,  /* pairs (i, i + rot_dims / 2) */
+       OXY_ROTARY_PAIRS = 1 }; /* pairs (2i, 2i + 1)          */
+enum { OXY_ROTARY_MAX_HEADS = 1024 };
+typedef struct {
+  int32_t rot_dims;    /* even, 2..256                                              */
+  int32_t layout;
+  const double *freqs; /* DEVICE [rot_dims / 2], radians per position               */
+  double amplitude;    /* 1, or what oxy_rotary_freqs returned                      */
+} oxy_rotary_config;
+/* Frequencies base^(-2i / rot_dims), and their forms for contexts longer than original_len (HOST
+ * only): LINEAR divides all by the factor; BASE raises the base to base * factor^(r / (r - 2)), which
+ * divides the slowest pair by it (rot_dims 2: as PLAIN); BANDS divides pairs of fewer than `low` turns in
+ * original_len positions, keeps those of more than `high`, and blends between by turns; RAMP blends
+ * between the same two limits by the pair's index, from the floor of the index that makes `high`
+ * turns (not below 0) to the ceiling of the one that makes `low` (not above rot_dims - 1), and asks for an
+ * amplitude of 1 + 0.1 ln(factor). */
+enum { OXY_ROTARY_PLAIN = 0, OXY_ROTARY_LINEAR = 1, OXY_ROTARY_BASE = 2, OXY_ROTARY_BANDS = 3,
+       OXY_ROTARY_RAMP = 4 };
+typedef struct {
+  double base;          /* above 0; RAMP: above 1                                     */
+  int32_t rot_dims;
+  int32_t kind;
+  double factor;        /* 1 or more (PLAIN: unused)                                  */
+  double low, high;     /* BANDS, RAMP: 0 < low < high                                */
+  int32_t original_len; /* BANDS, RAMP: positions of the original context, 1 or more  */
+} oxy_rotary_scaling;
+/* freqs: HOST [rot_dims / 2]; amplitude: HOST, may be NULL. */
+int32_t oxy_rotary_freqs(const oxy_rotary_scaling *scaling, double *freqs, double *amplitude);
+/* Rows of n_tokens tokens (0: nothing to do), n_heads of them side by side per token: row (t, h) at
+ * x + t * x_stride + h * 512 -> out + t * out_stride + h * 512, DEVICE bf16, strides in bytes, all
+ * 16-byte aligned.  positions: DEVICE int32 [n_tokens].  out may be x with the same stride; other
+ * overlaps of rows are not allowed. */
+int32_t oxy_rotary(const oxy_rotary_config *cfg, const int32_t *positions, const void *x,
+                   size_t x_stride, void *out, size_t out_stride, int32_t n_tokens,
+                   int32_t n_heads, void *hip_stream);
+/* The new tokens of a batch in one launch: queries turned into q_out (DEVICE bf16 [n][8][256], the q
+ * of oxy_mixed_attention), new keys turned and stored, new values stored, in the slots of `layer`, bf16
+ * or 8 bits.  Same results as oxy_rotary on queries and keys and oxy_stream_append of the turned
+ * keys.  Token t's rows: q + t * q_stride (8 x 256), k_new + t * k_stride, v_new + t * v_stride, strides
+ * in bytes, all 16-byte aligned, so a projection's [n][10 * 256] output is taken as it is.  q may be
+ * NULL (keys and values only; q_out is not touched); q_out may be q if q_stride is 4096. */
+int32_t oxy_rotary_append(oxy_pool *pool, const oxy_batch *batch, int32_t layer,
+                          const oxy_rotary_config *cfg, const int32_t *positions, const void *q,
+                          size_t q_stride, void *q_out, const void *k_new, size_t k_stride,
+                          const void *v_new, size_t v_stride, void *hip_stream);
 
 /* --- introspection (HOST outputs; these are the indexing results compared bit-exactly) -- */
 int32_t oxy_stream_info(oxy_pool *pool, int32_t stream_id, int32_t *prefix_id, int32_t *kind,

@@ -12,6 +12,8 @@ attention   float64 attention over the visible set of each query (numpy).
 brute       the same definition in pure-Python loops, for tiny cases.
 pool_model  the indexing oracle: free stack, refcounts, block tables, slots.
 replay      runs an operation trace through pool_model + attention.
+kv8         what a cache in 8 bits holds for a row.
+rotary      rotation of rows by their tokens' positions, and the frequencies.
 schedule    the per-frame execution flow (Alg. 1) under arbitrary arrivals, and the
             ablation variants, as a plain simulation.
 

@@ -19,10 +19,13 @@ ERR_INVALID_ARG, ERR_NO_BLOCKS, ERR_BAD_ID, ERR_SEALED = -1, -2, -3, -4
 ERR_BUSY, ERR_WORKSPACE, ERR_DEVICE = -5, -6, -7
 KIND_ACTION, KIND_DECODE = 0, 1
 POOL_HOST_ONLY = 1
+POOL_KV_FP8 = 2
 BATCH_APPEND_ONLY = 1
 STEP_FUSE_ACROSS_LAYERS = 1
 STEP_FOLD_APPEND = 2
 STEP_GRAPH = 4
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = 0, 1, 2, 3, 4
 SCHED_BATCHED, SCHED_UNBATCHED, SCHED_UPPER_BOUND = 0, 1, 2
 
 EXPORTS = [
@@ -34,7 +37,8 @@ EXPORTS = [
     "oxy_stream_append", "oxy_mixed_attention", "oxy_mixed_attention_static", "oxy_step_layers", "oxy_step_graph_stats",
     "oxy_append_attention",
     "oxy_batch_destroy",
-    "oxy_gather_kv",
+    "oxy_gather_kv", "oxy_gather_kv_layers",
+    "oxy_rotary_freqs", "oxy_rotary", "oxy_rotary_append",
     "oxy_stream_info", "oxy_stream_blocks", "oxy_prefix_info", "oxy_prefix_blocks",
     "oxy_block_refcounts", "oxy_free_blocks", "oxy_pool_stats", "oxy_batch_info",
     "oxy_batch_slots", "oxy_batch_work", "oxy_batch_records",
@@ -67,6 +71,17 @@ class PoolConfig(ctypes.Structure):
 class SchedConfig(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int32), ("denoise_steps", ctypes.c_int32), ("chunk", ctypes.c_int32),
                 ("max_active", ctypes.c_int32), ("mode", ctypes.c_int32)]
+
+
+class RotaryConfig(ctypes.Structure):
+    _fields_ = [("rot_dims", ctypes.c_int32), ("layout", ctypes.c_int32), ("freqs", ctypes.c_void_p),
+                ("amplitude", ctypes.c_double)]
+
+
+class RotaryScaling(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("rot_dims", ctypes.c_int32), ("kind", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("original_len", ctypes.c_int32)]
 
 
 class Item(ctypes.Structure):
@@ -120,6 +135,13 @@ def lib():
             "oxy_append_attention": [vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp],
             "oxy_batch_destroy": [vp],
             "oxy_gather_kv": [vp, i32, vp, i32, vp, vp, vp],
+            "oxy_gather_kv_layers": [vp, i32, i32, vp, i32, vp, vp, ctypes.c_size_t, vp],
+            "oxy_rotary_freqs": [ctypes.POINTER(RotaryScaling), ctypes.POINTER(ctypes.c_double),
+                                 ctypes.POINTER(ctypes.c_double)],
+            "oxy_rotary": [ctypes.POINTER(RotaryConfig), vp, vp, ctypes.c_size_t, vp, ctypes.c_size_t, i32,
+                           i32, vp],
+            "oxy_rotary_append": [vp, vp, i32, ctypes.POINTER(RotaryConfig), vp, vp, ctypes.c_size_t, vp, vp,
+                                  ctypes.c_size_t, vp, ctypes.c_size_t, vp],
             "oxy_stream_info": [vp, i32, pi32, pi32, pi32, pi32],
             "oxy_stream_blocks": [vp, i32, pi32, i32],
             "oxy_prefix_info": [vp, i32, pi32, pi32, pi32, pi32],
@@ -328,6 +350,38 @@ def _i64(values):
 def oxy_gather_kv(pool, layer, slots, k_out_ptr, v_out_ptr, stream):
     arr, ptr, n = _i64(slots)
     _check(lib().oxy_gather_kv(pool, layer, ptr, n, k_out_ptr, v_out_ptr, stream or None))
+
+
+def oxy_gather_kv_layers(pool, layer_begin, layer_end, slots, k_out_ptr, v_out_ptr, layer_stride, stream):
+    arr, ptr, n = _i64(slots)
+    _check(lib().oxy_gather_kv_layers(pool, layer_begin, layer_end, ptr, n, k_out_ptr, v_out_ptr, layer_stride,
+                                      stream or None))
+
+
+def make_rotary(freqs_ptr, rot_dims, layout=ROTARY_HALVES, amplitude=1.0):
+    """freqs_ptr: device address of rot_dims / 2 float64 frequencies (see oxy_rotary_freqs)."""
+    return RotaryConfig(rot_dims, layout, freqs_ptr or None, amplitude)
+
+
+def oxy_rotary_freqs(base, rot_dims, kind=ROTARY_PLAIN, factor=1.0, low=0.0, high=0.0, original_len=0):
+    """-> (frequencies as a float64 array [rot_dims / 2], amplitude)"""
+    scaling = RotaryScaling(base, rot_dims, kind, factor, low, high, original_len)
+    out, amplitude = np.zeros(max(rot_dims // 2, 1)), ctypes.c_double(1.0)
+    _check(lib().oxy_rotary_freqs(ctypes.byref(scaling), out.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                  ctypes.byref(amplitude)))
+    return out, amplitude.value
+
+
+def oxy_rotary(rotary, positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream):
+    _check(lib().oxy_rotary(ctypes.byref(rotary), positions_ptr or None, x_ptr or None, x_stride,
+                            out_ptr or None, out_stride, n_tokens, n_heads, stream or None))
+
+
+def oxy_rotary_append(pool, batch, layer, rotary, positions_ptr, q_ptr, q_stride, q_out_ptr, k_ptr, k_stride,
+                      v_ptr, v_stride, stream):
+    _check(lib().oxy_rotary_append(pool, batch, layer, ctypes.byref(rotary), positions_ptr or None,
+                                   q_ptr or None, q_stride, q_out_ptr or None, k_ptr or None, k_stride,
+                                   v_ptr or None, v_stride, stream or None))
 
 
 def oxy_stream_info(pool, stream_id):

@@ -5,6 +5,7 @@
 // descriptor build and UnBatch is a no-op.
 #include "../../include/oxy.h"
 #include "oxy_internal.h"
+#include "oxy_kv8.h"
 
 #include <algorithm>
 #include <cstdarg>
@@ -96,6 +97,7 @@ constexpr size_t kMaxStepGraphs = 8;
 struct oxy_pool {
   oxy_pool_config cfg;
   bool host_only = false;
+  bool kv8 = false;   // OXY_POOL_KV_FP8
   std::vector<int32_t> free_stack;  // top = back
   std::vector<int32_t> ref;
   std::unordered_map<int32_t, Prefix> prefixes;
@@ -222,8 +224,34 @@ int32_t stream_split_for(const oxy_pool_config& c, int32_t len) {
   return len <= 512 ? 128 : 256;
 }
 
+// bytes of one layer of the KV buffer, and of one block in it
+size_t layer_bytes_of(const oxy_pool_config& c) {
+  return c.flags & OXY_POOL_KV_FP8 ? oxy::layer_bytes8(c.num_blocks) : (size_t)c.num_blocks * oxy::kBlockBytes;
+}
+int32_t block_bytes_of(const oxy_pool* p) {
+  return p->kv8 ? oxy::kBlockBytes8 + oxy::kScaleBytes8 : oxy::kBlockBytes;
+}
+
 char* layer_base(const oxy_pool* p, int32_t layer) {
-  return (char*)p->cfg.kv_base + (size_t)layer * p->cfg.num_blocks * oxy::kBlockBytes;
+  return (char*)p->cfg.kv_base + (size_t)layer * layer_bytes_of(p->cfg);
+}
+oxy::Layer8 layer8(const oxy_pool* p, int32_t layer) {
+  return oxy::layer8_of(layer_base(p, layer), p->cfg.num_blocks);
+}
+
+// Launches by the form the pool holds its rows in.
+hipError_t append_rows(const oxy_pool* p, int32_t layer, const void* k_new, const void* v_new, const int32_t* d_slots,
+                       int32_t n_tokens, hipStream_t s) {
+  if (p->kv8) return oxy::launch_append8(k_new, v_new, d_slots, n_tokens, layer8(p, layer), s);
+  return oxy::launch_append(k_new, v_new, d_slots, n_tokens, layer_base(p, layer), s);
+}
+hipError_t attention_work(const oxy_pool* p, const oxy::AttnArgs& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
+  return p->kv8 ? oxy::launch_attention_work8(a, s, start, stop) : oxy::launch_attention_work(a, s, start, stop);
+}
+hipError_t attention(const oxy_pool* p, const oxy::AttnArgs& a, hipStream_t s) {
+  if (!p->kv8) return oxy::launch_attention(a, s);
+  const hipError_t e = oxy::launch_attention_work8(a, s, nullptr, nullptr);
+  return e != hipSuccess ? e : oxy::launch_merge_append(a, nullptr, s);
 }
 
 }  // namespace
@@ -237,7 +265,7 @@ int32_t oxy_version(void) { return 1; }
 size_t oxy_kv_bytes(const oxy_pool_config* cfg) {
   oxy_pool_config c;
   if (!resolve_config(cfg, &c)) return 0;
-  return (size_t)c.n_layers * c.num_blocks * oxy::kBlockBytes;
+  return (size_t)c.n_layers * layer_bytes_of(c);
 }
 
 size_t oxy_workspace_bytes(const oxy_pool_config* cfg) {
@@ -256,7 +284,9 @@ int32_t oxy_pool_create(const oxy_pool_config* cfg, oxy_pool** out) {
     return fail(OXY_ERR_INVALID_ARG,
                 "pool_create: unsupported geometry or sizes (need 8 q heads, 1 kv head, "
                 "head_dim 256, page 16, split_tokens a multiple of 32)");
-  const bool host_only = (c.flags & OXY_POOL_HOST_ONLY) != 0;
+  const bool host_only = (c.flags & OXY_POOL_HOST_ONLY) != 0, kv8 = (c.flags & OXY_POOL_KV_FP8) != 0;
+  if (kv8 && !host_only && !oxy::launch_attention_work8)
+    return fail(OXY_ERR_INVALID_ARG, "pool_create: this build has no kernels for a pool in 8 bits");
   if (!host_only) {
     if (!c.kv_base || c.kv_bytes < oxy_kv_bytes(cfg) || ((uintptr_t)c.kv_base & 255))
       return fail(OXY_ERR_INVALID_ARG, "pool_create: kv buffer missing, misaligned or < %zu bytes",
@@ -285,6 +315,7 @@ int32_t oxy_pool_create(const oxy_pool_config* cfg, oxy_pool** out) {
   p->cfg = c;
   p->cfg.free_order = nullptr;
   p->host_only = host_only;
+  p->kv8 = kv8;
   p->free_stack.assign(order.rbegin(), order.rend());  // first element of free_order on top
   p->ref.assign(c.num_blocks, 0);
   p->desc_words = desc_words_of(c);
@@ -399,7 +430,7 @@ int32_t prefix_append_impl(oxy_pool* p, int32_t pid, int32_t layer_begin, int32_
   // device copy, at most kMaxInlineBlocks blocks per launch (block ids travel by value)
   const char* kp = (const char*)k;
   const char* vp = (const char*)v;
-  const size_t pool_layer_stride = (size_t)p->cfg.num_blocks * oxy::kBlockBytes;
+  const size_t pool_layer_stride = layer_bytes_of(p->cfg);
   int32_t done = 0;
   while (done < n_tokens) {
     int32_t pos = pos0 + done;
@@ -409,10 +440,14 @@ int32_t prefix_append_impl(oxy_pool* p, int32_t pid, int32_t layer_begin, int32_
     oxy::InlineIds ids;
     int32_t nb = blocks_for(pos + n) - first_block;
     for (int32_t i = 0; i < nb; ++i) ids.v[i] = px.blocks[first_block + i];
-    hipError_t e = oxy::launch_append_inline(
-        kp + (size_t)done * oxy::kDim * 2, vp + (size_t)done * oxy::kDim * 2, ids,
-        pos - first_block * kPage, n, layer_base(p, layer_begin), layer_end - layer_begin,
-        src_layer_stride, pool_layer_stride, (hipStream_t)hip_stream);
+    const char* k_at = kp + (size_t)done * oxy::kDim * 2;
+    const char* v_at = vp + (size_t)done * oxy::kDim * 2;
+    const int32_t at = pos - first_block * kPage, layers = layer_end - layer_begin;
+    hipError_t e =
+        p->kv8 ? oxy::launch_append_inline8(k_at, v_at, ids, at, n, layer8(p, layer_begin), layers, src_layer_stride,
+                                            pool_layer_stride, (hipStream_t)hip_stream)
+               : oxy::launch_append_inline(k_at, v_at, ids, at, n, layer_base(p, layer_begin), layers, src_layer_stride,
+                                           pool_layer_stride, (hipStream_t)hip_stream);
     if (e != hipSuccess) {
       roll_back();
       return hip_fail(e, "prefix_append: launch");
@@ -732,7 +767,7 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
     int64_t live_tok = 0;
     for (const Group& g : groups) live_tok += g.px->len;
     for (const Plan& pl : plan) live_tok += pl.new_len;
-    const bool once = live_tok * c.n_layers * (oxy::kBlockBytes / kPage) > kOnceBytes;
+    const bool once = live_tok * c.n_layers * (block_bytes_of(p) / kPage) > kOnceBytes;
     for (const Plan& pl : plan) {
       const int32_t tbl_off = tbl_words;
       table_refs.push_back({tbl_off, &pl.s->blocks, blocks_for(pl.new_len)});
@@ -1120,8 +1155,7 @@ int32_t oxy_stream_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
     return fail(OXY_ERR_INVALID_ARG, "stream_append: null argument, foreign batch or host-only pool");
   if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "stream_append: layer %d", layer);
   const int32_t* d_desc = (const int32_t*)p->slots[b->slot].d_base;
-  hipError_t e = oxy::launch_append(k_new, v_new, d_desc + b->off_slots, b->n_tokens,
-                                    layer_base(p, layer), (hipStream_t)hip_stream);
+  hipError_t e = append_rows(p, layer, k_new, v_new, d_desc + b->off_slots, b->n_tokens, (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_fail(e, "stream_append: launch");
   return OXY_OK;
 }
@@ -1153,6 +1187,7 @@ oxy::AttnArgs attn_args(const oxy_pool* p, const oxy_batch* b, int32_t layer, co
   a.write_through = writes_through(b);
   a.k_new = a.v_new = nullptr;
   a.d_slots = nullptr;
+  a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
   return a;
 }
 }  // namespace
@@ -1164,8 +1199,7 @@ int32_t oxy_mixed_attention(oxy_pool* p, const oxy_batch* b, int32_t layer, cons
   if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "mixed_attention: layer %d", layer);
   if (b->flags & OXY_BATCH_APPEND_ONLY)
     return fail(OXY_ERR_INVALID_ARG, "mixed_attention: batch was built append-only");
-  hipError_t e = oxy::launch_attention(attn_args(p, b, layer, q, out, lse, scale),
-                                       (hipStream_t)hip_stream);
+  hipError_t e = attention(p, attn_args(p, b, layer, q, out, lse, scale), (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_fail(e, "mixed_attention: launch");
   return OXY_OK;
 }
@@ -1186,7 +1220,7 @@ int32_t oxy_mixed_attention_static(oxy_pool* p, const oxy_batch* b, int32_t laye
   oxy::AttnArgs a = attn_args(p, b, layer, q, out, lse, scale);
   hipError_t e = oxy::static_scratch(&a.part_acc, &a.part_ml);
   if (e != hipSuccess) return hip_fail(e, "mixed_attention_static: static buffer");
-  e = oxy::launch_attention(a, (hipStream_t)hip_stream);
+  e = attention(p, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_fail(e, "mixed_attention_static: launch");
   return OXY_OK;
 }
@@ -1227,7 +1261,7 @@ int32_t issue_step(const StepCall& c, hipStream_t s) {
   };
   auto append_now = [&](int32_t layer) {
     oxy::AppendArgs ap = append_of(layer);
-    return oxy::launch_append(ap.k_new, ap.v_new, ap.d_slots, ap.n_blocks, ap.layer_base, s);
+    return append_rows(p, layer, ap.k_new, ap.v_new, ap.d_slots, ap.n_blocks, s);
   };
   if (c.fuse) {
     hipError_t e = append_now(c.layer_begin);
@@ -1254,7 +1288,7 @@ int32_t issue_step(const StepCall& c, hipStream_t s) {
       a.v_new = ap.v_new;
       a.d_slots = ap.d_slots;
     }
-    e = oxy::launch_attention_work(a, s, ev[0], ev[1]);
+    e = attention_work(p, a, s, ev[0], ev[1]);
     if (e != hipSuccess) return hip_fail(e, "step_layers: attention");
     if (c.fuse && layer + 1 < c.layer_end) {
       oxy::AppendArgs nx = append_of(layer + 1);
@@ -1404,8 +1438,9 @@ int32_t oxy_step_layers(oxy_pool* p, const oxy_batch* b, int32_t layer_begin, in
   c.lse = lse;
   c.lse_layer_stride = lse_layer_stride;
   c.scale = scale;
-  c.fold = (flags & OXY_STEP_FOLD_APPEND) != 0 && b->append_foldable;
-  c.fuse = (flags & OXY_STEP_FUSE_ACROSS_LAYERS) != 0 && !c.fold;
+  // a pool in 8 bits quantises its new rows in a launch of their own
+  c.fold = (flags & OXY_STEP_FOLD_APPEND) != 0 && b->append_foldable && !p->kv8;
+  c.fuse = (flags & OXY_STEP_FUSE_ACROSS_LAYERS) != 0 && !c.fold && !p->kv8;
   c.events = events;
   if (flags & OXY_STEP_GRAPH) return replay_step(c, (hipStream_t)hip_stream);
   return issue_step(c, (hipStream_t)hip_stream);
@@ -1431,15 +1466,20 @@ int32_t oxy_append_attention(oxy_pool* p, const oxy_batch* b, int32_t layer, con
                          OXY_STEP_FOLD_APPEND, nullptr, hip_stream);
 }
 
-int32_t oxy_gather_kv(oxy_pool* p, int32_t layer, const int64_t* slots, int32_t n, void* k_out,
-                      void* v_out, void* hip_stream) {
+namespace {
+int32_t gather_impl(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const int64_t* slots, int32_t n, void* k_out,
+                    void* v_out, size_t layer_stride, void* hip_stream, const char* who) {
   if (!p || !slots || n < 1 || !k_out || !v_out || p->host_only)
-    return fail(OXY_ERR_INVALID_ARG, "gather_kv: null argument or host-only pool");
-  if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "gather_kv: layer %d", layer);
+    return fail(OXY_ERR_INVALID_ARG, "%s: null argument or host-only pool", who);
+  if (layer_begin < 0 || layer_end > p->cfg.n_layers || layer_begin >= layer_end)
+    return fail(OXY_ERR_INVALID_ARG, "%s: layers [%d, %d)", who, layer_begin, layer_end);
+  const int32_t layers = layer_end - layer_begin;
+  if (layers > 1 && layer_stride < (size_t)n * oxy::kDim * 2)
+    return fail(OXY_ERR_INVALID_ARG, "%s: layer stride below %d rows", who, n);
   const int64_t n_slots = (int64_t)p->cfg.num_blocks * kPage;
   for (int32_t i = 0; i < n; ++i)
     if (slots[i] < 0 || slots[i] >= n_slots)
-      return fail(OXY_ERR_INVALID_ARG, "gather_kv: slot %lld out of range", (long long)slots[i]);
+      return fail(OXY_ERR_INVALID_ARG, "%s: slot %lld out of range", who, (long long)slots[i]);
   // consecutive slots of one block travel as one run (see launch_gather_inline)
   for (int32_t done = 0; done < n;) {
     oxy::GatherRuns runs;
@@ -1455,12 +1495,67 @@ int32_t oxy_gather_kv(oxy_pool* p, int32_t layer, const int64_t* slots, int32_t 
       ++n_runs;
       done += len;
     }
-    hipError_t e = oxy::launch_gather_inline(layer_base(p, layer), runs, n_runs,
-                                             (char*)k_out + (size_t)first * oxy::kDim * 2,
-                                             (char*)v_out + (size_t)first * oxy::kDim * 2,
-                                             (hipStream_t)hip_stream);
+    char* k_at = (char*)k_out + (size_t)first * oxy::kDim * 2;
+    char* v_at = (char*)v_out + (size_t)first * oxy::kDim * 2;
+    hipError_t e = hipSuccess;
+    if (p->kv8)
+      e = oxy::launch_gather_inline8(layer8(p, layer_begin), runs, n_runs, k_at, v_at, layers, layer_stride,
+                                     layer_bytes_of(p->cfg), (hipStream_t)hip_stream);
+    else
+      for (int32_t l = 0; l < layers && e == hipSuccess; ++l)
+        e = oxy::launch_gather_inline(layer_base(p, layer_begin + l), runs, n_runs, k_at + l * layer_stride,
+                                      v_at + l * layer_stride, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail(e, "gather_kv: launch");
   }
+  return OXY_OK;
+}
+}  // namespace
+
+int32_t oxy_gather_kv(oxy_pool* p, int32_t layer, const int64_t* slots, int32_t n, void* k_out,
+                      void* v_out, void* hip_stream) {
+  if (p && (layer < 0 || layer >= p->cfg.n_layers)) return fail(OXY_ERR_INVALID_ARG, "gather_kv: layer %d", layer);
+  return gather_impl(p, layer, layer + 1, slots, n, k_out, v_out, 0, hip_stream, "gather_kv");
+}
+
+int32_t oxy_gather_kv_layers(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const int64_t* slots, int32_t n,
+                             void* k_out, void* v_out, size_t layer_stride, void* hip_stream) {
+  return gather_impl(p, layer_begin, layer_end, slots, n, k_out, v_out, layer_stride, hip_stream, "gather_kv_layers");
+}
+
+// ---- rotary positions ------------------------------------------------------------------
+int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const oxy_rotary_config* c,
+                          const int32_t* positions, const void* q, size_t q_stride, void* q_out, const void* k_new,
+                          size_t k_stride, const void* v_new, size_t v_stride, void* hip_stream) {
+  if (!p || !b || b->pool != p || !c || !c->freqs || !positions || !k_new || !v_new || (q && !q_out) || p->host_only)
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: null argument, foreign batch or host-only pool");
+  if (!oxy::launch_rotary_append) return fail(OXY_ERR_INVALID_ARG, "rotary_append: this build has no kernels for it");
+  if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "rotary_append: layer %d", layer);
+  if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2)
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: rot_dims %d, must be even, 2 to 256", c->rot_dims);
+  if (c->layout != OXY_ROTARY_HALVES && c->layout != OXY_ROTARY_PAIRS)
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: layout %d", c->layout);
+  const size_t row = (size_t)oxy::kDim * 2;
+  const uintptr_t bits = (uintptr_t)k_new | (uintptr_t)v_new | k_stride | v_stride |
+                         (q ? (uintptr_t)q | (uintptr_t)q_out | q_stride : 0);
+  if (bits & 15) return fail(OXY_ERR_INVALID_ARG, "rotary_append: rows must be 16-byte aligned");
+  if (b->n_tokens > 1 && (k_stride < row || v_stride < row || (q && q_stride < oxy::kHeads * row)))
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: stride below a token's rows");
+  const int32_t* d_desc = (const int32_t*)p->slots[b->slot].d_base;
+  oxy::RotaryAppendArgs a;
+  a.rotary = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};
+  a.q = q;
+  a.q_out = q_out;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.d_slots = d_desc + b->off_slots;
+  a.layer_base = layer_base(p, layer);
+  a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
+  a.n_tokens = b->n_tokens;
+  hipError_t e = oxy::launch_rotary_append(a, (hipStream_t)hip_stream);
+  if (e != hipSuccess) return hip_fail(e, "rotary_append: launch");
   return OXY_OK;
 }
 

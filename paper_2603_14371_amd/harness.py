@@ -37,7 +37,7 @@ class GpuWorld:
                  stream_split_tokens=0,
                  max_live_batches=2, max_q_tokens=None, max_append_tokens=None,
                  max_work_items=0, max_partials=0, want_lse=True, poison=False,
-                 fold_append=False):
+                 fold_append=False, kv8=False):
         if not torch.cuda.is_available():
             raise RuntimeError("GpuWorld needs a GPU; there is no CPU fallback")
         w = workload
@@ -55,14 +55,15 @@ class GpuWorld:
                             max_q_tokens=max_q_tokens or mq, max_append_tokens=max_append_tokens or ma,
                             max_work_items=max_work_items, max_partials=max_partials,
                             split_tokens=split_tokens,
-                            stream_split_tokens=stream_split_tokens)
+                            stream_split_tokens=stream_split_tokens,
+                            flags=B.POOL_KV_FP8 if kv8 else 0)
         kv_bytes = B.oxy_kv_bytes(cfg)
         ws_bytes = B.oxy_workspace_bytes(cfg)
         if kv_bytes == 0 or ws_bytes == 0:
             raise ValueError("invalid pool configuration")
         self.kv = torch.empty(kv_bytes, dtype=torch.uint8, device=self.device)
-        if poison:      # every bf16 of the pool is a NaN until something is appended
-            self.kv.view(torch.int16).fill_(0x7FC1)
+        if poison:      # every number of the pool is a NaN until something is appended
+            self.kv.fill_(0xFF) if kv8 else self.kv.view(torch.int16).fill_(0x7FC1)
         self.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
         cfg.kv_base, cfg.kv_bytes = self.kv.data_ptr(), kv_bytes
         cfg.workspace, cfg.workspace_bytes = self.ws.data_ptr(), ws_bytes
