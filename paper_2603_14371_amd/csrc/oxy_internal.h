@@ -83,7 +83,6 @@ struct AttnArgs {
   const void* k_new;
   const void* v_new;
   const int32_t* d_slots;
-  const uint8_t* scales;    // exponent bytes of this layer of a pool in 8 bits, else null
 };
 // Launches with more split results than kWriteThroughParts write them through, those with decode items
 // (whose work items are short and end a launch, acknowledgement included) and two workgroups on some CU

@@ -34,8 +34,15 @@ OXY_WEAK hipError_t launch_append_inline8(const void* k_new, const void* v_new, 
 OXY_WEAK hipError_t launch_gather_inline8(Layer8 layer, const GatherRuns& runs, int32_t n_runs, void* k_out, void* v_out,
                                           int32_t n_layers, size_t out_layer_stride, size_t pool_layer_stride,
                                           hipStream_t s);
-// As launch_attention_work; a.layer_base and a.scales are those of the Layer8.
-OXY_WEAK hipError_t launch_attention_work8(const AttnArgs& a, hipStream_t s, hipEvent_t start, hipEvent_t stop);
+struct AttnArgs8 : AttnArgs {
+  const uint8_t* scales;    // layer_base and scales: those of the Layer8
+  int32_t max_parts;        // most split results of a token
+};
+// As launch_attention_work.
+OXY_WEAK hipError_t launch_attention_work8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop);
+// Merge of a pool in 8 bits: launch_merge_append's where every token has at most kLongParts split results.
+constexpr int32_t kLongParts = 32;
+OXY_WEAK hipError_t launch_merge8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop);
 
 // ---- rotary positions
 struct RotaryArgs {

@@ -17,6 +17,7 @@
 // probabilities would have to be split into two and three 8-bit parts.  A conversion of two codes takes about 5 cycles
 // of a wavefront: 128 of them a round beside 48 matrix instructions of 16 cycles per 16 query rows.
 #include "oxy_kv8_device.h"
+#include "oxy_merge.h"
 
 #include <hip/hip_ext.h>
 
@@ -225,9 +226,9 @@ __device__ __forceinline__ float scaled_weights(const f32x4 s0, const f32x4 s1, 
 // kSteps: 32-key steps of a round that are loaded, 4, or 2 for a split of at most 64 keys.
 // kOnce: non-temporal page loads (see kOnceBytes).
 template <int G, bool kOnce, int kSteps>
-__device__ __forceinline__ void attend8(const AttnArgs& early_args, const WorkItem& wi, WorkLds& sm) {
+__device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds& sm) {
   constexpr int kLate8 = 5 * 8;
-  AttnArgs a = early_args;
+  AttnArgs8 a = early_args;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));   // what comes from the thread id stays inside this instance
   const int lane = tid & 63;
@@ -490,7 +491,7 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
     const int32_t* work, const void* q, const void* layer_base, const uint8_t* scales, const int32_t part_off,
     const float scale, const LateArgs) {
   __shared__ WorkLds sm;
-  AttnArgs a;
+  AttnArgs8 a;
   a.q = q;
   a.layer_base = layer_base;
   a.scales = scales;
@@ -514,13 +515,93 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
   if (path_word & kPathOnce)
     attend8<1, true, 4>(a, wi, sm);
   else if (wi.n_tok > 4)
-    attend8<4, false, 4>(a, wi, sm);
+    few_keys ? attend8<4, false, 2>(a, wi, sm) : attend8<4, false, 4>(a, wi, sm);
   else if (wi.n_tok > 2)
     few_keys ? attend8<2, false, 2>(a, wi, sm) : attend8<2, false, 4>(a, wi, sm);
   else
     few_keys ? attend8<1, false, 2>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
 }
 static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "attend8 reads the last argument there");
+
+// ------------------------------------------------------------------------------------------
+// merge of tokens with many split results
+// ------------------------------------------------------------------------------------------
+// A wavefront per token and head takes 0.9 us for every 16 split results behind the first (29 us for the 512 of a history
+// of 131072 tokens: two workgroups read 2 MB in turn).  Here a workgroup per token and head: a token of more than
+// kLongParts results has them shared out among 16 wavefronts, 16 at a time, each with a maximum of its own, and the first
+// one joins the sixteen.  Tokens of fewer are merged by one wavefront as in every other launch, so that a token's bits do
+// not depend on what else is in the batch.
+constexpr int kLongWaves = 16;
+__global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint16_t* part_acc, const float* part_ml, void* out,
+                                                                    float* lse, const int32_t* n_parts,
+                                                                    const int32_t* part_off) {
+  __shared__ f32x4 os[kLongWaves][64];
+  __shared__ float bigs[kLongWaves], totals[kLongWaves];
+  const MergeArgs a = {part_acc, part_ml, out, lse, n_parts, part_off};
+  const int tok = blockIdx.x / kHeads, h = blockIdx.x % kHeads;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int np = ((DescPtr)n_parts)[tok];
+  const size_t base = (size_t)((DescPtr)part_off)[tok];
+  if (np <= kLongParts) {
+    if (wv == 0) merge_any(a, base, np, tok, h, lane);
+    return;
+  }
+  const int i = lane & 15, q = lane >> 4;
+  const char* ml = (const char*)(part_ml + (base * kHeads + h) * 4);
+  const char* acc = (const char*)(part_acc + (base * kHeads + h) * kDim);
+  constexpr uint32_t kMlStride = kHeads * 4 * sizeof(float), kAccStride = kHeads * kDim * sizeof(uint16_t);
+  const float ninf = -__builtin_inff();
+  float big = ninf;
+  for (int p0 = 16 * wv; p0 < np; p0 += 16 * kLongWaves)
+    big = fmaxf(big, *(const float*)(ml + (size_t)min(p0 + i, np - 1) * kMlStride));
+  big = lanes16_max(big);
+  float total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 16 * wv; p0 < np; p0 += 16 * kLongWaves) {
+    const f32x4 w = *(const f32x4*)(ml + (size_t)min(p0 + i, np - 1) * kMlStride);
+    u32x2 x[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      x[u] = __builtin_nontemporal_load((const u32x2*)(acc + (size_t)min(p0 + u, np - 1) * kAccStride + (uint32_t)lane * 8u));
+    const bool live = p0 + i < np && w[0] != ninf;
+    const float wgt = live ? fast_exp2(w[0] - big) : 0.f;
+    total += wgt * (live ? w[1] : 0.f);
+    const int ex = (int32_t)(__float_as_uint(w[2]) << (24 - 8 * q)) >> 24;
+    const float ws = __builtin_amdgcn_ldexpf(wgt, ex - 14);
+    static_for<16>([&](auto u) {
+      const float wu = __uint_as_float(
+          __builtin_amdgcn_update_dpp(0, __float_as_uint(ws), kRowBcast0 + u.value, 0xf, 0xf, false));
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float lo, hi;
+        unpack_f16(x[u.value][k], lo, hi);
+        o[2 * k] = __builtin_fmaf(wu, lo, o[2 * k]);
+        o[2 * k + 1] = __builtin_fmaf(wu, hi, o[2 * k + 1]);
+      }
+    });
+  }
+  os[wv][lane] = (f32x4){o[0], o[1], o[2], o[3]};
+  total = lanes16_sum(total);
+  if (lane == 0) bigs[wv] = big, totals[wv] = total;
+  __syncthreads();
+  if (wv != 0) return;
+  const float mine = bigs[i];
+  const float top = lanes16_max(mine);
+  const float wgt = mine == ninf ? 0.f : fast_exp2(mine - top);
+  const float sum = lanes16_sum(wgt * totals[i]);
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  static_for<kLongWaves>([&](auto u) {
+    const float wu = __uint_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_uint(wgt), kRowBcast0 + u.value, 0xf, 0xf, false));
+    const f32x4 part = os[u.value][lane];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = __builtin_fmaf(wu, part[k], r[k]);
+  });
+  const float inv = 1.f / sum;
+  const u32x2 packed = {pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv)};
+  *(u32x2*)((uint16_t*)out + ((size_t)tok * kHeads + h) * kDim + 4 * lane) = packed;
+  if (lse && lane == 0)
+    lse[(size_t)tok * kHeads + h] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
 
 // ------------------------------------------------------------------------------------------
 // launches
@@ -552,7 +633,7 @@ hipError_t launch_gather_inline8(Layer8 layer, const GatherRuns& runs, int32_t n
   return hipGetLastError();
 }
 
-hipError_t launch_attention_work8(const AttnArgs& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
+hipError_t launch_attention_work8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
   if (a.n_work <= 0 || a.n_q <= 0) return hipErrorInvalidValue;
   const LateArgs late = {a.part_acc, a.part_ml, a.tables, a.write_through};
   const int32_t part_off = (int32_t)(a.part_off - a.work);   // of one descriptor
@@ -561,6 +642,17 @@ hipError_t launch_attention_work8(const AttnArgs& a, hipStream_t s, hipEvent_t s
                           part_off, a.scale, late);
   else
     attn8_kernel<<<a.n_work, 256, 0, s>>>(a.work, a.q, a.layer_base, a.scales, part_off, a.scale, late);
+  return hipGetLastError();
+}
+
+hipError_t launch_merge8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
+  if (a.max_parts <= kLongParts) return launch_merge_append(a, nullptr, s, start, stop);
+  if (a.n_q <= 0) return hipErrorInvalidValue;
+  if (start || stop)
+    hipExtLaunchKernelGGL(merge_long_kernel, dim3(kHeads * a.n_q), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc,
+                          a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
+  else
+    merge_long_kernel<<<kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
   return hipGetLastError();
 }
 

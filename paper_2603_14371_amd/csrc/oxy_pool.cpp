@@ -68,7 +68,7 @@ struct StepKey {
   float scale = 0.f;
   int32_t layer_begin = 0, layer_end = 0, mode = 0;   // mode: 0 separate, 1 fused, 2 folded
   int32_t n_work = 0, n_tokens = 0, n_fresh = 0, off_work = 0, off_tables = 0, off_part_off = 0,
-          off_n_parts = 0, write_through = 0;
+          off_n_parts = 0, write_through = 0, long_merge = 0;
   bool operator==(const StepKey& o) const {
     return d_base == o.d_base && k_new == o.k_new && v_new == o.v_new && q == o.q &&
            out == o.out && lse == o.lse && kv_stride == o.kv_stride && q_stride == o.q_stride &&
@@ -76,13 +76,14 @@ struct StepKey {
            layer_end == o.layer_end && mode == o.mode && n_work == o.n_work &&
            n_tokens == o.n_tokens && n_fresh == o.n_fresh && off_work == o.off_work && off_tables == o.off_tables &&
            off_part_off == o.off_part_off && off_n_parts == o.off_n_parts &&
-           write_through == o.write_through;
+           write_through == o.write_through && long_merge == o.long_merge;
   }
   // same number and kernels of launches in the same order: an instantiated graph can be updated
   // in place from a recording of the other
   bool same_topology(const StepKey& o) const {
     return layer_end - layer_begin == o.layer_end - o.layer_begin && mode == o.mode &&
-           oxy::merge_heads(n_tokens) == oxy::merge_heads(o.n_tokens) && (n_fresh > 0) == (o.n_fresh > 0);
+           oxy::merge_heads(n_tokens) == oxy::merge_heads(o.n_tokens) && (n_fresh > 0) == (o.n_fresh > 0) &&
+           long_merge == o.long_merge;
   }
 };
 struct StepGraph {
@@ -125,6 +126,7 @@ struct oxy_batch {
   int32_t n_launch = 0;   // records rounded up to a multiple of 64 with padding records: the grid
   int32_t n_fresh = 0;    // blocks of items whose own-phase tiles read k_new / v_new (folded append)
   int32_t off_fresh = 0;
+  int32_t max_parts = 0;  // most split results of a token
   bool decodes = false;           // some item has <= 2 new tokens
   bool append_foldable = false;   // every item has <= 2 new tokens or an empty own history
   // word offsets inside the descriptor
@@ -245,13 +247,44 @@ hipError_t append_rows(const oxy_pool* p, int32_t layer, const void* k_new, cons
   if (p->kv8) return oxy::launch_append8(k_new, v_new, d_slots, n_tokens, layer8(p, layer), s);
   return oxy::launch_append(k_new, v_new, d_slots, n_tokens, layer_base(p, layer), s);
 }
-hipError_t attention_work(const oxy_pool* p, const oxy::AttnArgs& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
+hipError_t attention_work(const oxy_pool* p, const oxy::AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
   return p->kv8 ? oxy::launch_attention_work8(a, s, start, stop) : oxy::launch_attention_work(a, s, start, stop);
 }
-hipError_t attention(const oxy_pool* p, const oxy::AttnArgs& a, hipStream_t s) {
+hipError_t attention(const oxy_pool* p, const oxy::AttnArgs8& a, hipStream_t s) {
   if (!p->kv8) return oxy::launch_attention(a, s);
   const hipError_t e = oxy::launch_attention_work8(a, s, nullptr, nullptr);
-  return e != hipSuccess ? e : oxy::launch_merge_append(a, nullptr, s);
+  return e != hipSuccess ? e : oxy::launch_merge8(a, s, nullptr, nullptr);
+}
+
+int32_t writes_through(const oxy_batch* b) {
+  const bool mixed = b->decodes && b->n_launch > 256;
+  return b->n_partials > (mixed ? oxy::kWriteThroughMixed : oxy::kWriteThroughParts);
+}
+
+oxy::AttnArgs8 attn_args(const oxy_pool* p, const oxy_batch* b, int32_t layer, const void* q, void* out,
+                        float* lse, float scale) {
+  const DescSlot& ds = p->slots[b->slot];
+  const int32_t* d = (const int32_t*)ds.d_base;
+  oxy::AttnArgs8 a;
+  a.layer_base = layer_base(p, layer);
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.work = d + b->off_work;
+  a.tables = d + b->off_tables;
+  a.part_off = d + b->off_part_off;
+  a.n_parts = d + b->off_n_parts;
+  a.part_acc = (uint16_t*)(ds.d_base + p->acc_offset);
+  a.part_ml = (float*)(ds.d_base + p->ml_offset);
+  a.n_work = b->n_launch;
+  a.n_q = b->n_tokens;
+  a.scale = scale;
+  a.write_through = writes_through(b);
+  a.k_new = a.v_new = nullptr;
+  a.d_slots = nullptr;
+  a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
+  a.max_parts = b->max_parts;
+  return a;
 }
 
 }  // namespace
@@ -643,9 +676,12 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
     groups.reserve(16);
     // How an item's own phase is cut, from the item alone.
     struct OwnCut {
-      bool causal, streams, fresh, short_chunk;
+      bool causal, streams, fresh, short_chunk, by_width;
       int32_t n_new, tile, split;   // new tokens, query tokens per work item, keys per split
     };
+    // In 8 bits a chunk's keys are in the pool when the work items run (appends quantise in a launch of their own), so
+    // its own phase is an item like any other: one split, as many tokens as share an item of its prefix.
+    int32_t chunk_tile8 = 8;
     auto own_cut = [&](const Plan& pl) {
       OwnCut o;
       o.n_new = pl.new_len - pl.old_len;
@@ -659,6 +695,12 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
       o.tile = o.streams ? 2 : o.short_chunk ? 8 : tile_tok_for(pl.new_len);
       o.split = o.streams ? stream_split_for(c, pl.new_len)
                           : o.short_chunk ? 32 : tile_split_for(c, pl.new_len);
+      o.by_width = p->kv8 && o.short_chunk;
+      if (o.by_width) {
+        o.tile = chunk_tile8;
+        o.split = 64;
+      }
+      if (p->kv8) o.fresh = o.short_chunk = false;
       return o;
     };
     for (const Plan& pl : plan) {
@@ -697,12 +739,18 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
     int32_t width = 8;
     {
       int64_t other = 0, pairs = 0, by4 = 0, by8 = 0, limited = 0, for_pairs = 512;
+      int64_t more_by2 = 0, more_by4 = 0;   // own items of chunks in 8 bits when cut narrower than 8
       for (const Plan& pl : plan) {
         const OwnCut o = own_cut(pl);
         for (int32_t t0 = 0; t0 < o.n_new; t0 += o.tile) {
           const int32_t n = std::min(o.tile, o.n_new - t0);
           const int32_t hi = o.causal ? pl.old_len + t0 + n : pl.new_len;
           other += (hi + o.split - 1) / o.split;
+        }
+        if (o.by_width) {
+          const int32_t by_8 = (o.n_new + 7) / 8;
+          more_by2 += (o.n_new + 1) / 2 - by_8;
+          more_by4 += (o.n_new + 3) / 4 - by_8;
         }
       }
       for (const Group& g : groups) {
@@ -721,10 +769,11 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
         return fail(OXY_ERR_WORKSPACE, "batch_build: %lld work items > max_work_items %d",
                     (long long)(limited + other), c.max_work_items);
       const int64_t resident = std::min<int64_t>(512, c.max_work_items);
-      if (pairs + other <= std::min(for_pairs, resident))
+      if (pairs + other + more_by2 <= std::min(for_pairs, resident))
         width = 2;
-      else if (by4 + other <= resident || (by8 == by4 && by4 + other <= c.max_work_items))
+      else if (by4 + other + more_by4 <= resident || (by8 == by4 && by4 + other + more_by4 <= c.max_work_items))
         width = 4;
+      chunk_tile8 = width;
     }
     for (const Group& g : groups) {
       const Prefix& px = *g.px;
@@ -1035,6 +1084,7 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
   b->n_work = n_work - (int32_t)wide_tiles.size();
   b->n_partials = (int32_t)n_partials;
   b->decodes = decodes;
+  for (int32_t n : n_parts) b->max_parts = std::max(b->max_parts, n);
   b->append_foldable = foldable;
   // Sections in the order work | slots | part_off | n_parts | fresh runs | token lists | tables: the block
   // tables, whose size changes whenever a stream takes a new block, come last, so that the
@@ -1160,38 +1210,6 @@ int32_t oxy_stream_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
   return OXY_OK;
 }
 
-namespace {
-int32_t writes_through(const oxy_batch* b) {
-  const bool mixed = b->decodes && b->n_launch > 256;
-  return b->n_partials > (mixed ? oxy::kWriteThroughMixed : oxy::kWriteThroughParts);
-}
-
-oxy::AttnArgs attn_args(const oxy_pool* p, const oxy_batch* b, int32_t layer, const void* q, void* out,
-                        float* lse, float scale) {
-  const DescSlot& ds = p->slots[b->slot];
-  const int32_t* d = (const int32_t*)ds.d_base;
-  oxy::AttnArgs a;
-  a.layer_base = layer_base(p, layer);
-  a.q = q;
-  a.out = out;
-  a.lse = lse;
-  a.work = d + b->off_work;
-  a.tables = d + b->off_tables;
-  a.part_off = d + b->off_part_off;
-  a.n_parts = d + b->off_n_parts;
-  a.part_acc = (uint16_t*)(ds.d_base + p->acc_offset);
-  a.part_ml = (float*)(ds.d_base + p->ml_offset);
-  a.n_work = b->n_launch;
-  a.n_q = b->n_tokens;
-  a.scale = scale;
-  a.write_through = writes_through(b);
-  a.k_new = a.v_new = nullptr;
-  a.d_slots = nullptr;
-  a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
-  return a;
-}
-}  // namespace
-
 int32_t oxy_mixed_attention(oxy_pool* p, const oxy_batch* b, int32_t layer, const void* q,
                             void* out, float* lse, float scale, void* hip_stream) {
   if (!p || !b || b->pool != p || !q || !out || p->host_only)
@@ -1217,7 +1235,7 @@ int32_t oxy_mixed_attention_static(oxy_pool* p, const oxy_batch* b, int32_t laye
     return fail(OXY_ERR_WORKSPACE,
                 "mixed_attention_static: the batch has %d split results, the static buffer holds %d",
                 b->n_partials, oxy::kStaticMaxPartials);
-  oxy::AttnArgs a = attn_args(p, b, layer, q, out, lse, scale);
+  oxy::AttnArgs8 a = attn_args(p, b, layer, q, out, lse, scale);
   hipError_t e = oxy::static_scratch(&a.part_acc, &a.part_ml);
   if (e != hipSuccess) return hip_fail(e, "mixed_attention_static: static buffer");
   e = attention(p, a, (hipStream_t)hip_stream);
@@ -1277,7 +1295,7 @@ int32_t issue_step(const StepCall& c, hipStream_t s) {
     hipEvent_t ev[4] = {nullptr, nullptr, nullptr, nullptr};
     if (c.events)
       for (int j = 0; j < 4; ++j) ev[j] = (hipEvent_t)c.events[4 * i + j];
-    oxy::AttnArgs a =
+    oxy::AttnArgs8 a =
         attn_args(p, b, layer, (const char*)c.q + (size_t)layer * c.q_layer_stride,
                   (char*)c.out + (size_t)layer * c.q_layer_stride,
                   c.lse ? (float*)((char*)c.lse + (size_t)layer * c.lse_layer_stride) : nullptr,
@@ -1300,7 +1318,7 @@ int32_t issue_step(const StepCall& c, hipStream_t s) {
       fr.runs = d_desc + b->off_fresh;
       e = oxy::launch_merge_append(a, &fr, s, ev[2], ev[3]);
     } else {
-      e = oxy::launch_merge_append(a, nullptr, s, ev[2], ev[3]);
+      e = p->kv8 ? oxy::launch_merge8(a, s, ev[2], ev[3]) : oxy::launch_merge_append(a, nullptr, s, ev[2], ev[3]);
     }
     if (e != hipSuccess) return hip_fail(e, "step_layers: merge");
   }
@@ -1337,6 +1355,7 @@ int32_t replay_step(const StepCall& c, hipStream_t s) {
   key.off_part_off = b->off_part_off;
   key.off_n_parts = b->off_n_parts;
   key.write_through = writes_through(b);
+  key.long_merge = p->kv8 && b->max_parts > oxy::kLongParts;
   const uint64_t now = ++p->graph_clock;
   StepGraph* hit = nullptr;
   for (StepGraph& g : p->graphs)

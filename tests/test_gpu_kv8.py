@@ -329,7 +329,7 @@ def _only(prefixes, chunks, requests, take):
     items += [(sid, n, tag) for sid, h, n, tag in reqs]
     w = _workload("only", 4, 1, 4000, b.trace)
     data = synth.DataSource(4)
-    gw = GpuWorld(w, data, kv8=True, max_q_tokens=2048, max_append_tokens=4096, max_partials=40000)
+    gw = GpuWorld(w, data, kv8=True, max_q_tokens=2048, max_append_tokens=32768, max_partials=40000)
     gw.run(w["trace"])
 
     def stitched(recipe, layer, what, n):
@@ -512,3 +512,27 @@ def test_another_stream():
             gw.close()
     for layer in outs[0]:
         assert np.array_equal(outs[0][layer], outs[1][layer])
+
+
+@pytest.mark.parametrize("hist", [4200, 9001])
+def test_long_histories_are_merged_by_many(hist):
+    """Tokens of more than 32 split results take another merge; beside them, tokens of fewer give the bits that they
+    give in any other launch."""
+    b = _TraceBuilder()
+    pid = b.prefix(300)
+    d, e, a = b.stream(pid, DECODE), b.stream(-1, DECODE), b.stream(pid, ACTION)
+    b.step([(d, hist), (e, 700)], attend=False)
+    b.step([(a, 5), (d, 1), (e, 2)])
+    b.step([(d, 2)])
+    w = _workload("long", 11, 1, 800, b.trace)
+    gw, ow = run_both8(w, poison=True, max_partials=4096, stream_split_tokens=32)
+    gw.close()
+    gw, ow = run_both8(w, poison=True)
+    gw.close()
+
+
+def test_short_tokens_beside_a_long_one_give_the_same_bits():
+    me = (0, 700, 1, 7)
+    alone = _only([900], [], [me], 7)
+    beside = _only([900], [(0, 13, 1)], [(0, 20000, 1, 2), me], 7)
+    assert np.array_equal(alone[0], beside[0]) and np.array_equal(alone[1], beside[1])
