@@ -185,9 +185,19 @@ __global__ __launch_bounds__(256) void gather8_kernel(const char* __restrict__ b
 // ------------------------------------------------------------------------------------------
 // attention work items
 // ------------------------------------------------------------------------------------------
-typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+// largest of lanes n, n+16, n+32, n+48
+__device__ __forceinline__ uint32_t rows4_largest(uint32_t x) {
+  x = swap16_max(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return larger(b[0], b[1]);
+}
+__device__ __forceinline__ f32x4 mfma16_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 // eight codes (two words) times a power of two -> eight bf16, one 16-byte matrix operand
-__device__ __forceinline__ u32x4 operand_of(const uint32_t lo, const uint32_t hi, const float scale) {
+__device__ __forceinline__ u32x4 bf16_operand(const uint32_t lo, const uint32_t hi, const float scale) {
   u32x4 r;
   r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
   r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
@@ -195,39 +205,66 @@ __device__ __forceinline__ u32x4 operand_of(const uint32_t lo, const uint32_t hi
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   return r;
 }
+// eight codes -> eight fp16 (every code is an fp16 number)
+__device__ __forceinline__ u32x4 f16_operand(const uint32_t lo, const uint32_t hi) {
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
+  return r;
+}
 // first `left` of four bytes
 __device__ __forceinline__ uint32_t byte_mask(const int left) {
   return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 }
-// P = 2^(sl2 * s - m) of a lane's eight dot products; what meets the value codes is P times the values' scales, as
-// hi + lo bf16 (see softmax_weights).  Returns the sum of P itself.
-__device__ __forceinline__ float scaled_weights(const f32x4 s0, const f32x4 s1, const float sl2, const float m,
-                                                const float (&vs)[8], u32x4& hi, u32x4& lo) {
-  float w[8], sum = 0.f;
+// P = 2^(sl2 * s - m) of a lane's eight dot products; what meets the value codes is P times its key's factor, as fp16.
+// Returns the sum of P itself.
+__device__ __forceinline__ float weights8(const f32x4 s0, const f32x4 s1, const float sl2, const float m,
+                                          const float (&factor)[8], u32x4& w) {
+  float p[8], sum = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = fast_exp2(__builtin_fmaf(e < 4 ? s0[e & 3] : s1[e & 3], sl2, -m));
-    sum += p;
-    w[e] = p * vs[e];
+    p[e] = fast_exp2(__builtin_fmaf(e < 4 ? s0[e & 3] : s1[e & 3], sl2, -m));
+    sum += p[e];
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    hi[i] = pack_bf16(w[2 * i], w[2 * i + 1]);
-    lo[i] = pack_bf16(w[2 * i] - __uint_as_float(hi[i] << 16), w[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
-  }
+  for (int i = 0; i < 4; ++i) w[i] = pack_f16(p[2 * i] * factor[2 * i], p[2 * i + 1] * factor[2 * i + 1]);
   return sum;
 }
 
-// One work item: up to 2*G query tokens against one split of a KV source, in rounds of 128 keys, as `attend` in
-// oxy_kernels.hip: wavefront w takes the logits of keys 32w..32w+31 and contracts all 128 for dims 64w..64w+63.  A
-// round's pages are 32 + 32 registers of codes (64 + 64 in bf16).  A K operand is converted once for all groups, with
-// its rows' exponents as the conversion's scale; the V operands with scale 1, since a lane's eight codes are of eight
-// keys: their exponents go into P.  A row's arithmetic does not depend on G or on the other rows.
-// kSteps: 32-key steps of a round that are loaded, 4, or 2 for a split of at most 64 keys.
+// LDS of a work item: nothing of K and V, only what the four wavefronts exchange.
+struct __align__(16) WorkLds8 {
+  u32x4 q[kMaxGroups][8][64];      // query fragments, the same for all wavefronts
+  u32x4 p[4 * kMaxGroups][64];     // [32-key step][group]: P of a round's keys
+  float mx[kMaxGroups][16][4];     // largest logit of a row among each wavefront's keys
+  int slot[2 * kMaxGroups];        // split result of each token
+  int top[4];                      // largest exponent byte of each wavefront's values
+  float ls[kMaxGroups][64][4];     // sum of a lane's P over each wavefront's keys
+};
+
+// One work item: up to 2*G query tokens against one split of a KV source, in rounds of kSub * 128 keys, as `attend` in
+// oxy_kernels.hip: wavefront w takes the logits of its kSub 32-key steps and contracts all keys of the round for dims
+// 64w..64w+63.  A round of 128 keys is 32 + 32 registers of codes (64 + 64 in bf16).  A K operand is converted once
+// for all groups, with its rows' exponents as the conversion's scale.  A lane's eight V codes are of eight keys, so
+// theirs go into P.
+//
+// P travels as ONE fp16 number (hi + lo bf16 in a bf16 cache: twice the products, the LDS traffic and the packing).
+// A single bf16 would be too coarse (2^-8 of it at most, for queries that see few keys); fp16 has 2^-11, like the split
+// results behind it, and e4m3 codes are fp16 numbers.  Its range: with `vref` the largest exponent of the values seen so
+// far, P (at most 2^8) times 2^(exponent - vref + 7) is at most 2^15; what contributes 2^-21 of the largest value or more
+// keeps 11 bits, below that the error is 2^-32 of the largest value.  acc is in units of 2^(vref - 7) and rescaled
+// when vref grows, which a power of two does exactly.
+//
+// A row's arithmetic does not depend on G or on the other rows.
+// kSteps: 32-key steps of a round that are loaded: 4 * kSub, or 2 for a split of at most 64 keys.
+// kSub 2 (own pages of more than 128 keys in a split, one group): all 256 keys' pages in flight at once.
 // kOnce: non-temporal page loads (see kOnceBytes).
 template <int G, bool kOnce, int kSteps>
-__device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds& sm) {
-  constexpr int kLate8 = 5 * 8;
+__device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
+  constexpr int kLate8 = 5 * 8, kSub = kSteps == 8 ? 2 : 1;
+  constexpr int kRound = 4 * kSub;   // steps
+  static_assert(kSteps <= 4 * kMaxGroups / G, "P of a round");
   AttnArgs8 a = early_args;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));   // what comes from the thread id stays inside this instance
@@ -240,56 +277,73 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
   const char* __restrict__ base = (const char*)a.layer_base;
   const uint8_t* __restrict__ scales = a.scales;
   const int nsteps = (wi.kv_end - wi.kv_begin + 31) >> 5;
-  const int rounds = (nsteps + 3) >> 2;
+  const int rounds = (nsteps + kRound - 1) / kRound;
   const int npg = ((wi.kv_end + 15) >> 4) - (wi.kv_begin >> 4);
 
-  u32x4 kr[8];            // kr[2jj+hf]: K chunk (jj, hf) of this wavefront's 32 keys
+  u32x4 kr[kSub][8];      // kr[u][2jj+hf]: K chunk (jj, hf) of this wavefront's step u
   u32x4 vr[kSteps][2];    // vr[s][cp]: V chunk cp of this wavefront's 64 dims, step s of the round
-  uint32_t ke = 0;        // exponents of this lane's keys of the first product (hf = 0, 1)
-  u32x2 ve = {0, 0};      // of the eight keys whose logits it receives
+  uint32_t ke[kSub];      // exponents of this lane's keys of the first product (hf = 0, 1)
+  u32x2 ve[kSub];         // of the eight keys whose logits it receives
   auto page_load = [](const char* p) {
     if constexpr (kOnce) return __builtin_nontemporal_load((const u32x4*)p);
     return *(const u32x4*)p;
   };
   // A step past the split's end re-reads a page of the split; its logits are masked and its V operands are zeros.
-  auto load_k_of = [&](const int blk_a, const int blk_b) {
+  auto load_k_of = [&](const int u, const int blk_a, const int blk_b) {
     int off = (g * 8 + (n & 7)) * 16, off_k = 2 * (n & 7), off_v = kPage + 8 * (g & 1);
     asm volatile("" : "+v"(off), "+v"(off_k), "+v"(off_v));
-    ke = *(const uint16_t*)(scales + (size_t)((n >> 3) ? blk_b : blk_a) * kScaleBytes8 + off_k);
-    ve = *(const u32x2*)(scales + (size_t)((g >> 1) ? blk_b : blk_a) * kScaleBytes8 + off_v);
+    ke[u] = *(const uint16_t*)(scales + (size_t)((n >> 3) ? blk_b : blk_a) * kScaleBytes8 + off_k);
+    ve[u] = *(const u32x2*)(scales + (size_t)((g >> 1) ? blk_b : blk_a) * kScaleBytes8 + off_v);
     const char* p = base + (size_t)((n >> 3) ? blk_b : blk_a) * kBlockBytes8 + off;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) kr[i] = page_load(p + i * 512);
+    for (int i = 0; i < 8; ++i) kr[u][i] = page_load(p + i * 512);
   };
-  auto load_v_of = [&](const i32x8 blks) {
+  auto load_v_of = [&](const int s, const int blk_a, const int blk_b) {
     int off = kPageBytes8 + v8_chunk_offset(wv, 0, g & 1, n);
     asm volatile("" : "+v"(off));
+    const char* p = base + (size_t)((g >> 1) ? blk_b : blk_a) * kBlockBytes8 + off;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const char* p = base + (size_t)((g >> 1) ? blks[2 * s + 1] : blks[2 * s]) * kBlockBytes8 + off;
-#pragma unroll
-      for (int cp = 0; cp < 2; ++cp) vr[s][cp] = page_load(p + cp * 512);
-    }
+    for (int cp = 0; cp < 2; ++cp) vr[s][cp] = page_load(p + cp * 512);
   };
+  // The block ids of the first 16 pages are in the record (no dependent load in front of the first pages), those of
+  // later rounds in the block table.
+  constexpr int kInlineRounds = kWorkInlinePages / (2 * kRound);
   auto load_k = [&](const int round) {
-    if (round < 2) {
-      const DescPtr id = wi.rec + 16 + 8 * round + 2 * wv;
-      load_k_of(id[0], id[1]);
+    if (round < kInlineRounds) {
+      const DescPtr id = wi.rec + 16 + 2 * kRound * round + 2 * kSub * wv;
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) load_k_of(u, id[2 * u], id[2 * u + 1]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
-      const int pi = 8 * round + 2 * wv;
-      load_k_of(ids[min(pi, npg - 1)], ids[min(pi + 1, npg - 1)]);
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) {
+        const int pi = 2 * kRound * round + 2 * (kSub * wv + u);
+        load_k_of(u, ids[min(pi, npg - 1)], ids[min(pi + 1, npg - 1)]);
+      }
     }
   };
   auto load_v = [&](const int round) {
-    if (round < 2) {
-      load_v_of(*(DescPtr8)(wi.rec + 16 + 8 * round));
+    if (round < kInlineRounds) {
+      const DescPtr8 id = (DescPtr8)(wi.rec + 16 + 2 * kRound * round);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) load_v_of(s, id[s / 4][2 * (s % 4)], id[s / 4][2 * (s % 4) + 1]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
-      i32x8 blks;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) blks[i] = ids[min(8 * round + i, npg - 1)];
-      load_v_of(blks);
+      for (int s = 0; s < kSteps; ++s) {
+        const int pi = 2 * kRound * round + 2 * s;
+        load_v_of(s, ids[min(pi, npg - 1)], ids[min(pi + 1, npg - 1)]);
+      }
+    }
+  };
+
+  auto load_first_v = [&]() {   // with the ids that came with the record
+    i32x8 more = wi.pages;
+    if constexpr (kSteps > 4) more = ((DescPtr8)wi.rec)[3];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const i32x8 ids = s < 4 ? wi.pages : more;
+      load_v_of(s, ids[2 * (s % 4)], ids[2 * (s % 4) + 1]);
     }
   };
 
@@ -318,11 +372,13 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       }
     };
     if (kSteps == 2 && wv >= 2) {
-      load_v_of(wi.pages);
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) ke[u] = 0, ve[u] = (u32x2){0, 0};
+      load_first_v();
       store_q();
     } else {
-      load_k_of(wi.rec[16 + 2 * wv], wi.rec[17 + 2 * wv]);
-      load_v_of(wi.pages);
+      load_k(0);
+      load_first_v();
       store_q();
     }
   }
@@ -331,6 +387,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
 
   float m[G], l[G];   // reference max (scaled log2 domain) of this lane's row, and the sum of P
   f32x4 acc[G][4];    // over this wavefront's keys; acc[r][c][e] = dim 64w + 16g + 4e + c
+  int vref = 1;       // exponent byte that acc's unit goes by
 #pragma unroll
   for (int r = 0; r < G; ++r) {
     m[r] = ninf;
@@ -344,56 +401,70 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     int lane_now = tid & 63;
     asm volatile("" : "+v"(lane_now));
     const int lane = lane_now, n = lane & 15, g = lane >> 4, sub = n >> 3;
-    const int pos = wi.kv_begin + 32 * (4 * round + wv);
-    const int left = wi.kv_end - pos;
-    const bool need_mask = (kLast && left < 32) || pos + 31 > wi.q0;
-    f32x4 s0[G], s1[G];
-    float vs[8];
+    f32x4 s0[kSub][G], s1[kSub][G];
+    int vb[kSub][8];   // exponent bytes of this lane's values, 0 for keys that are not there
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vs[e] = 0.f;
-    if (kSteps == 4 || wv < 2) {
+    for (int u = 0; u < kSub; ++u) {
+      const int pos = wi.kv_begin + 32 * (kRound * round + kSub * wv + u);
+      const int left = wi.kv_end - pos;
+      const bool need_mask = (kLast && left < 32) || pos + 31 > wi.q0;
+      if (kSteps != 2 || wv < 2) {
 #pragma unroll
-      for (int r = 0; r < G; ++r) s0[r] = s1[r] = (f32x4){0.f, 0.f, 0.f, 0.f};
-      const float ks0 = scale_of(ke & 0xffu), ks1 = scale_of(ke >> 8);
+        for (int r = 0; r < G; ++r) s0[u][r] = s1[u][r] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        const float ks0 = scale_of(ke[u] & 0xffu), ks1 = scale_of(ke[u] >> 8);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const u32x4 a0 = kr[2 * (j >> 1)], a1 = kr[2 * (j >> 1) + 1];
-        const u32x4 k0 = operand_of(a0[2 * (j & 1)], a0[2 * (j & 1) + 1], ks0);
-        const u32x4 k1 = operand_of(a1[2 * (j & 1)], a1[2 * (j & 1) + 1], ks1);
+        for (int j = 0; j < 8; ++j) {
+          const u32x4 a0 = kr[u][2 * (j >> 1)], a1 = kr[u][2 * (j >> 1) + 1];
+          const u32x4 k0 = bf16_operand(a0[2 * (j & 1)], a0[2 * (j & 1) + 1], ks0);
+          const u32x4 k1 = bf16_operand(a1[2 * (j & 1)], a1[2 * (j & 1) + 1], ks1);
 #pragma unroll
-        for (int r = 0; r < G; ++r) {
-          const u32x4 q = sm.q[r][j][lane];
-          s0[r] = mfma16(k0, q, s0[r]);
-          s1[r] = mfma16(k1, q, s1[r]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) vs[e] = scale_of((ve[e >> 2] >> (8 * (e & 3))) & 0xffu);
-      if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
-        const int k0 = pos + 16 * (g >> 1) + 4 * (g & 1);
-#pragma unroll
-        for (int r = 0; r < G; ++r) {
-          const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s0[r][e] = e < end ? s0[r][e] : ninf;
-            s1[r][e] = 8 + e < end ? s1[r][e] : ninf;
+          for (int r = 0; r < G; ++r) {
+            const u32x4 q = sm.q[r][j][lane];
+            s0[u][r] = mfma16(k0, q, s0[u][r]);
+            s1[u][r] = mfma16(k1, q, s1[u][r]);
           }
         }
-        // the exponent byte of a slot that was never written may be anything: 0 * inf would poison a row
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vs[e] = (e < 4 ? e : 4 + e) < wi.kv_end - k0 ? vs[e] : 0.f;
+        for (int e = 0; e < 8; ++e) vb[u][e] = (int)((ve[u][e >> 2] >> (8 * (e & 3))) & 0xffu);
+        if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
+          const int k0 = pos + 16 * (g >> 1) + 4 * (g & 1);
+#pragma unroll
+          for (int r = 0; r < G; ++r) {
+            const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              s0[u][r][e] = e < end ? s0[u][r][e] : ninf;
+              s1[u][r][e] = 8 + e < end ? s1[u][r][e] : ninf;
+            }
+          }
+          // the exponent byte of a slot that was never written may be anything
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vb[u][e] = (e < 4 ? e : 4 + e) < wi.kv_end - k0 ? vb[u][e] : 0;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < G; ++r) s0[u][r] = s1[u][r] = (f32x4){ninf, ninf, ninf, ninf};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vb[u][e] = 0;
       }
-    } else {
-#pragma unroll
-      for (int r = 0; r < G; ++r) s0[r] = s1[r] = (f32x4){ninf, ninf, ninf, ninf};
     }
     {
       float mx[G];
 #pragma unroll
-      for (int r = 0; r < G; ++r) mx[r] = row_max8(s0[r], s1[r]) * sl2;
+      for (int r = 0; r < G; ++r) {
+        mx[r] = row_max8(s0[0][r], s1[0][r]);
+        if constexpr (kSub == 2) mx[r] = fmaxf(mx[r], row_max8(s0[kSub - 1][r], s1[kSub - 1][r]));
+        mx[r] *= sl2;
+      }
       const float mine = row_max4_each(mx);
       if (g < G) sm.mx[g][n][wv] = mine;
+      int top = 1;
+#pragma unroll
+      for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, vb[u][e]);
+      top = (int)rows4_largest((uint32_t)top);   // the same in all lanes of 16
+      if (lane == 0) sm.top[wv] = top;
     }
     __syncthreads();
     // online softmax with a reference that only moves by more than kGrow: see `attend`
@@ -404,6 +475,18 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       const f32x4 mw = *(const f32x4*)sm.mx[r][n];
       mx[r] = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3]));
       grow |= mx[r] > m[r] + kGrow;
+    }
+    const i32x4 tops = *(const i32x4*)sm.top;
+    const int top = __builtin_amdgcn_readfirstlane(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    if (top > vref) {   // wave-uniform; acc holds zeros in the first round
+      if (round > 0) {
+        const float down = __builtin_amdgcn_ldexpf(1.f, vref - top);
+#pragma unroll
+        for (int r = 0; r < G; ++r)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[r][c] *= down;
+      }
+      vref = top;
     }
     if (__any(grow)) {
 #pragma unroll
@@ -419,59 +502,62 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       }
     }
 #pragma unroll
-    for (int r = 0; r < G; ++r) {
-      u32x4 hi, lo;
-      l[r] += scaled_weights(s0[r], s1[r], sl2, (m[r] == ninf) ? 0.f : m[r], vs, hi, lo);
-      sm.p[wv][r][0][lane] = hi;
-      sm.p[wv][r][1][lane] = lo;
-      if constexpr (kLast) sm.ls[r][lane][wv] = l[r];
+    for (int u = 0; u < kSub; ++u) {
+      // 2^(exponent - vref + 7); nothing for a key that is not there
+      float factor[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) factor[e] = scale_of((uint32_t)max(vb[u][e] ? vb[u][e] - vref + 127 + 7 : 0, 0));
+#pragma unroll
+      for (int r = 0; r < G; ++r) {
+        u32x4 w;
+        l[r] += weights8(s0[u][r], s1[u][r], sl2, (m[r] == ninf) ? 0.f : m[r], factor, w);
+        sm.p[(kSub * wv + u) * G + r][lane] = w;
+        if constexpr (kLast)
+          if (u == kSub - 1) sm.ls[r][lane][wv] = l[r];
+      }
     }
     __builtin_amdgcn_sched_barrier(0);   // the next K chunks reuse kr[]
     if constexpr (!kLast) load_k(round + 1);
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
-    auto value_operands = [&](const int s, u32x4 (&v)[4]) {
+    auto contract = [&](const int s) {
+      u32x4 v[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = operand_of(vr[s][c >> 1][2 * (c & 1)], vr[s][c >> 1][2 * (c & 1) + 1], 1.f);
-    };
-    auto contract = [&](const u32x4 (&v)[4], const int s, const int r) {
-      const u32x4 hi = sm.p[s][r][0][lane], lo = sm.p[s][r][1][lane];
+      for (int c = 0; c < 4; ++c) v[c] = f16_operand(vr[s][c >> 1][2 * (c & 1)], vr[s][c >> 1][2 * (c & 1) + 1]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[r][c] = mfma16(v[c], hi, acc[r][c]);
+      for (int r = 0; r < G; ++r) {
+        const u32x4 w = sm.p[s * G + r][lane];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[r][c] = mfma16(v[c], lo, acc[r][c]);
+        for (int c = 0; c < 4; ++c) acc[r][c] = mfma16_f16(v[c], w, acc[r][c]);
+      }
     };
     if constexpr (!kLast) {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        u32x4 v[4];
-        value_operands(s, v);
-#pragma unroll
-        for (int r = 0; r < G; ++r) contract(v, s, r);
-      }
+      for (int s = 0; s < kSteps; ++s) contract(s);
       __builtin_amdgcn_sched_barrier(0);   // likewise vr[]
       load_v(round + 1);
       __builtin_amdgcn_sched_barrier(0);
     } else {
-      const int nv = nsteps - 4 * round;   // 1..4 steps
+      const int nv = nsteps - kRound * round;   // steps with keys
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
         if (s < nv) {
-          const int left_s = wi.kv_end - (wi.kv_begin + 32 * (4 * round + s));
+          const int left_s = wi.kv_end - (wi.kv_begin + 32 * (kRound * round + s));
           if (left_s < 32) {   // codes of slots beyond the end may be anything
             const int k0 = 16 * (g >> 1) + 4 * (g & 1);
             const uint32_t m0 = byte_mask(left_s - k0), m1 = byte_mask(left_s - k0 - 8);
 #pragma unroll
             for (int cp = 0; cp < 2; ++cp) vr[s][cp] &= (u32x4){m0, m1, m0, m1};
           }
-          u32x4 v[4];
-          value_operands(s, v);
-#pragma unroll
-          for (int r = 0; r < G; ++r) contract(v, s, r);
+          contract(s);
         }
 #pragma unroll
       for (int r = 0; r < G; ++r) {
         const int slot = sm.slot[2 * r + sub];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[r][c][e] = __builtin_amdgcn_ldexpf(acc[r][c][e], vref - 127 - 7);
         store_part<(G >= 4)>(a, wi, slot, acc[r], r, wv, lane);
         if (wv == r) {   // wave-uniform: the sums of the groups are shared out
           const f32x4 lw = *(const f32x4*)sm.ls[r][lane];
@@ -482,15 +568,15 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       }
     }
   };
-  if constexpr (kSteps == 4)
+  if constexpr (kSteps != 2)
     for (int round = 0; round + 1 < rounds; ++round) round_body(round, std::false_type());
-  round_body(kSteps == 4 ? rounds - 1 : 0, std::true_type());
+  round_body(kSteps != 2 ? rounds - 1 : 0, std::true_type());
 }
 
 __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_kernel(
     const int32_t* work, const void* q, const void* layer_base, const uint8_t* scales, const int32_t part_off,
     const float scale, const LateArgs) {
-  __shared__ WorkLds sm;
+  __shared__ WorkLds8 sm;
   AttnArgs8 a;
   a.q = q;
   a.layer_base = layer_base;
@@ -512,8 +598,12 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
   const int path_word = head[W_PATH];
   if ((path_word & kPathMask) == PATH_NOOP) return;
   const bool few_keys = wi.kv_end - wi.kv_begin <= 64;
-  if (path_word & kPathOnce)
-    attend8<1, true, 4>(a, wi, sm);
+  if (path_word & kPathAppends) {   // one or two tokens on their own pages
+    if (wi.kv_end - wi.kv_begin > 128)
+      path_word & kPathOnce ? attend8<1, true, 8>(a, wi, sm) : attend8<1, false, 8>(a, wi, sm);
+    else
+      path_word & kPathOnce ? attend8<1, true, 4>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
+  }
   else if (wi.n_tok > 4)
     few_keys ? attend8<4, false, 2>(a, wi, sm) : attend8<4, false, 4>(a, wi, sm);
   else if (wi.n_tok > 2)
@@ -527,79 +617,88 @@ static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "atten
 // merge of tokens with many split results
 // ------------------------------------------------------------------------------------------
 // A wavefront per token and head takes 0.9 us for every 16 split results behind the first (29 us for the 512 of a history
-// of 131072 tokens: two workgroups read 2 MB in turn).  Here a workgroup per token and head: a token of more than
-// kLongParts results has them shared out among 16 wavefronts, 16 at a time, each with a maximum of its own, and the first
-// one joins the sixteen.  Tokens of fewer are merged by one wavefront as in every other launch, so that a token's bits do
-// not depend on what else is in the batch.
-constexpr int kLongWaves = 16;
+// of 131072 tokens: two workgroups read 2 MB in turn).  Here a token of more than kLongParts results takes a workgroup for
+// each head and 64 dims: eight wavefronts share the results out, 64 at a time with everything in flight at once, each with
+// a maximum of its own, and the first one joins the eight.  Tokens of fewer are merged by one wavefront as in every
+// other launch, so that a token's bits do not depend on what else is in the batch.
+constexpr int kLongWaves = 8, kLongAhead = 16;   // a wavefront's loads: kLongAhead times four results of 128 bytes
 __global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint16_t* part_acc, const float* part_ml, void* out,
                                                                     float* lse, const int32_t* n_parts,
                                                                     const int32_t* part_off) {
-  __shared__ f32x4 os[kLongWaves][64];
+  __shared__ f32x4 os[kLongWaves][16];
   __shared__ float bigs[kLongWaves], totals[kLongWaves];
-  const MergeArgs a = {part_acc, part_ml, out, lse, n_parts, part_off};
-  const int tok = blockIdx.x / kHeads, h = blockIdx.x % kHeads;
+  const int tok = blockIdx.x / (4 * kHeads), h = (blockIdx.x >> 2) % kHeads, part = blockIdx.x & 3;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int np = ((DescPtr)n_parts)[tok];
   const size_t base = (size_t)((DescPtr)part_off)[tok];
   if (np <= kLongParts) {
-    if (wv == 0) merge_any(a, base, np, tok, h, lane);
+    if (wv == 0 && part == 0) merge_any({part_acc, part_ml, out, lse, n_parts, part_off}, base, np, tok, h, lane);
     return;
   }
-  const int i = lane & 15, q = lane >> 4;
+  const int i = lane & 15, p = lane >> 4;   // dims 64 * part + 4i..+3 of every fourth result
   const char* ml = (const char*)(part_ml + (base * kHeads + h) * 4);
-  const char* acc = (const char*)(part_acc + (base * kHeads + h) * kDim);
-  constexpr uint32_t kMlStride = kHeads * 4 * sizeof(float), kAccStride = kHeads * kDim * sizeof(uint16_t);
+  const char* acc = (const char*)(part_acc + (base * kHeads + h) * kDim + 64 * part + 4 * i);
+  constexpr size_t kMlStride = kHeads * 4 * sizeof(float), kAccStride = kHeads * kDim * sizeof(uint16_t);
   const float ninf = -__builtin_inff();
-  float big = ninf;
-  for (int p0 = 16 * wv; p0 < np; p0 += 16 * kLongWaves)
-    big = fmaxf(big, *(const float*)(ml + (size_t)min(p0 + i, np - 1) * kMlStride));
-  big = lanes16_max(big);
-  float total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 16 * wv; p0 < np; p0 += 16 * kLongWaves) {
-    const f32x4 w = *(const f32x4*)(ml + (size_t)min(p0 + i, np - 1) * kMlStride);
-    u32x2 x[16];
+  float big = ninf, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 4 * kLongAhead * wv; p0 < np; p0 += 4 * kLongAhead * kLongWaves) {
+    f32x4 w[kLongAhead];
+    u32x2 x[kLongAhead];
 #pragma unroll
-    for (int u = 0; u < 16; ++u)
-      x[u] = __builtin_nontemporal_load((const u32x2*)(acc + (size_t)min(p0 + u, np - 1) * kAccStride + (uint32_t)lane * 8u));
-    const bool live = p0 + i < np && w[0] != ninf;
-    const float wgt = live ? fast_exp2(w[0] - big) : 0.f;
-    total += wgt * (live ? w[1] : 0.f);
-    const int ex = (int32_t)(__float_as_uint(w[2]) << (24 - 8 * q)) >> 24;
-    const float ws = __builtin_amdgcn_ldexpf(wgt, ex - 14);
-    static_for<16>([&](auto u) {
-      const float wu = __uint_as_float(
-          __builtin_amdgcn_update_dpp(0, __float_as_uint(ws), kRowBcast0 + u.value, 0xf, 0xf, false));
+    for (int u = 0; u < kLongAhead; ++u) {
+      const size_t at = min(p0 + 4 * u + p, np - 1);
+      w[u] = *(const f32x4*)(ml + at * kMlStride);
+      x[u] = __builtin_nontemporal_load((const u32x2*)(acc + at * kAccStride));
+    }
+    float top = big;
+#pragma unroll
+    for (int u = 0; u < kLongAhead; ++u) top = fmaxf(top, w[u][0]);
+    top = row_max4(top);   // of the wavefront: every lane of 16 has the same results
+    const float down = big == ninf ? 0.f : fast_exp2(big - top);
+    total *= down;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] *= down;
+    big = top;
+#pragma unroll
+    for (int u = 0; u < kLongAhead; ++u) {
+      const bool live = p0 + 4 * u + p < np && w[u][0] != ninf;
+      const float wgt = live ? fast_exp2(w[u][0] - big) : 0.f;
+      total += wgt * (live ? w[u][1] : 0.f);
+      const int ex = (int32_t)(__float_as_uint(w[u][2]) << (24 - 8 * part)) >> 24;   // signed byte `part`
+      const float ws = __builtin_amdgcn_ldexpf(wgt, ex - 14);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         float lo, hi;
-        unpack_f16(x[u.value][k], lo, hi);
-        o[2 * k] = __builtin_fmaf(wu, lo, o[2 * k]);
-        o[2 * k + 1] = __builtin_fmaf(wu, hi, o[2 * k + 1]);
+        unpack_f16(x[u][k], lo, hi);
+        o[2 * k] = __builtin_fmaf(ws, lo, o[2 * k]);
+        o[2 * k + 1] = __builtin_fmaf(ws, hi, o[2 * k + 1]);
       }
-    });
+    }
   }
-  os[wv][lane] = (f32x4){o[0], o[1], o[2], o[3]};
-  total = lanes16_sum(total);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = row_sum4(o[k]);
+  total = row_sum4(total);
+  if (p == 0) os[wv][i] = (f32x4){o[0], o[1], o[2], o[3]};
   if (lane == 0) bigs[wv] = big, totals[wv] = total;
   __syncthreads();
   if (wv != 0) return;
-  const float mine = bigs[i];
-  const float top = lanes16_max(mine);
-  const float wgt = mine == ninf ? 0.f : fast_exp2(mine - top);
-  const float sum = lanes16_sum(wgt * totals[i]);
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  static_for<kLongWaves>([&](auto u) {
-    const float wu = __uint_as_float(
-        __builtin_amdgcn_update_dpp(0, __float_as_uint(wgt), kRowBcast0 + u.value, 0xf, 0xf, false));
-    const f32x4 part = os[u.value][lane];
+  float top = bigs[0];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = __builtin_fmaf(wu, part[k], r[k]);
-  });
+  for (int w = 1; w < kLongWaves; ++w) top = fmaxf(top, bigs[w]);
+  float sum = 0.f;
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kLongWaves; ++w) {
+    const float wgt = bigs[w] == ninf ? 0.f : fast_exp2(bigs[w] - top);
+    sum = __builtin_fmaf(wgt, totals[w], sum);
+    const f32x4 theirs = os[w][i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = __builtin_fmaf(wgt, theirs[k], r[k]);
+  }
   const float inv = 1.f / sum;
   const u32x2 packed = {pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv)};
-  *(u32x2*)((uint16_t*)out + ((size_t)tok * kHeads + h) * kDim + 4 * lane) = packed;
-  if (lse && lane == 0)
+  if (p == 0) *(u32x2*)((uint16_t*)out + ((size_t)tok * kHeads + h) * kDim + 64 * part + 4 * i) = packed;
+  if (lse && part == 0 && lane == 0)
     lse[(size_t)tok * kHeads + h] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
@@ -649,10 +748,10 @@ hipError_t launch_merge8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hi
   if (a.max_parts <= kLongParts) return launch_merge_append(a, nullptr, s, start, stop);
   if (a.n_q <= 0) return hipErrorInvalidValue;
   if (start || stop)
-    hipExtLaunchKernelGGL(merge_long_kernel, dim3(kHeads * a.n_q), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc,
+    hipExtLaunchKernelGGL(merge_long_kernel, dim3(4 * kHeads * a.n_q), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc,
                           a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
   else
-    merge_long_kernel<<<kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
+    merge_long_kernel<<<4 * kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
   return hipGetLastError();
 }
 

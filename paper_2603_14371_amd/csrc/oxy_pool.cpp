@@ -695,9 +695,9 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
       o.tile = o.streams ? 2 : o.short_chunk ? 8 : tile_tok_for(pl.new_len);
       o.split = o.streams ? stream_split_for(c, pl.new_len)
                           : o.short_chunk ? 32 : tile_split_for(c, pl.new_len);
-      o.by_width = p->kv8 && o.short_chunk;
-      if (o.by_width) {
-        o.tile = chunk_tile8;
+      o.by_width = p->kv8 && o.short_chunk && !o.causal;   // causal ones: the keys of an item go with its width
+      if (p->kv8 && o.short_chunk) {
+        o.tile = o.by_width ? chunk_tile8 : 4;
         o.split = 64;
       }
       if (p->kv8) o.fresh = o.short_chunk = false;
