@@ -303,11 +303,11 @@ constexpr int kRowRor8 = 0x128;   // DPP: lane n of each 16 gets lane n^8's valu
 // values.  kLines: whole lines, for items of eight tokens, whose launches write the most (us per layer, pieces /
 // lines: eight chunks on 2048 tokens 24.4 / 23.6, six on 1500 22.1 / 21.6, four and 32 requests on 1024 17.9 / 17.1,
 // eight on 832 17.36 / 17.32; narrower items are up to 1 % slower with it).  acc[c][e] = dim 16g + 4e + c of the 64: a lane's sixteen values are consecutive.  slot:
-// split result of this lane's token.
-template <bool kLines>
+// split result of this lane's token.  kUnit: acc is in units of 2^unit.
+template <bool kLines, bool kUnit = false>
 __device__ __forceinline__ void store_part(const AttnArgs& a, const WorkItem& wi, const int slot,
                                            const f32x4 (&acc)[4], const int group, const int wv,
-                                           const int lane) {
+                                           const int lane, const int unit = 0) {
   const int n = lane & 15, g = lane >> 4;
   float amax = 0.f;
 #pragma unroll
@@ -319,8 +319,15 @@ __device__ __forceinline__ void store_part(const AttnArgs& a, const WorkItem& wi
   const int eb = max(24, min(253, (int)(__float_as_uint(amax) >> 23)));
   // an infinite value leaves no exponent for the others: all 64 are NaN then, instead of zeros (looking
   // for the largest finite one in a branch of its own cost 0.5 % of a launch of chunks)
-  const float up = __uint_as_float((uint32_t)(127 + 14 + 126 - eb) << 23) + (amax - amax);
-  const int ex = eb - 126;
+  float up;
+  int ex;
+  if constexpr (kUnit) {   // the exponent that is stored is that of the values, within its eight bits
+    ex = max(-128, min(127, eb - 126 + unit));
+    up = __uint_as_float((uint32_t)(127 + 14 - (ex - unit)) << 23) + (amax - amax);
+  } else {
+    up = __uint_as_float((uint32_t)(127 + 14 + 126 - eb) << 23) + (amax - amax);
+    ex = eb - 126;
+  }
   u32x4 o[2];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {

@@ -214,6 +214,15 @@ __device__ __forceinline__ u32x4 f16_operand(const uint32_t lo, const uint32_t h
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
   return r;
 }
+// Largest of a lane's eight dot products, in four instructions (fmaxf makes every matrix result canonical first: eleven).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float largest8(const f32x4 s0, const f32x4 s1) {
+  return max3(max3(max3(s0[0], s0[1], s0[2]), s0[3], s1[0]), max3(s1[1], s1[2], s1[3]), -__builtin_inff());
+}
 // first `left` of four bytes
 __device__ __forceinline__ uint32_t byte_mask(const int left) {
   return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
@@ -364,12 +373,9 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       __builtin_amdgcn_sched_barrier(0);
       take_late<kLate8>(a);
 #pragma unroll
-      for (int r = 0; r < G; ++r) {
-        const u32x4 z = {0, 0, 0, 0};
+      for (int r = 0; r < G; ++r)   // rows past the item's tokens are its last one's again; nothing of them is stored
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          sm.q[r][2 * wv + i][lane] = 2 * r + sub < wi.n_tok ? query_sign(a, qtmp[r][i]) : z;
-      }
+        for (int i = 0; i < 2; ++i) sm.q[r][2 * wv + i][lane] = query_sign(a, qtmp[r][i]);
     };
     if (kSteps == 2 && wv >= 2) {
 #pragma unroll
@@ -427,7 +433,8 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
 #pragma unroll
         for (int e = 0; e < 8; ++e) vb[u][e] = (int)((ve[u][e >> 2] >> (8 * (e & 3))) & 0xffu);
         if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
-          const int k0 = pos + 16 * (g >> 1) + 4 * (g & 1);
+          int k0 = pos + 16 * (g >> 1) + 4 * (g & 1);
+          asm volatile("" : "+v"(k0));   // a branch: as selects the masks are a quarter of a round's instructions
 #pragma unroll
           for (int r = 0; r < G; ++r) {
             const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
@@ -452,8 +459,8 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       float mx[G];
 #pragma unroll
       for (int r = 0; r < G; ++r) {
-        mx[r] = row_max8(s0[0][r], s1[0][r]);
-        if constexpr (kSub == 2) mx[r] = fmaxf(mx[r], row_max8(s0[kSub - 1][r], s1[kSub - 1][r]));
+        mx[r] = largest8(s0[0][r], s1[0][r]);
+        if constexpr (kSub == 2) mx[r] = fmaxf(mx[r], largest8(s0[kSub - 1][r], s1[kSub - 1][r]));
         mx[r] *= sl2;
       }
       const float mine = row_max4_each(mx);
@@ -503,10 +510,10 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     }
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
-      // 2^(exponent - vref + 7); nothing for a key that is not there
+      // 2^(exponent - vref + 7); for a key that is not there (P is 0) something finite
       float factor[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) factor[e] = scale_of((uint32_t)max(vb[u][e] ? vb[u][e] - vref + 127 + 7 : 0, 0));
+      for (int e = 0; e < 8; ++e) factor[e] = __uint_as_float((uint32_t)max((vb[u][e] << 23) + ((127 + 7 - vref) << 23), 0));
 #pragma unroll
       for (int r = 0; r < G; ++r) {
         u32x4 w;
@@ -520,50 +527,71 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     if constexpr (!kLast) load_k(round + 1);
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
-    auto contract = [&](const int s) {
-      u32x4 v[4];
+    auto operands = [&](const int s, u32x4 (&v)[4]) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) v[c] = f16_operand(vr[s][c >> 1][2 * (c & 1)], vr[s][c >> 1][2 * (c & 1) + 1]);
+    };
+    auto contract = [&](const int s, const int r, const u32x4 (&v)[4]) {
+      const u32x4 w = sm.p[s * G + r][lane];
 #pragma unroll
-      for (int r = 0; r < G; ++r) {
-        const u32x4 w = sm.p[s * G + r][lane];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[r][c] = mfma16_f16(v[c], w, acc[r][c]);
-      }
+      for (int c = 0; c < 4; ++c) acc[r][c] = mfma16_f16(v[c], w, acc[r][c]);
     };
     if constexpr (!kLast) {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) contract(s);
+      for (int s = 0; s < kSteps; ++s) {
+        u32x4 v[4];
+        operands(s, v);
+#pragma unroll
+        for (int r = 0; r < G; ++r) contract(s, r, v);
+      }
       __builtin_amdgcn_sched_barrier(0);   // likewise vr[]
       load_v(round + 1);
       __builtin_amdgcn_sched_barrier(0);
     } else {
       const int nv = nsteps - kRound * round;   // steps with keys
+      auto clear_past_end = [&](const int s) {   // codes of slots beyond the end may be anything
+        const int left_s = wi.kv_end - (wi.kv_begin + 32 * (kRound * round + s));
+        if (left_s < 32) {
+          const int k0 = 16 * (g >> 1) + 4 * (g & 1);
+          const uint32_t m0 = byte_mask(left_s - k0), m1 = byte_mask(left_s - k0 - 8);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        if (s < nv) {
-          const int left_s = wi.kv_end - (wi.kv_begin + 32 * (kRound * round + s));
-          if (left_s < 32) {   // codes of slots beyond the end may be anything
-            const int k0 = 16 * (g >> 1) + 4 * (g & 1);
-            const uint32_t m0 = byte_mask(left_s - k0), m1 = byte_mask(left_s - k0 - 8);
-#pragma unroll
-            for (int cp = 0; cp < 2; ++cp) vr[s][cp] &= (u32x4){m0, m1, m0, m1};
-          }
-          contract(s);
+          for (int cp = 0; cp < 2; ++cp) vr[s][cp] &= (u32x4){m0, m1, m0, m1};
         }
-#pragma unroll
-      for (int r = 0; r < G; ++r) {
+      };
+      auto finish_group = [&](const int r) {
         const int slot = sm.slot[2 * r + sub];
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[r][c][e] = __builtin_amdgcn_ldexpf(acc[r][c][e], vref - 127 - 7);
-        store_part<(G >= 4)>(a, wi, slot, acc[r], r, wv, lane);
+        store_part<(G >= 4), true>(a, wi, slot, acc[r], r, wv, lane, vref - 127 - 7);
         if (wv == r) {   // wave-uniform: the sums of the groups are shared out
           const f32x4 lw = *(const f32x4*)sm.ls[r][lane];
           const float total = row_sum4((lw[0] + lw[1]) + (lw[2] + lw[3]));
           if (g == 0 && 2 * r + sub < wi.n_tok)
             *(f32x2*)(a.part_ml + ((size_t)slot * kHeads + (n & 7)) * 4) = (f32x2){m[r], total};
+        }
+      };
+      if constexpr (G == 1) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          if (s < nv) {
+            u32x4 v[4];
+            clear_past_end(s);
+            operands(s, v);
+            contract(s, 0, v);
+          }
+        finish_group(0);
+      } else {
+        // Group by group, so that a group's scaling and stores fall into the products of the next.  Steps without keys
+        // are zeros.
+        u32x4 v[kSteps][4];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          clear_past_end(s);
+          operands(s, v[s]);
+        }
+#pragma unroll
+        for (int r = 0; r < G; ++r) {
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) contract(s, r, v[s]);
+          finish_group(r);
         }
       }
     }
