@@ -334,7 +334,7 @@ int32_t oxy_rotary(const oxy_rotary_config *cfg, const int32_t *positions, const
  * of oxy_mixed_attention), new keys turned and stored, new values stored, in the slots of `layer`, bf16
  * or 8 bits.  Same results as oxy_rotary on queries and keys and oxy_stream_append of the turned
  * keys.  Token t's rows: q + t * q_stride (8 x 256), k_new + t * k_stride, v_new + t * v_stride, strides
- * in bytes, all 16-byte aligned, so a projection's [n][10 * 256] output is taken as it is.  q may be
+ * in bytes (below 4 GiB), all 16-byte aligned, so a projection's [n][10 * 256] output is taken as it is.  q may be
  * NULL (keys and values only; q_out is not touched); q_out may be q if q_stride is 4096. */
 int32_t oxy_rotary_append(oxy_pool *pool, const oxy_batch *batch, int32_t layer,
                           const oxy_rotary_config *cfg, const int32_t *positions, const void *q,

@@ -60,7 +60,7 @@ struct RotaryAppendArgs {
   const void* q;               // null: no queries
   void* q_out;                 // [n_tokens][8][256]
   const void *k_new, *v_new;
-  size_t q_stride, k_stride, v_stride;   // bytes from token to token
+  uint32_t q_stride, k_stride, v_stride;   // bytes from token to token
   const int32_t* d_slots;
   void* layer_base;            // of a bf16 layer, or the blocks of one in 8 bits
   uint8_t* scales;             // null: bf16

@@ -1559,6 +1559,8 @@ int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
   if (bits & 15) return fail(OXY_ERR_INVALID_ARG, "rotary_append: rows must be 16-byte aligned");
   if (b->n_tokens > 1 && (k_stride < row || v_stride < row || (q && q_stride < oxy::kHeads * row)))
     return fail(OXY_ERR_INVALID_ARG, "rotary_append: stride below a token's rows");
+  if (b->n_tokens > 1 && (k_stride > UINT32_MAX || v_stride > UINT32_MAX || (q && q_stride > UINT32_MAX)))
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: stride of 4 GiB or more");
   const int32_t* d_desc = (const int32_t*)p->slots[b->slot].d_base;
   oxy::RotaryAppendArgs a;
   a.rotary = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};
@@ -1566,9 +1568,9 @@ int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
   a.q_out = q_out;
   a.k_new = k_new;
   a.v_new = v_new;
-  a.q_stride = q_stride;
-  a.k_stride = k_stride;
-  a.v_stride = v_stride;
+  a.q_stride = (uint32_t)q_stride;
+  a.k_stride = (uint32_t)k_stride;
+  a.v_stride = (uint32_t)v_stride;
   a.d_slots = d_desc + b->off_slots;
   a.layer_base = layer_base(p, layer);
   a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;

@@ -24,12 +24,26 @@ constexpr int kMaxPairs = kDim / 2;
 // How a lane finds its dims' partners: pairs lie side by side; halves a whole number of 16-byte chunks apart; or not.
 enum RotaryForm { FORM_PAIRS, FORM_HALVES, FORM_HALVES_ANY };
 
-__device__ __forceinline__ void turn_of(const RotaryArgs& r, const int position, const int pair, float& c, float& s) {
-  const double turns = (double)position * r.freqs[pair] * 0.15915494309189533577;   // 1 / (2 pi)
-  double sd, cd;
-  sincospi(2.0 * (turns - rint(turns)), &sd, &cd);
-  c = (float)(cd * r.amplitude);
-  s = (float)(sd * r.amplitude);
+// Cosine and sine of position * freq times the amplitude, rounded to 32 bits once.  The angle is brought to a fraction of a
+// turn, then to within an eighth of one around the nearest quarter, where the series of the two functions are cut where
+// their next terms are below 1e-11 (a fiftieth of a thousandth of half a unit of the 32-bit result).  20 instructions in 64
+// bits, which run at the rate of 32 (the library's sincospi, whose last bits are rounded off here, takes three times as many: prefill of
+// 8192 tokens 20.7 us, now 17.5).
+__device__ __forceinline__ void turn_of(const double freq, const double amplitude, const int position, float& c, float& s) {
+  const double turns = (double)position * freq * 0.15915494309189533577;   // 1 / (2 pi)
+  const double part = turns - rint(turns), quarter = rint(4.0 * part);
+  const double x = (part - 0.25 * quarter) * 6.28318530717958647693, z = x * x;   // |x| <= pi / 4
+  double sd = 1.0 / 6227020800.0, cd = -1.0 / 87178291200.0;
+  sd = fma(sd, z, -1.0 / 39916800.0), cd = fma(cd, z, 1.0 / 479001600.0);
+  sd = fma(sd, z, 1.0 / 362880.0), cd = fma(cd, z, -1.0 / 3628800.0);
+  sd = fma(sd, z, -1.0 / 5040.0), cd = fma(cd, z, 1.0 / 40320.0);
+  sd = fma(sd, z, 1.0 / 120.0), cd = fma(cd, z, -1.0 / 720.0);
+  sd = fma(sd, z, -1.0 / 6.0), cd = fma(cd, z, 1.0 / 24.0);
+  sd = fma(sd * z, x, x), cd = fma(fma(cd, z, -0.5), z, 1.0);
+  const int k = (int)quarter;   // -2..2 quarters on
+  const double cq = (k & 1) ? sd : cd, sq = (k & 1) ? cd : sd;
+  c = (float)(((k + 1) & 2) ? -cq * amplitude : cq * amplitude);
+  s = (float)((k & 2) ? -sq * amplitude : sq * amplitude);
 }
 __device__ __forceinline__ float element(const u32x4 x, const int e) {
   const uint32_t w = x[e >> 1];
@@ -39,13 +53,15 @@ __device__ __forceinline__ float element(const u32x4 x, const int e) {
 struct RowLoad {
   u32x4 own, other;
 };
-template <int kForm>
+// kPartners: partners a whole number of chunks apart are loaded too; otherwise `turned` fetches them from the lanes that
+// hold them.
+template <int kForm, bool kPartners>
 __device__ __forceinline__ RowLoad load_turning(const uint16_t* row, const int rot, const int c) {
   RowLoad x;
   x.own = *(const u32x4*)(row + 8 * c);
   x.other = x.own;
   const int half = rot >> 1;
-  if constexpr (kForm == FORM_HALVES) {
+  if constexpr (kForm == FORM_HALVES && kPartners) {
     if (8 * c < rot) x.other = *(const u32x4*)(row + (8 * c < half ? 8 * c + half : 8 * c - half));
   } else if constexpr (kForm == FORM_HALVES_ANY) {
 #pragma unroll
@@ -62,95 +78,144 @@ __device__ __forceinline__ RowLoad load_turning(const uint16_t* row, const int r
   }
   return x;
 }
-// cs, sn: cosines and sines of this row's token
+// Cosines and sines of a lane's eight dims, the same for all heads of a token.
+struct LaneTurns {
+  float c[8], s[8];
+};
 template <int kForm>
-__device__ __forceinline__ u32x4 turned(const RowLoad& x, const float* cs, const float* sn, const int rot, const int c) {
+__device__ __forceinline__ LaneTurns turns_of_lane(const float* cs, const float* sn, const int rot, const int c) {
+  LaneTurns r;
+  const int half = rot >> 1;
+  // a - b * s is a + b * -s, bit for bit.  Past the rotated dims: read, and not used
+  if constexpr (kForm == FORM_PAIRS) {
+    const f32x4 ct = *(const f32x4*)(cs + 4 * c), st = *(const f32x4*)(sn + 4 * c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.c[e] = ct[e >> 1], r.s[e] = (e & 1) ? st[e >> 1] : -st[e >> 1];
+  } else if constexpr (kForm == FORM_HALVES) {
+    const bool first = 8 * c < half;
+    const int at = first ? 8 * c : min(8 * c - half, kMaxPairs - 8);
+    const uint32_t flip = first ? 0x80000000u : 0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f32x4 ct = *(const f32x4*)(cs + at + 4 * i), st = *(const f32x4*)(sn + at + 4 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.c[4 * i + e] = ct[e], r.s[4 * i + e] = __uint_as_float(__float_as_uint(st[e]) ^ flip);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int d = 8 * c + e, at = min(d < half ? d : d - half, kMaxPairs - 1);
+      r.c[e] = cs[at];
+      r.s[e] = d < half ? -sn[at] : sn[at];
+    }
+  }
+  return r;
+}
+// By all lanes of a half wavefront.  In a prefill partners come from other lanes (loaded a second time instead: 8192
+// tokens 21.9 us, so 19.9); in a step they are loaded, while the angles are taken (58 tokens 2.85 us; from lanes 3.05).
+template <int kForm, bool kPartners>
+__device__ __forceinline__ u32x4 turned(RowLoad x, const LaneTurns& w, const int rot, const int c) {
 #pragma clang fp contract(off)
   u32x4 out = x.own;
-  const int half = rot >> 1;
+  if constexpr (kForm == FORM_HALVES && !kPartners) {
+    const int apart = rot >> 4, lane = threadIdx.x & 63;
+    const int from = c < apart ? lane + apart : c < 2 * apart ? lane - apart : lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.other[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)x.own[i]);
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float y[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int e = 2 * i + k, d = 8 * c + e;
-      int pair;
-      float other;
-      bool first;
-      if constexpr (kForm == FORM_PAIRS) {
-        pair = d >> 1;
-        other = element(x.own, e ^ 1);
-        first = k == 0;
-      } else {
-        first = d < half;
-        pair = first ? d : d - half;
-        other = element(x.other, e);
-      }
-      pair = min(pair, kMaxPairs - 1);   // past the rotated dims: read, and not used
-      const float a = element(x.own, e) * cs[pair], b = other * sn[pair];
-      y[k] = first ? a - b : a + b;
+      const int e = 2 * i + k;
+      const float other = kForm == FORM_PAIRS ? element(x.own, e ^ 1) : element(x.other, e);
+      const float a = element(x.own, e) * w.c[e], b = other * w.s[e];
+      y[k] = a + b;
     }
-    const uint32_t w = pack_bf16(y[0], y[1]);
-    const int d = 8 * c + 2 * i;
-    out[i] = d < rot ? w : x.own[i];   // both or neither: rot is even
+    out[i] = 8 * c + 2 * i < rot ? pack_bf16(y[0], y[1]) : x.own[i];   // both or neither: rot is even
   }
   return out;
 }
 
-constexpr int kRotaryTokens = 4;   // of a workgroup: their angles are taken once for all heads
-template <int kForm>
+// kTokens of a workgroup: their angles are taken once for all heads, by all threads, and come to the lanes through LDS.
+// With four, two half wavefronts share a token's heads; with one, all eight do.  A half wavefront keeps its cosines and
+// sines, and kRows rows in flight.
+template <int kForm, int kTokens>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const char* x, const size_t x_stride, char* out,
                                                      const size_t out_stride, const int32_t n_tokens,
                                                      const int32_t n_heads) {
-  __shared__ __align__(16) float cs[kRotaryTokens][kMaxPairs], sn[kRotaryTokens][kMaxPairs];
-  const int tok0 = blockIdx.x * kRotaryTokens, here = min(kRotaryTokens, n_tokens - tok0);
-  const int t = threadIdx.x, c = t & 31, rows = here * n_heads, half = r.rot_dims >> 1;
-  auto row_of = [&](int i) {
-    const int tok = i / n_heads;
-    return (const uint16_t*)(x + (size_t)(tok0 + tok) * x_stride) + (i - tok * n_heads) * kDim;
+  constexpr int kStep = 8 / kTokens, kRows = kForm == FORM_HALVES_ANY ? 1 : kTokens == 1 ? 2 : 3;   // half wavefronts of a token; rows at a time
+  __shared__ __align__(16) float cs[kTokens][kMaxPairs], sn[kTokens][kMaxPairs];
+  const int tok0 = blockIdx.x * kTokens, here = min(kTokens, n_tokens - tok0);
+  const int t = threadIdx.x, c = t & 31, half = r.rot_dims >> 1;
+  const int mine = (t >> 5) / kStep, tok = min(mine, here - 1), head0 = (t >> 5) % kStep;
+  const char* src = x + (size_t)(tok0 + tok) * x_stride;
+  char* dst = out + (size_t)(tok0 + tok) * out_stride + 16 * c;
+  RowLoad rows[kRows];
+  auto load = [&](const int head) {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)   // a row past the last is the last one again
+      rows[k] = load_turning<kForm, false>((const uint16_t*)src + min(head + k * kStep, n_heads - 1) * kDim, r.rot_dims, c);
   };
-  int i = t >> 5;
-  RowLoad now = {};
-  if (i < rows) now = load_turning<kForm>(row_of(i), r.rot_dims, c);   // on its way while the angles are taken
+  load(head0);   // on their way while the angles are taken
   for (int k = t; k < here * half; k += 256) {
-    const int tok = k / half, pair = k - tok * half;
-    turn_of(r, r.positions[tok0 + tok], pair, cs[tok][pair], sn[tok][pair]);
+    const int at = k / half, pair = k - at * half;
+    turn_of(r.freqs[pair], r.amplitude, r.positions[tok0 + at], cs[at][pair], sn[at][pair]);
   }
   __syncthreads();
-  while (i < rows) {
-    const int tok = i / n_heads, next = i + 8;
-    RowLoad ahead = {};
-    if (next < rows) ahead = load_turning<kForm>(row_of(next), r.rot_dims, c);
-    *(u32x4*)(out + (size_t)(tok0 + tok) * out_stride + (size_t)(i - tok * n_heads) * (kDim * 2) + 16 * c) =
-        turned<kForm>(now, cs[tok], sn[tok], r.rot_dims, c);
-    now = ahead;
-    i = next;
+  const LaneTurns w = turns_of_lane<kForm>(cs[tok], sn[tok], r.rot_dims, c);
+  for (int head = head0;;) {
+    u32x4 y[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) y[k] = turned<kForm, false>(rows[k], w, r.rot_dims, c);
+    const int next = head + kRows * kStep;
+    if (next - head0 < n_heads) load(next);   // the same for both halves of a wavefront
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+      if (head + k * kStep < n_heads && mine < here) *(u32x4*)(dst + (head + k * kStep) * (kDim * 2)) = y[k];
+    if (next - head0 >= n_heads) break;
+    head = next;
   }
 }
 
-// One token per workgroup: ten half wavefronts take its eight query rows, its key and its value.
+// What a workgroup needs behind its first loads.
+struct RotaryLate {
+  const double* freqs;
+  const int32_t* d_slots;
+  void* q_out;
+  void* layer_base;
+  uint8_t* scales;
+  double amplitude;
+};
+// One token per workgroup: ten half wavefronts take its eight query rows, its key and its value.  The addresses of the
+// first loads are preloaded into scalar registers (see build.py).
 template <int kForm, bool kBits8>
-__global__ __launch_bounds__(320) void rotary_append_kernel(const RotaryAppendArgs a) {
+__global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* positions, const char* q, const char* k_new,
+                                                            const char* v_new, const uint32_t q_stride,
+                                                            const uint32_t k_stride, const uint32_t v_stride,
+                                                            const int32_t rot, const RotaryLate a) {
   __shared__ __align__(16) float cs[kMaxPairs], sn[kMaxPairs];
-  const int tok = blockIdx.x, t = threadIdx.x, c = t & 31, row = t >> 5, rot = a.rotary.rot_dims;
+  const int t = threadIdx.x, c = t & 31, row = t >> 5;
+  const size_t tok = blockIdx.x;
   const bool is_q = row < kHeads, is_v = row == kHeads + 1;
-  const char* src = is_q ? (const char*)a.q + tok * a.q_stride + row * (kDim * 2)
-                  : is_v ? (const char*)a.v_new + tok * a.v_stride : (const char*)a.k_new + tok * a.k_stride;
+  const char* src = is_q ? q + tok * q_stride + row * (kDim * 2) : is_v ? v_new + tok * v_stride : k_new + tok * k_stride;
   RowLoad x = {};
-  const bool live = !is_q || a.q;
+  const bool live = !is_q || q;
+  const int32_t position = ((DescPtr)positions)[tok];
   if (live) {
     if (is_v)
       x.own = *(const u32x4*)((const uint16_t*)src + 8 * c);
     else
-      x = load_turning<kForm>((const uint16_t*)src, rot, c);
+      x = load_turning<kForm, true>((const uint16_t*)src, rot, c);
   }
-  const int32_t slot = a.d_slots[tok];
-  if (t < rot >> 1) turn_of(a.rotary, a.rotary.positions[tok], t, cs[t], sn[t]);
+  const int32_t slot = ((DescPtr)a.d_slots)[tok];
+  if (t < rot >> 1) turn_of(a.freqs[t], a.amplitude, position, cs[t], sn[t]);
   __syncthreads();
   u32x4 y = x.own;
-  if (!is_v) y = turned<kForm>(x, cs, sn, rot, c);
+  if (!is_v) y = turned<kForm, true>(x, turns_of_lane<kForm>(cs, sn, rot, c), rot, c);
   if (is_q) {   // whole wavefronts: the key and the value are the two halves of the last one
-    if (live) *(u32x4*)((uint16_t*)a.q_out + ((size_t)tok * kHeads + row) * kDim + 8 * c) = y;
+    if (live) *(u32x4*)((uint16_t*)a.q_out + (tok * kHeads + row) * kDim + 8 * c) = y;
     return;
   }
   const int key = slot & 15;
@@ -176,29 +241,37 @@ __global__ __launch_bounds__(320) void rotary_append_kernel(const RotaryAppendAr
 }
 
 namespace {
+constexpr int kManyTokens = 2049;
 int form_of(const RotaryArgs& r) {
   return r.pairs ? FORM_PAIRS : (r.rot_dims >> 1) % 8 == 0 ? FORM_HALVES : FORM_HALVES_ANY;
 }
 template <int kForm>
 void launch_append_form(const RotaryAppendArgs& a, hipStream_t s) {
+  const RotaryLate late = {a.rotary.freqs, a.d_slots, a.q_out, a.layer_base, a.scales, a.rotary.amplitude};
+  const auto launch = [&](auto kernel) {
+    kernel<<<a.n_tokens, 320, 0, s>>>(a.rotary.positions, (const char*)a.q, (const char*)a.k_new, (const char*)a.v_new,
+                                      a.q_stride, a.k_stride, a.v_stride, a.rotary.rot_dims, late);
+  };
   if (a.scales)
-    rotary_append_kernel<kForm, true><<<a.n_tokens, 320, 0, s>>>(a);
+    launch(rotary_append_kernel<kForm, true>);
   else
-    rotary_append_kernel<kForm, false><<<a.n_tokens, 320, 0, s>>>(a);
+    launch(rotary_append_kernel<kForm, false>);
 }
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs& r, const void* x, size_t x_stride, void* out, size_t out_stride,
                          int32_t n_tokens, int32_t n_heads, hipStream_t s) {
   if (n_tokens <= 0) return hipSuccess;
-  const dim3 grid((n_tokens + kRotaryTokens - 1) / kRotaryTokens);
-  const auto launch = [&](auto kernel) {
-    kernel<<<grid, 256, 0, s>>>(r, (const char*)x, x_stride, (char*)out, out_stride, n_tokens, n_heads);
+  // four tokens share a workgroup's start where there are enough of them for every CU
+  const bool many = n_tokens >= kManyTokens;
+  const auto launch = [&](auto one, auto four) {
+    const dim3 grid(many ? (n_tokens + 3) / 4 : n_tokens);
+    (many ? four : one)<<<grid, 256, 0, s>>>(r, (const char*)x, x_stride, (char*)out, out_stride, n_tokens, n_heads);
   };
   switch (form_of(r)) {
-    case FORM_PAIRS: launch(rotary_kernel<FORM_PAIRS>); break;
-    case FORM_HALVES: launch(rotary_kernel<FORM_HALVES>); break;
-    default: launch(rotary_kernel<FORM_HALVES_ANY>);
+    case FORM_PAIRS: launch(rotary_kernel<FORM_PAIRS, 1>, rotary_kernel<FORM_PAIRS, 4>); break;
+    case FORM_HALVES: launch(rotary_kernel<FORM_HALVES, 1>, rotary_kernel<FORM_HALVES, 4>); break;
+    default: launch(rotary_kernel<FORM_HALVES_ANY, 1>, rotary_kernel<FORM_HALVES_ANY, 4>);
   }
   return hipGetLastError();
 }
