@@ -6,6 +6,8 @@ on a negative status.  There is no fallback: if the library is missing, loading 
 """
 import array
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 
 import numpy as np
@@ -169,7 +171,41 @@ def lib():
             fn.argtypes = args
             fn.restype = ctypes.c_int32
         _lib = L
+        _bind_quick(L)
     return _lib
+
+
+def _not_bound(*args):
+    return None
+
+
+class _Quick:
+    """Calls that a program makes in every layer, through libmarshal.so where it is there: the status, or None
+    where an argument needs ctypes' own conversion (or nothing is bound) and no call was made.  ctypes takes 1.1 us for
+    an attention call's arguments and 1.8 for a rotating append's, this 0.3 and 0.4."""
+    oxy_mixed_attention = staticmethod(_not_bound)
+    oxy_mixed_attention_static = staticmethod(_not_bound)
+    oxy_stream_append = staticmethod(_not_bound)
+    oxy_append_attention = staticmethod(_not_bound)
+    oxy_rotary = staticmethod(_not_bound)
+    oxy_rotary_append = staticmethod(_not_bound)
+
+
+_quick = _Quick()
+
+
+def _bind_quick(L):
+    try:
+        loader = importlib.machinery.ExtensionFileLoader("libmarshal", MARSHAL_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("libmarshal", loader))
+        loader.exec_module(module)
+        bound = module.bound
+    except (ImportError, OSError, AttributeError):
+        return
+    for name in [n for n in vars(_Quick) if n.startswith("oxy_")]:
+        call = bound(name, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
+        if call is not None:
+            setattr(_quick, name, call)
 
 
 _marshal_lib = None
@@ -288,17 +324,29 @@ def oxy_batch_build(pool, items, flags, stream):
 
 
 def oxy_stream_append(pool, batch, layer, k_ptr, v_ptr, stream):
-    _check(lib().oxy_stream_append(pool, batch, layer, k_ptr, v_ptr, stream or None))
+    status = _quick.oxy_stream_append(pool, batch, layer, k_ptr, v_ptr, stream)
+    if status is None:
+        status = lib().oxy_stream_append(pool, batch, layer, k_ptr, v_ptr, stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_mixed_attention(pool, batch, layer, q_ptr, out_ptr, lse_ptr, scale, stream):
-    _check(lib().oxy_mixed_attention(pool, batch, layer, q_ptr, out_ptr, lse_ptr or None,
-                                     ctypes.c_float(scale), stream or None))
+    status = _quick.oxy_mixed_attention(pool, batch, layer, q_ptr, out_ptr, lse_ptr, scale, stream)
+    if status is None:
+        status = lib().oxy_mixed_attention(pool, batch, layer, q_ptr, out_ptr, lse_ptr or None,
+                                           ctypes.c_float(scale), stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_mixed_attention_static(pool, batch, layer, q_ptr, out_ptr, lse_ptr, scale, stream):
-    _check(lib().oxy_mixed_attention_static(pool, batch, layer, q_ptr, out_ptr, lse_ptr or None,
-                                            ctypes.c_float(scale), stream or None))
+    status = _quick.oxy_mixed_attention_static(pool, batch, layer, q_ptr, out_ptr, lse_ptr, scale, stream)
+    if status is None:
+        status = lib().oxy_mixed_attention_static(pool, batch, layer, q_ptr, out_ptr, lse_ptr or None,
+                                                  ctypes.c_float(scale), stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_step_layers(pool, batch, layer_begin, layer_end, k_ptr, v_ptr, kv_layer_stride, q_ptr,
@@ -317,8 +365,12 @@ def oxy_step_graph_stats(pool):
 
 
 def oxy_append_attention(pool, batch, layer, k_ptr, v_ptr, q_ptr, out_ptr, lse_ptr, scale, stream):
-    _check(lib().oxy_append_attention(pool, batch, layer, k_ptr, v_ptr, q_ptr, out_ptr,
-                                      lse_ptr or None, ctypes.c_float(scale), stream or None))
+    status = _quick.oxy_append_attention(pool, batch, layer, k_ptr, v_ptr, q_ptr, out_ptr, lse_ptr, scale, stream)
+    if status is None:
+        status = lib().oxy_append_attention(pool, batch, layer, k_ptr, v_ptr, q_ptr, out_ptr,
+                                            lse_ptr or None, ctypes.c_float(scale), stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_batch_destroy(batch):
@@ -373,15 +425,24 @@ def oxy_rotary_freqs(base, rot_dims, kind=ROTARY_PLAIN, factor=1.0, low=0.0, hig
 
 
 def oxy_rotary(rotary, positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream):
-    _check(lib().oxy_rotary(ctypes.byref(rotary), positions_ptr or None, x_ptr or None, x_stride,
-                            out_ptr or None, out_stride, n_tokens, n_heads, stream or None))
+    status = _quick.oxy_rotary(ctypes.addressof(rotary), positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream)
+    if status is None:
+        status = lib().oxy_rotary(ctypes.byref(rotary), positions_ptr or None, x_ptr or None, x_stride,
+                                  out_ptr or None, out_stride, n_tokens, n_heads, stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_rotary_append(pool, batch, layer, rotary, positions_ptr, q_ptr, q_stride, q_out_ptr, k_ptr, k_stride,
                       v_ptr, v_stride, stream):
-    _check(lib().oxy_rotary_append(pool, batch, layer, ctypes.byref(rotary), positions_ptr or None,
-                                   q_ptr or None, q_stride, q_out_ptr or None, k_ptr or None, k_stride,
-                                   v_ptr or None, v_stride, stream or None))
+    status = _quick.oxy_rotary_append(pool, batch, layer, ctypes.addressof(rotary), positions_ptr, q_ptr, q_stride,
+                                      q_out_ptr, k_ptr, k_stride, v_ptr, v_stride, stream)
+    if status is None:
+        status = lib().oxy_rotary_append(pool, batch, layer, ctypes.byref(rotary), positions_ptr or None,
+                                         q_ptr or None, q_stride, q_out_ptr or None, k_ptr or None, k_stride,
+                                         v_ptr or None, v_stride, stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_stream_info(pool, stream_id):
@@ -402,9 +463,9 @@ def _p32(arr):
 
 def oxy_stream_blocks(pool, stream_id):
     n = oxy_stream_info(pool, stream_id)[3]
-    out = _int_array(n)
-    _check(lib().oxy_stream_blocks(pool, stream_id, _p32(out), n))
-    return out[:n].tolist()
+    out = (ctypes.c_int32 * max(n, 1))()
+    _check(lib().oxy_stream_blocks(pool, stream_id, out, n))
+    return out[:n]
 
 
 def oxy_prefix_info(pool, prefix_id):
@@ -417,9 +478,9 @@ def oxy_prefix_info(pool, prefix_id):
 
 def oxy_prefix_blocks(pool, prefix_id):
     n = oxy_prefix_info(pool, prefix_id)[1]
-    out = _int_array(n)
-    _check(lib().oxy_prefix_blocks(pool, prefix_id, _p32(out), n))
-    return out[:n].tolist()
+    out = (ctypes.c_int32 * max(n, 1))()
+    _check(lib().oxy_prefix_blocks(pool, prefix_id, out, n))
+    return out[:n]
 
 
 def oxy_pool_stats(pool):
