@@ -24,13 +24,24 @@ inline size_t layer_bytes8(int32_t num_blocks) {
   return ((size_t)num_blocks * (kBlockBytes8 + kScaleBytes8) + 255) / 256 * 256;
 }
 
-// As launch_append, launch_append_inline and launch_gather_inline, for n_layers layers that lie pool_layer_stride
-// bytes apart (sources and outputs src_layer_stride / out_layer_stride).
+// As launch_append and launch_gather_inline, the latter for n_layers layers that lie pool_layer_stride bytes apart
+// (outputs out_layer_stride).
 OXY_WEAK hipError_t launch_append8(const void* k_new, const void* v_new, const int32_t* d_slots, int32_t n_tokens,
                                    Layer8 layer, hipStream_t s);
-OXY_WEAK hipError_t launch_append_inline8(const void* k_new, const void* v_new, const InlineIds& blocks, int32_t pos0,
-                                          int32_t n_tokens, Layer8 layer, int32_t n_layers, size_t src_layer_stride,
-                                          size_t pool_layer_stride, hipStream_t s);
+// Consecutive tokens of one table: block i holds tokens 16i - offset .. of rows k, v (or to k_out, v_out), offset =
+// the first token's place in blocks[0].  Block ids travel by value, in 16 bits where they fit (ids of up to 1920 blocks
+// a launch), else in 32 (960).  n_layers layers; rows of a layer lie rows_layer_stride bytes behind the last one's.
+struct Table8 {
+  Layer8 layer;            // the first one
+  int32_t n_layers;
+  size_t pool_layer_stride, rows_layer_stride;
+  bool small_ids;          // every id of the pool is below 65536
+};
+constexpr int32_t max_table_blocks(bool small_ids) { return small_ids ? 1920 : 960; }
+OXY_WEAK hipError_t launch_append_table8(const void* k, const void* v, const Table8& t, const int32_t* blocks, int32_t offset,
+                                         int32_t n_tokens, hipStream_t s);
+OXY_WEAK hipError_t launch_gather_table8(void* k_out, void* v_out, const Table8& t, const int32_t* blocks, int32_t offset,
+                                         int32_t n_tokens, hipStream_t s);
 OXY_WEAK hipError_t launch_gather_inline8(Layer8 layer, const GatherRuns& runs, int32_t n_runs, void* k_out, void* v_out,
                                           int32_t n_layers, size_t out_layer_stride, size_t pool_layer_stride,
                                           hipStream_t s);

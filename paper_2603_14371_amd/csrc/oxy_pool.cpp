@@ -241,6 +241,10 @@ oxy::Layer8 layer8(const oxy_pool* p, int32_t layer) {
   return oxy::layer8_of(layer_base(p, layer), p->cfg.num_blocks);
 }
 
+oxy::Table8 table8(const oxy_pool* p, int32_t layer_begin, int32_t n_layers, size_t rows_layer_stride) {
+  return {layer8(p, layer_begin), n_layers, layer_bytes_of(p->cfg), rows_layer_stride, p->cfg.num_blocks <= 65536};
+}
+
 // Launches by the form the pool holds its rows in.
 hipError_t append_rows(const oxy_pool* p, int32_t layer, const void* k_new, const void* v_new, const int32_t* d_slots,
                        int32_t n_tokens, hipStream_t s) {
@@ -460,27 +464,30 @@ int32_t prefix_append_impl(oxy_pool* p, int32_t pid, int32_t layer_begin, int32_
     }
     px.len = old_len;
   };
-  // device copy, at most kMaxInlineBlocks blocks per launch (block ids travel by value)
+  // device copy, a launch for as many blocks as ids travel by value
   const char* kp = (const char*)k;
   const char* vp = (const char*)v;
   const size_t pool_layer_stride = layer_bytes_of(p->cfg);
+  const oxy::Table8 table = table8(p, layer_begin, layer_end - layer_begin, src_layer_stride);
+  const int32_t most_blocks = p->kv8 ? oxy::max_table_blocks(table.small_ids) : oxy::kMaxInlineBlocks;
   int32_t done = 0;
   while (done < n_tokens) {
     int32_t pos = pos0 + done;
     int32_t first_block = pos / kPage;
-    int32_t max_tok = (first_block + oxy::kMaxInlineBlocks) * kPage - pos;
-    int32_t n = std::min(n_tokens - done, max_tok);
-    oxy::InlineIds ids;
+    int32_t n = (int32_t)std::min<int64_t>(n_tokens - done, ((int64_t)first_block + most_blocks) * kPage - pos);
     int32_t nb = blocks_for(pos + n) - first_block;
-    for (int32_t i = 0; i < nb; ++i) ids.v[i] = px.blocks[first_block + i];
     const char* k_at = kp + (size_t)done * oxy::kDim * 2;
     const char* v_at = vp + (size_t)done * oxy::kDim * 2;
     const int32_t at = pos - first_block * kPage, layers = layer_end - layer_begin;
-    hipError_t e =
-        p->kv8 ? oxy::launch_append_inline8(k_at, v_at, ids, at, n, layer8(p, layer_begin), layers, src_layer_stride,
-                                            pool_layer_stride, (hipStream_t)hip_stream)
-               : oxy::launch_append_inline(k_at, v_at, ids, at, n, layer_base(p, layer_begin), layers, src_layer_stride,
-                                           pool_layer_stride, (hipStream_t)hip_stream);
+    hipError_t e;
+    if (p->kv8) {
+      e = oxy::launch_append_table8(k_at, v_at, table, px.blocks.data() + first_block, at, n, (hipStream_t)hip_stream);
+    } else {
+      oxy::InlineIds ids;
+      for (int32_t i = 0; i < nb; ++i) ids.v[i] = px.blocks[first_block + i];
+      e = oxy::launch_append_inline(k_at, v_at, ids, at, n, layer_base(p, layer_begin), layers, src_layer_stride,
+                                    pool_layer_stride, (hipStream_t)hip_stream);
+    }
     if (e != hipSuccess) {
       roll_back();
       return hip_fail(e, "prefix_append: launch");
@@ -1499,8 +1506,34 @@ int32_t gather_impl(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const i
   for (int32_t i = 0; i < n; ++i)
     if (slots[i] < 0 || slots[i] >= n_slots)
       return fail(OXY_ERR_INVALID_ARG, "%s: slot %lld out of range", who, (long long)slots[i]);
-  // consecutive slots of one block travel as one run (see launch_gather_inline)
+  // consecutive slots of one block travel as one run (see launch_gather_inline); in 8 bits consecutive tokens of one table
+  // as its block ids (see Table8), where there are more than a few blocks of them
+  const oxy::Table8 table = table8(p, layer_begin, layers, layer_stride);
+  int32_t ids[oxy::max_table_blocks(true)];
   for (int32_t done = 0; done < n;) {
+    if (p->kv8) {
+      const int32_t offset = (int32_t)(slots[done] & (kPage - 1));
+      const int32_t most = oxy::max_table_blocks(table.small_ids);
+      int32_t n_ids = 0, at = done;
+      while (at < n && n_ids < most) {   // whole blocks, but for the first one's start and the last one's end
+        const int64_t slot = slots[at];
+        if (at > done && (slot & (kPage - 1))) break;
+        const int32_t most_here = std::min(n - at, kPage - (int32_t)(slot & (kPage - 1)));
+        int32_t len = 1;
+        while (len < most_here && slots[at + len] == slot + len) ++len;
+        ids[n_ids++] = (int32_t)(slot / kPage);
+        at += len;
+        if ((slot & (kPage - 1)) + len < kPage) break;
+      }
+      if (at == n || n_ids >= 64) {
+        hipError_t e = oxy::launch_gather_table8((char*)k_out + (size_t)done * oxy::kDim * 2,
+                                                 (char*)v_out + (size_t)done * oxy::kDim * 2, table, ids, offset,
+                                                 at - done, (hipStream_t)hip_stream);
+        if (e != hipSuccess) return hip_fail(e, "gather_kv: launch");
+        done = at;
+        continue;
+      }
+    }
     oxy::GatherRuns runs;
     int32_t n_runs = 0;
     const int32_t first = done, end = std::min(n, done + oxy::kMaxGatherRows);

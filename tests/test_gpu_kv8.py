@@ -536,3 +536,26 @@ def test_short_tokens_beside_a_long_one_give_the_same_bits():
     alone = _only([900], [], [me], 7)
     beside = _only([900], [(0, 13, 1)], [(0, 20000, 1, 2), me], 7)
     assert np.array_equal(alone[0], beside[0]) and np.array_equal(alone[1], beside[1])
+
+
+@pytest.mark.parametrize("n,blocks,first", [(16 * 1920 + 40, 2000, 0), (16 * 1920 + 40, 2000, 7), (16 * 960 + 21, 65600, 0)])
+def test_more_tokens_than_a_launch_takes(n, blocks, first):
+    """Ids of 1920 blocks travel with a launch, or of 960 where one of the pool's needs more than 16 bits."""
+    order = np.random.default_rng(blocks).permutation(blocks)
+    order = np.roll(order, -int(np.argmax(order == blocks - 1)) + 3).tolist()      # the largest id is among them
+    c = Cache(n_layers=1, blocks=blocks, order=order)
+    k, v = _rows("normal", n, 1), _rows("normal", n, 2)
+    dk, dv = c.up(k), c.up(v)
+    pid = c.B.oxy_prefix_create(c.pool)
+    if first:
+        c.B.oxy_prefix_append(c.pool, pid, 0, dk.data_ptr(), dv.data_ptr(), first, 0, c.stream)
+    c.B.oxy_prefix_append(c.pool, pid, 0, dk[first:].data_ptr(), dv[first:].data_ptr(), n - first, first, c.stream)
+    slots = c.prefix_slots(pid)
+    assert max(slots) // 16 == blocks - 1
+    gk, gv = c.gather(0, slots)
+    pick = np.unique(np.r_[0:40, n - 60:n, 16 * 960 - 20:16 * 960 + 20, np.random.default_rng(0).integers(0, n, 500)])
+    _same_rows(gk[pick], kv8.bf16_bits(kv8.cached_values(k[pick])))
+    _same_rows(gv[pick], kv8.bf16_bits(kv8.cached_values(v[pick])))
+    backwards, _ = c.gather(0, slots[::-1])                  # another path reads the same rows
+    assert np.array_equal(backwards[::-1], gk)
+    c.close()
