@@ -74,11 +74,11 @@
  * cut into calls, what else is in its page or what was there before.  About half the memory
  * (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded up to 256): first
  * the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.
- *   K page: 16-byte chunk (jj, hf, g, k8), jj<4, hf<2, g<4, k8<8, at ((((jj*2+hf)*4+g)*8)+k8)*16
- *           holds the codes of K[8hf+k8][64jj+16g .. +15].
- *   V page: chunk (w, cp, gp, n), w<4, cp<2, gp<2, n<16, at ((((w*2+cp)*2+gp)*16)+n)*16 holds those of
- *           V[4gp..4gp+3][d], V[8+4gp..8+4gp+3][d], then the same of d+1, d = 64w+4n+2cp.
- *   exponents: K key k at 2*(k%8) + k/8; V key k at 16 + 8*((k/4)%2) + 4*(k/8) + k%4.
+ *   K page: 16-byte chunk (jj, g, key), jj<4, g<4, key<16, at ((jj*4+g)*16+key)*16 holds the codes of
+ *           K[key][64jj+16g .. +15].
+ *   V page: chunk (w, g, n), w<4, g<4, n<16, at ((w*4+g)*16+n)*16 holds those of V[4g..4g+3][d], then of
+ *           d+1, d+2 and d+3, d = 64w+4n.
+ *   exponents: K rows 0..15, then V rows 0..15.
  */
 #ifndef OXY_H
 #define OXY_H

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64 * kAppendTokens8) void append8_kernel(const uint
 }
 
 // Rows of keys key0..key0+n-1 of one block, by one workgroup: every half wavefront quantises two K rows and two V rows;
-// V is turned through LDS and goes out in whole chunks where all eight keys of one are among the rows, byte by byte
+// V is turned through LDS and goes out in whole chunks where all four keys of one are among the rows, byte by byte
 // elsewhere, so that nothing else in the page is touched.
 struct __align__(16) PageLds8 {
   uint8_t v[kPage][kDim + 16];   // +16: rows land in different banks
@@ -78,27 +78,22 @@ __device__ __forceinline__ void append_page8(const uint16_t* __restrict__ k_src,
     *(u32x2*)(&sm.v[key][8 * c]) = (u32x2){rv.codes[0], rv.codes[1]};
   }
   __syncthreads();
-  // thread t: chunk t of the V page, eight keys of dims d and d+1
-  const int gp = (t >> 4) & 1, d = 64 * (t >> 6) + 4 * (t & 15) + 2 * ((t >> 5) & 1);
-  u32x4 out = {0, 0, 0, 0};
+  // thread t: chunk t of the V page, four keys of dims d..d+3
+  const int key4 = 4 * ((t >> 4) & 3), d = 64 * (t >> 6) + 4 * (t & 15);
+  u32x4 rows;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t two = *(const uint16_t*)(&sm.v[(e < 4 ? 4 * gp : 4 + 4 * gp) + e][d]);
-    out[e >> 2] |= (two & 0xffu) << (8 * (e & 3));
-    out[2 + (e >> 2)] |= (two >> 8) << (8 * (e & 3));
-  }
+  for (int e = 0; e < 4; ++e) rows[e] = *(const uint32_t*)(&sm.v[key4 + e][d]);
+  const u32x4 out = transposed4(rows);
   char* vp = block + kPageBytes8 + t * 16;
-  if (kWhole || (key0 <= 4 * gp && key0 + n >= 12 + 4 * gp)) {
+  if (kWhole || (key0 <= key4 && key0 + n >= key4 + 4)) {
     *(u32x4*)vp = out;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int key = (e < 4 ? 4 * gp : 4 + 4 * gp) + e;
-      if (key >= key0 && key < key0 + n) {
-        vp[e] = (char)(out[e >> 2] >> (8 * (e & 3)));
-        vp[8 + e] = (char)(out[2 + (e >> 2)] >> (8 * (e & 3)));
+    for (int e = 0; e < 4; ++e)
+      if (key4 + e >= key0 && key4 + e < key0 + n) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) vp[4 * c + e] = (char)(out[c] >> (8 * e));
       }
-    }
   }
 }
 
@@ -157,9 +152,8 @@ __device__ __forceinline__ void store_values16(uint16_t* dst, const u32x4 codes,
 __device__ __forceinline__ void gather_page8(const char* __restrict__ block, const uint8_t* __restrict__ sc, const int key0,
                                              const int len, uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out,
                                              PageLds8& sm, const int t) {
-  const int gp = (t >> 4) & 1, d = 64 * (t >> 6) + 4 * (t & 15) + 2 * ((t >> 5) & 1);
-  const int lo = 4 * gp, hi = lo + 8, end = key0 + len;
-  const bool wanted = (key0 < lo + 4 && end > lo) || (key0 < hi + 4 && end > hi);   // a key of the run in the chunk
+  const int key4 = 4 * ((t >> 4) & 3), d = 64 * (t >> 6) + 4 * (t & 15), end = key0 + len;
+  const bool wanted = key0 < key4 + 4 && end > key4;   // a key of the run in the chunk
   // row `key`, dims 16c..16c+15 of this thread
   const int key = t >> 4, c = t & 15;
   const bool mine = key >= key0 && key < end;
@@ -167,14 +161,13 @@ __device__ __forceinline__ void gather_page8(const char* __restrict__ block, con
   uint32_t ek = 0, ev = 0;
   if (wanted) v = *(const u32x4*)(block + kPageBytes8 + t * 16);
   if (mine) {
-    k = *(const u32x4*)(block + k8_chunk_offset(c >> 2, key >> 3, c & 3, key & 7));
+    k = *(const u32x4*)(block + k8_chunk_offset(c >> 2, c & 3, key));
     ek = sc[k8_scale_offset(key)];
     ev = sc[v8_scale_offset(key)];
   }
+  const u32x4 rows = transposed4(v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    *(uint16_t*)(&sm.v[(e < 4 ? 4 * gp : 4 + 4 * gp) + e][d]) =
-        (uint16_t)(((v[e >> 2] >> (8 * (e & 3))) & 0xffu) | (((v[2 + (e >> 2)] >> (8 * (e & 3))) & 0xffu) << 8));
+  for (int e = 0; e < 4; ++e) *(uint32_t*)(&sm.v[key4 + e][d]) = rows[e];
   __syncthreads();
   if (mine) {
     const size_t at = (size_t)(key - key0) * kDim + 16 * c;
@@ -315,30 +308,27 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
   const int rounds = (nsteps + kRound - 1) / kRound;
   const int npg = ((wi.kv_end + 15) >> 4) - (wi.kv_begin >> 4);
 
-  u32x4 kr[kSub][8];      // kr[u][2jj+hf]: K chunk (jj, hf) of this wavefront's step u
-  u32x4 vr[kSteps][2];    // vr[s][cp]: V chunk cp of this wavefront's 64 dims, step s of the round
-  uint32_t ke[kSub];      // exponents of this lane's keys of the first product (hf = 0, 1)
-  u32x2 ve[kSub];         // of the eight keys whose logits it receives
+  // A step is two pages, and every load is of one of them: its address is a scalar, and this lane's place in a page.
+  u32x4 kr[kSub][8];      // kr[u][2jj+t]: K chunk jj of this lane's key of page t, step u of this wavefront
+  u32x4 vr[kSteps][2];    // vr[s][t]: V chunk of this wavefront's 64 dims, page t of step s of the round
+  uint32_t ke[kSub][2];   // exponent of this lane's key of page t
+  uint32_t ve[kSub][2];   // of the four keys of page t whose logits it receives
+  const uint32_t at_k = (g * 16 + n) * 16, at_v = kPageBytes8 + v8_chunk_offset(wv, g, n);
   auto page_load = [](const char* p) {
     if constexpr (kOnce) return __builtin_nontemporal_load((const u32x4*)p);
     return *(const u32x4*)p;
   };
   // A step past the split's end re-reads a page of the split; its logits are masked and its V operands are zeros.
-  auto load_k_of = [&](const int u, const int blk_a, const int blk_b) {
-    int off = (g * 8 + (n & 7)) * 16, off_k = 2 * (n & 7), off_v = kPage + 8 * (g & 1);
-    asm volatile("" : "+v"(off), "+v"(off_k), "+v"(off_v));
-    ke[u] = *(const uint16_t*)(scales + (size_t)((n >> 3) ? blk_b : blk_a) * kScaleBytes8 + off_k);
-    ve[u] = *(const u32x2*)(scales + (size_t)((g >> 1) ? blk_b : blk_a) * kScaleBytes8 + off_v);
-    const char* p = base + (size_t)((n >> 3) ? blk_b : blk_a) * kBlockBytes8 + off;
+  auto load_k_of = [&](const int u, const int t, const int blk) {
+    const uint8_t* e = scales + (size_t)(uint32_t)blk * kScaleBytes8;
+    ke[u][t] = e[(uint32_t)n];
+    ve[u][t] = *(const uint32_t*)(e + (uint32_t)(kPage + 4 * g));
+    const char* p = base + (size_t)(uint32_t)blk * kBlockBytes8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) kr[u][i] = page_load(p + i * 512);
+    for (int jj = 0; jj < 4; ++jj) kr[u][2 * jj + t] = page_load(p + at_k + jj * 1024);
   };
-  auto load_v_of = [&](const int s, const int blk_a, const int blk_b) {
-    int off = kPageBytes8 + v8_chunk_offset(wv, 0, g & 1, n);
-    asm volatile("" : "+v"(off));
-    const char* p = base + (size_t)((g >> 1) ? blk_b : blk_a) * kBlockBytes8 + off;
-#pragma unroll
-    for (int cp = 0; cp < 2; ++cp) vr[s][cp] = page_load(p + cp * 512);
+  auto load_v_of = [&](const int s, const int t, const int blk) {
+    vr[s][t] = page_load(base + (size_t)(uint32_t)blk * kBlockBytes8 + at_v);
   };
   // The block ids of the first 16 pages are in the record (no dependent load in front of the first pages), those of
   // later rounds in the block table.
@@ -347,39 +337,29 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     if (round < kInlineRounds) {
       const DescPtr id = wi.rec + 16 + 2 * kRound * round + 2 * kSub * wv;
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) load_k_of(u, id[2 * u], id[2 * u + 1]);
+      for (int i = 0; i < 2 * kSub; ++i) load_k_of(i >> 1, i & 1, id[i]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) {
-        const int pi = 2 * kRound * round + 2 * (kSub * wv + u);
-        load_k_of(u, ids[min(pi, npg - 1)], ids[min(pi + 1, npg - 1)]);
-      }
+      for (int i = 0; i < 2 * kSub; ++i) load_k_of(i >> 1, i & 1, ids[min(2 * kRound * round + 2 * kSub * wv + i, npg - 1)]);
     }
   };
   auto load_v = [&](const int round) {
     if (round < kInlineRounds) {
       const DescPtr8 id = (DescPtr8)(wi.rec + 16 + 2 * kRound * round);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) load_v_of(s, id[s / 4][2 * (s % 4)], id[s / 4][2 * (s % 4) + 1]);
+      for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, id[i / 8][i % 8]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int pi = 2 * kRound * round + 2 * s;
-        load_v_of(s, ids[min(pi, npg - 1)], ids[min(pi + 1, npg - 1)]);
-      }
+      for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, ids[min(2 * kRound * round + i, npg - 1)]);
     }
   };
-
   auto load_first_v = [&]() {   // with the ids that came with the record
     i32x8 more = wi.pages;
     if constexpr (kSteps > 4) more = ((DescPtr8)wi.rec)[3];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const i32x8 ids = s < 4 ? wi.pages : more;
-      load_v_of(s, ids[2 * (s % 4)], ids[2 * (s % 4) + 1]);
-    }
+    for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, i < 8 ? wi.pages[i % 8] : more[i % 8]);
   };
 
   // The queries first: loads complete in order, so the barrier below waits for them only.  Fragment 2jj+i of a row holds
@@ -405,7 +385,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     };
     if (kSteps == 2 && wv >= 2) {
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) ke[u] = 0, ve[u] = (u32x2){0, 0};
+      for (int u = 0; u < kSub; ++u) ke[u][0] = ke[u][1] = ve[u][0] = ve[u][1] = 0;
       load_first_v();
       store_q();
     } else {
@@ -443,7 +423,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       if (kSteps != 2 || wv < 2) {
 #pragma unroll
         for (int r = 0; r < G; ++r) s0[u][r] = s1[u][r] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        const float ks0 = scale_of(ke[u] & 0xffu), ks1 = scale_of(ke[u] >> 8);
+        const float ks0 = scale_of(ke[u][0]), ks1 = scale_of(ke[u][1]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const u32x4 a0 = kr[u][2 * (j >> 1)], a1 = kr[u][2 * (j >> 1) + 1];
@@ -459,7 +439,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
 #pragma unroll
         for (int e = 0; e < 8; ++e) vb[u][e] = (int)((ve[u][e >> 2] >> (8 * (e & 3))) & 0xffu);
         if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
-          int k0 = pos + 16 * (g >> 1) + 4 * (g & 1);
+          int k0 = pos + 4 * g;
           asm volatile("" : "+v"(k0));   // a branch: as selects the masks are a quarter of a round's instructions
 #pragma unroll
           for (int r = 0; r < G; ++r) {
@@ -467,12 +447,12 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               s0[u][r][e] = e < end ? s0[u][r][e] : ninf;
-              s1[u][r][e] = 8 + e < end ? s1[u][r][e] : ninf;
+              s1[u][r][e] = 16 + e < end ? s1[u][r][e] : ninf;
             }
           }
           // the exponent byte of a slot that was never written may be anything
 #pragma unroll
-          for (int e = 0; e < 8; ++e) vb[u][e] = (e < 4 ? e : 4 + e) < wi.kv_end - k0 ? vb[u][e] : 0;
+          for (int e = 0; e < 8; ++e) vb[u][e] = (e < 4 ? e : 12 + e) < wi.kv_end - k0 ? vb[u][e] : 0;
         }
       } else {
 #pragma unroll
@@ -555,7 +535,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     __syncthreads();
     auto operands = [&](const int s, u32x4 (&v)[4]) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = f16_operand(vr[s][c >> 1][2 * (c & 1)], vr[s][c >> 1][2 * (c & 1) + 1]);
+      for (int c = 0; c < 4; ++c) v[c] = f16_operand(vr[s][0][c], vr[s][1][c]);
     };
     auto contract = [&](const int s, const int r, const u32x4 (&v)[4]) {
       const u32x4 w = sm.p[s * G + r][lane];
@@ -578,10 +558,9 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       auto clear_past_end = [&](const int s) {   // codes of slots beyond the end may be anything
         const int left_s = wi.kv_end - (wi.kv_begin + 32 * (kRound * round + s));
         if (left_s < 32) {
-          const int k0 = 16 * (g >> 1) + 4 * (g & 1);
-          const uint32_t m0 = byte_mask(left_s - k0), m1 = byte_mask(left_s - k0 - 8);
-#pragma unroll
-          for (int cp = 0; cp < 2; ++cp) vr[s][cp] &= (u32x4){m0, m1, m0, m1};
+          const uint32_t m0 = byte_mask(left_s - 4 * g), m1 = byte_mask(left_s - 16 - 4 * g);
+          vr[s][0] &= (u32x4){m0, m0, m0, m0};
+          vr[s][1] &= (u32x4){m1, m1, m1, m1};
         }
       };
       auto finish_group = [&](const int r) {

@@ -8,22 +8,25 @@ namespace oxy {
 // ------------------------------------------------------------------------------------------
 // page layout (see oxy.h)
 // ------------------------------------------------------------------------------------------
-// K page: chunk (jj, hf, g, k8) holds K[8hf+k8][64jj+16g .. +15]
-__device__ __forceinline__ int k8_chunk_offset(int jj, int hf, int g, int k8) {
-  return ((((jj * 2 + hf) * 4 + g) * 8) + k8) * 16;
-}
-// V page: chunk (w, cp, gp, n) holds eight keys (4gp..4gp+3, 8+4gp..8+4gp+3) of dim d = 64w+4n+2cp, then those of d+1
-__device__ __forceinline__ int v8_chunk_offset(int w, int cp, int gp, int n) {
-  return ((((w * 2 + cp) * 2 + gp) * 16) + n) * 16;
-}
+// K page: chunk (jj, g, key) holds K[key][64jj+16g .. +15]
+__device__ __forceinline__ int k8_chunk_offset(int jj, int g, int key) { return ((jj * 4 + g) * 16 + key) * 16; }
+// V page: chunk (w, g, n) holds four keys 4g..4g+3 of dim d = 64w+4n, then those of d+1, d+2 and d+3
+__device__ __forceinline__ int v8_chunk_offset(int w, int g, int n) { return ((w * 4 + g) * 16 + n) * 16; }
 // byte of (dim d, key)
 __device__ __forceinline__ int v8_offset(int d, int key) {
-  return v8_chunk_offset(d >> 6, (d >> 1) & 1, (key >> 2) & 1, (d >> 2) & 15) + (d & 1) * 8 + v_slot_of_key(key);
+  return v8_chunk_offset(d >> 6, key >> 2, (d >> 2) & 15) + (d & 3) * 4 + (key & 3);
 }
-// A block's exponent bytes: lane k8 of the first product wants those of keys k8 and 8+k8, a lane of the second those of
-// its eight keys (in the order of a V chunk).
-__device__ __forceinline__ int k8_scale_offset(int key) { return 2 * (key & 7) + (key >> 3); }
-__device__ __forceinline__ int v8_scale_offset(int key) { return kPage + ((key >> 2) & 1) * 8 + v_slot_of_key(key); }
+// A block's exponent bytes: its K rows', then its V rows'.
+__device__ __forceinline__ int k8_scale_offset(int key) { return key; }
+__device__ __forceinline__ int v8_scale_offset(int key) { return kPage + key; }
+
+// Rows and columns of a 4 x 4 square of bytes (a word per row) change places.
+__device__ __forceinline__ u32x4 transposed4(const u32x4 r) {
+  const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+  return (u32x4){__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u),
+                 __builtin_amdgcn_perm(d, b, 0x05040100u), __builtin_amdgcn_perm(d, b, 0x07060302u)};
+}
 
 __device__ __forceinline__ float scale_of(uint32_t exponent_byte) { return __uint_as_float(exponent_byte << 23); }
 
@@ -81,10 +84,10 @@ __device__ __forceinline__ Row8 quantise_row(const u32x4 x) {
 }
 __device__ __forceinline__ void store_key(const Row8& r, int key, char* __restrict__ block, uint8_t* __restrict__ scales,
                                           int c) {
-  *(u32x2*)(block + k8_chunk_offset(c >> 3, key >> 3, (c >> 1) & 3, key & 7) + (c & 1) * 8) = (u32x2){r.codes[0], r.codes[1]};
+  *(u32x2*)(block + k8_chunk_offset(c >> 3, (c >> 1) & 3, key) + (c & 1) * 8) = (u32x2){r.codes[0], r.codes[1]};
   if (c == 0) scales[k8_scale_offset(key)] = (uint8_t)r.exponent;
 }
-// dims 8c..8c+7 of one key: two chunks of each pair of dims, byte by byte
+// dims 8c..8c+7 of one key, byte by byte
 __device__ __forceinline__ void store_value(const Row8& r, int key, char* __restrict__ block, uint8_t* __restrict__ scales,
                                             int c) {
   char* p = block + kPageBytes8;
