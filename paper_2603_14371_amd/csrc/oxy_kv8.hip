@@ -570,7 +570,8 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
           const f32x4 lw = *(const f32x4*)sm.ls[r][lane];
           const float total = row_sum4((lw[0] + lw[1]) + (lw[2] + lw[3]));
           if (g == 0 && 2 * r + sub < wi.n_tok)
-            *(f32x2*)(a.part_ml + ((size_t)slot * kHeads + (n & 7)) * 4) = (f32x2){m[r], total};
+            // a sum that is not a number has no reference, and would pass for that of a row without visible keys
+            *(f32x2*)(a.part_ml + ((size_t)slot * kHeads + (n & 7)) * 4) = (f32x2){total != total ? 0.f : m[r], total};
         }
       };
       if constexpr (G == 1) {

@@ -559,3 +559,107 @@ def test_more_tokens_than_a_launch_takes(n, blocks, first):
     backwards, _ = c.gather(0, slots[::-1])                  # another path reads the same rows
     assert np.array_equal(backwards[::-1], gk)
     c.close()
+
+
+@pytest.mark.parametrize("where", ["prefix", "chunk", "history", "only"])
+@pytest.mark.parametrize("bits", [0x7f80, 0xff80, 0x7fc0], ids=["inf", "-inf", "nan"])
+def test_a_key_that_is_not_finite_leaves_no_finite_output(where, bits):
+    """Held as NaN, it makes the logits of the queries that see it NaN, also where a split has no other key; all others
+    equal the oracle's."""
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    pid = b.prefix(300, b.recipe(300, tag=100))
+    act, dec, one = b.stream(pid, ACTION), b.stream(pid, DECODE), b.stream(pid, DECODE)
+    b.tag = 10
+    b.step([(dec, 150)], attend=False)                 # tag 10
+    b.step([(act, 50), (dec, 1), (one, 1)])            # tag 11
+    w = _workload("nan_key", 5181, 1, 512, b.trace)
+    src = synth.DataSource(w["seed"])
+    tag, row = {"prefix": (100, 17), "chunk": (11, 9), "history": (10, 70), "only": (11, 51)}[where]
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "k" and recipe["tag"] == tag:
+            x[row - recipe["tok0"], 77] = bits
+        return x
+
+    gw = GpuWorld(w, planted, poison=True, kv8=True)
+    ow = OracleWorld(w["num_blocks"], 1, kv8.cached_source(src), w["scale"])
+    for op in w["trace"]:
+        g, o = gw.apply(op), ow.apply(op)
+    gw.close()
+    got, ref = g["O"][0], o["O"][0]
+    sees = {"prefix": list(range(52)), "chunk": list(range(50)), "history": [50], "only": [51]}[where]
+    assert np.isnan(widen_bf16(got[sees])).all() and np.isnan(g["LSE"][0][sees]).all()
+    rest = np.setdiff1d(np.arange(len(ref)), sees)
+    if len(rest):
+        assert_o_close(got[rest], ref[rest], where)
+        assert_lse_close(g["LSE"][0][rest], o["LSE"][0][rest], where)
+
+
+def test_a_query_that_is_not_finite_leaves_the_others_alone():
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    pid = b.prefix(300)
+    act, dec = b.stream(pid, ACTION), b.stream(pid, DECODE)
+    b.step([(act, 9), (dec, 1)])
+    w = _workload("nan_query", 77, 1, 64, b.trace)
+    src = synth.DataSource(w["seed"])
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "q":
+            x[3, 2, 100], x[9, 5, 0] = 0x7fc0, 0x7f80
+        return x
+
+    gw = GpuWorld(w, planted, kv8=True)
+    ow = OracleWorld(w["num_blocks"], 1, kv8.cached_source(src), w["scale"])
+    for op in w["trace"]:
+        g, o = gw.apply(op), ow.apply(op)
+    gw.close()
+    bad = np.zeros((10, 8), dtype=bool)
+    bad[3, 2] = bad[9, 5] = True
+    got = widen_bf16(g["O"][0])
+    assert not np.isfinite(got[bad]).any() and not np.isfinite(g["LSE"][0][bad]).any()
+    for r in range(10):
+        ok = ~bad[r]
+        assert_o_close(g["O"][0][r][ok], o["O"][0][r][ok], "row %d" % r)
+
+
+@pytest.mark.parametrize("sizes", ["zeros", "zeros_then_normal", "tiny", "huge"])
+def test_values_at_the_ends_of_the_range(sizes):
+    """Rows of zeros (the lowest exponent), of 2^-120 and of 2^120: the unit that an item's sums go by follows."""
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    pid = b.prefix(400, b.recipe(400, tag=100))
+    act, dec = b.stream(pid, ACTION), b.stream(pid, DECODE)
+    b.step([(dec, 600)], attend=False)
+    b.step([(act, 20), (dec, 1)])
+    w = _workload("ends", 13, 1, 128, b.trace)
+    src = synth.DataSource(w["seed"])
+    shift = {"tiny": -120, "huge": 120}.get(sizes, 0)
+
+    def sized(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "v":
+            at = np.arange(n) + recipe["tok0"]
+            if sizes == "zeros":
+                x[:] = 0
+            elif sizes == "zeros_then_normal":
+                x[at % 256 < 128] = 0
+            else:                                # exponents moved, as far as they stay those of normal numbers
+                e = (x >> 7) & 0xff
+                moved = np.clip(e.astype(np.int32) + shift, 1, 250)
+                x = ((x & 0x807f) | (moved << 7)).astype(np.uint16)
+        return x
+
+    gw = GpuWorld(w, sized, kv8=True, poison=True)
+    ow = OracleWorld(w["num_blocks"], 1, kv8.cached_source(sized), w["scale"])
+    for op in w["trace"]:
+        g, o = gw.apply(op), ow.apply(op)
+    gw.close()
+    if sizes == "zeros":
+        assert not (g["O"][0] & 0x7fff).any()
+    else:
+        assert_o_close_scaled(g["O"][0], o["O"][0], 2.0 ** shift)
+    assert_lse_close(g["LSE"][0], o["LSE"][0], sizes)
