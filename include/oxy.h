@@ -71,7 +71,11 @@
  *   value_i = code_i * 2^e            (a bf16 number; infinite where |x_i| >= 1.9375 * 2^127 makes it 2^128)
  * Every call takes and returns bf16 as with a bf16 pool; the attention is that of the values, and
  * oxy_gather_kv returns them.  What a row holds depends on that row alone, not on how a history was
- * cut into calls, what else is in its page or what was there before.  About half the memory
+ * cut into calls, what else is in its page or what was there before.  Probabilities meet the values in
+ * fp16: a value counts to 2^-11 of itself, and to 2^-32 of the largest value among the same few hundred
+ * keys.  A key that is not finite makes the outputs of the queries that see it NaN; a value that is not
+ * finite the dim, or its 64 dims, of those queries, and of tokens before it in the same chunk of new tokens.
+ * About half the memory
  * (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded up to 256): first
  * the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.
  *   K page: 16-byte chunk (jj, g, key), jj<4, g<4, key<16, at ((jj*4+g)*16+key)*16 holds the codes of
@@ -285,7 +289,7 @@ int32_t oxy_batch_destroy(oxy_batch *batch);
 int32_t oxy_gather_kv(oxy_pool *pool, int32_t layer, const int64_t *slots, int32_t n,
                       void *k_out, void *v_out, void *hip_stream);
 /* The same of layers [layer_begin, layer_end): layer l's rows go to k_out + (l - layer_begin) * layer_stride
- * and v_out likewise (bytes, at least n * 512).  On a pool in 8 bits one launch serves all the layers. */
+ * and v_out likewise (bytes, at least n * 512, a multiple of 16).  On a pool in 8 bits one launch serves all the layers. */
 int32_t oxy_gather_kv_layers(oxy_pool *pool, int32_t layer_begin, int32_t layer_end,
                              const int64_t *slots, int32_t n, void *k_out, void *v_out,
                              size_t layer_stride, void *hip_stream);
@@ -297,7 +301,7 @@ int32_t oxy_gather_kv_layers(oxy_pool *pool, int32_t layer_begin, int32_t layer_
  * bf16 once.  The gradient, or the way back (amplitude 1), is the call with negated positions. */
 enum { OXY_ROTARY_HALVES = 0,  /* pairs (i, i + rot_dims / 2) */
        OXY_ROTARY_PAIRS = 1 }; /* pairs (2i, 2i + 1)          */
-enum { OXY_ROTARY_MAX_HEADS = 1024 };
+enum { OXY_ROTARY_MAX_HEADS = 1024, OXY_ROTARY_MAX_TOKENS = 1 << 25 };
 typedef struct {
   int32_t rot_dims;    /* even, 2..256                                              */
   int32_t layout;

@@ -1502,6 +1502,8 @@ int32_t gather_impl(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const i
   const int32_t layers = layer_end - layer_begin;
   if (layers > 1 && layer_stride < (size_t)n * oxy::kDim * 2)
     return fail(OXY_ERR_INVALID_ARG, "%s: layer stride below %d rows", who, n);
+  if (layers > 1 && layer_stride & 15)
+    return fail(OXY_ERR_INVALID_ARG, "%s: layer stride must be a multiple of 16", who);
   const int64_t n_slots = (int64_t)p->cfg.num_blocks * kPage;
   for (int32_t i = 0; i < n; ++i)
     if (slots[i] < 0 || slots[i] >= n_slots)
@@ -1594,6 +1596,8 @@ int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
     return fail(OXY_ERR_INVALID_ARG, "rotary_append: stride below a token's rows");
   if (b->n_tokens > 1 && (k_stride > UINT32_MAX || v_stride > UINT32_MAX || (q && q_stride > UINT32_MAX)))
     return fail(OXY_ERR_INVALID_ARG, "rotary_append: stride of 4 GiB or more");
+  if (b->n_tokens > 1 && q && q == q_out && q_stride != oxy::kHeads * row)
+    return fail(OXY_ERR_INVALID_ARG, "rotary_append: queries in place need a stride of 4096");
   const int32_t* d_desc = (const int32_t*)p->slots[b->slot].d_base;
   oxy::RotaryAppendArgs a;
   a.rotary = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};

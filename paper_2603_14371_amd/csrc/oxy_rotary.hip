@@ -339,10 +339,12 @@ int32_t oxy_rotary(const oxy_rotary_config* c, const int32_t* positions, const v
   if (!c || !c->freqs || !positions || !x || !out) return refuse("rotary: null argument");
   if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2) return refuse("rotary: rot_dims must be even, 2 to 256");
   if (c->layout != OXY_ROTARY_HALVES && c->layout != OXY_ROTARY_PAIRS) return refuse("rotary: unknown layout");
-  if (n_tokens < 0 || n_heads < 1 || n_heads > OXY_ROTARY_MAX_HEADS) return refuse("rotary: n_tokens or n_heads");
+  if (n_tokens < 0 || n_tokens > OXY_ROTARY_MAX_TOKENS || n_heads < 1 || n_heads > OXY_ROTARY_MAX_HEADS)
+    return refuse("rotary: n_tokens or n_heads");
   const size_t row = (size_t)n_heads * oxy::kDim * 2;
   if (((uintptr_t)x | (uintptr_t)out | x_stride | out_stride) & 15) return refuse("rotary: rows must be 16-byte aligned");
   if (n_tokens > 1 && (x_stride < row || out_stride < row)) return refuse("rotary: stride below n_heads rows");
+  if (n_tokens > 1 && x == out && x_stride != out_stride) return refuse("rotary: in place with two strides");
   const oxy::RotaryArgs r = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};
   const hipError_t e = oxy::launch_rotary(r, x, x_stride, out, out_stride, n_tokens, n_heads, (hipStream_t)hip_stream);
   if (e != hipSuccess) {

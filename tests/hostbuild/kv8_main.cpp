@@ -162,13 +162,16 @@ int main() {
       }
       const double* f = (const double*)rows;
       oxy_rotary_config r = {64, OXY_ROTARY_PAIRS, f, 1.0};
-      void* a = (void*)((uintptr_t)1 << 30);
+      void *a = (void*)((uintptr_t)1 << 30), *out = (char*)a + 65536;
       g_rotary = 0;
-      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, 5120, a, a, 5120, a, 5120, nullptr) == OXY_OK && g_rotary == 1);
+      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, 5120, out, a, 5120, a, 5120, nullptr) == OXY_OK && g_rotary == 1);
       CHECK(g_rotary_args.n_tokens == 3 && g_rotary_args.scales && g_rotary_args.q_stride == 5120 && g_rotary_args.rotary.pairs);
       CHECK((char*)g_rotary_args.layer_base == (char*)c.kv_base + c.kv_bytes / 2);
-      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, (size_t)1 << 32, a, a, 5120, a, 5120, nullptr) == OXY_ERR_INVALID_ARG);
+      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, (size_t)1 << 32, out, a, 5120, a, 5120, nullptr) == OXY_ERR_INVALID_ARG);
+      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, 5120, a, a, 5120, a, 5120, nullptr) == OXY_ERR_INVALID_ARG);
       CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, nullptr, 0, nullptr, a, 512, a, 512, nullptr) == OXY_OK && g_rotary == 2);
+      CHECK(oxy_rotary_append(p, b, 1, &r, (const int32_t*)a, a, 4096, a, a, 5120, a, 5120, nullptr) == OXY_OK && g_rotary == 3);
+      CHECK(oxy_gather_kv_layers(p, 0, 2, slot_of.data(), 3, rows, rows, 1544, nullptr) == OXY_ERR_INVALID_ARG);
       CHECK(oxy_batch_destroy(b) == OXY_OK);
     }
     CHECK(oxy_pool_destroy(p) == OXY_OK);

@@ -212,7 +212,7 @@ def test_rotating_append_refuses():
                 dict(rotary=B.make_rotary(d, 255)), dict(rotary=B.make_rotary(d, 258)), dict(rotary=B.make_rotary(d, 0)),
                 dict(rotary=B.make_rotary(d, 256, 2)), dict(pos=0), dict(qo=0), dict(k=0), dict(v=0), dict(q=p + 2),
                 dict(k=p + 8), dict(v=p + 4), dict(qo=p + 8), dict(qs=4088), dict(qs=4080), dict(ks=504), dict(ks=496),
-                dict(vs=16)):
+                dict(vs=16), dict(qo=p)):
         a = dict(good, **bad)
         with pytest.raises(B.OxyError) as e:
             B.oxy_rotary_append(a["pool"], a["batch"], a["layer"], a["rotary"], a["pos"], a["q"], a["qs"], a["qo"], a["k"],

@@ -111,7 +111,7 @@ A16 = 1 << 20     # an aligned address that no refused call reads
 @pytest.mark.parametrize("kw", [
     dict(rot=0), dict(rot=3), dict(rot=512), dict(layout=2), dict(layout=-1), dict(freqs=0), dict(positions=0), dict(x=0),
     dict(out=0), dict(x=A16 + 2), dict(out=A16 + 8), dict(x_stride=4096 + 8), dict(x_stride=4096 - 16),
-    dict(out_stride=512), dict(n=-1), dict(heads=0), dict(heads=1025, x_stride=1 << 20, out_stride=1 << 20),
+    dict(out_stride=512), dict(n=(1 << 25) + 1), dict(out_stride=8192), dict(n=-1), dict(heads=0), dict(heads=1025, x_stride=1 << 20, out_stride=1 << 20),
 ], ids=str)
 def test_rotary_refuses(kw):
     a = dict(dict(rot=256, layout=0, freqs=A16, positions=A16, x=A16, out=A16, x_stride=4096, out_stride=4096, n=4,
