@@ -271,8 +271,8 @@ struct __align__(16) WorkLds8 {
   float ls[kMaxGroups][64][4];     // sum of a lane's P over each wavefront's keys
 };
 
-// One work item: up to 2*G query tokens against one split of a KV source, in rounds of kSub * 128 keys, as `attend` in
-// oxy_kernels.hip: wavefront w takes the logits of its kSub 32-key steps and contracts all keys of the round for dims
+// One work item: up to 2*G query tokens against one split of a KV source, in rounds of 128 keys, as `attend` in
+// oxy_kernels.hip: wavefront w takes the logits of its 32-key step and contracts all keys of the round for dims
 // 64w..64w+63.  A round of 128 keys is 32 + 32 registers of codes (64 + 64 in bf16).  A K operand is converted once
 // for all groups, with its rows' exponents as the conversion's scale.  A lane's eight V codes are of eight keys, so
 // theirs go into P.
@@ -285,14 +285,11 @@ struct __align__(16) WorkLds8 {
 // when vref grows, which a power of two does exactly.
 //
 // A row's arithmetic does not depend on G or on the other rows.
-// kSteps: 32-key steps of a round that are loaded: 4 * kSub, or 2 for a split of at most 64 keys.
-// kSub 2 (own pages of more than 128 keys in a split, one group): all 256 keys' pages in flight at once.
+// kSteps: 32-key steps of a round that are loaded: 4, or 2 for a split of at most 64 keys.
 // kOnce: non-temporal page loads (see kOnceBytes).
 template <int G, bool kOnce, int kSteps>
 __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
-  constexpr int kLate8 = 5 * 8, kSub = kSteps == 8 ? 2 : 1;
-  constexpr int kRound = 4 * kSub;   // steps
-  static_assert(kSteps <= 4 * kMaxGroups / G, "P of a round");
+  constexpr int kLate8 = 5 * 8, kRound = 4;   // steps
   AttnArgs8 a = early_args;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));   // what comes from the thread id stays inside this instance
@@ -309,23 +306,23 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
   const int npg = ((wi.kv_end + 15) >> 4) - (wi.kv_begin >> 4);
 
   // A step is two pages, and every load is of one of them: its address is a scalar, and this lane's place in a page.
-  u32x4 kr[kSub][8];      // kr[u][2jj+t]: K chunk jj of this lane's key of page t, step u of this wavefront
+  u32x4 kr[8];            // kr[2jj+t]: K chunk jj of this lane's key of page t, this wavefront's step
   u32x4 vr[kSteps][2];    // vr[s][t]: V chunk of this wavefront's 64 dims, page t of step s of the round
-  uint32_t ke[kSub][2];   // exponent of this lane's key of page t
-  uint32_t ve[kSub][2];   // of the four keys of page t whose logits it receives
+  uint32_t ke[2];         // exponent of this lane's key of page t
+  uint32_t ve[2];         // of the four keys of page t whose logits it receives
   const uint32_t at_k = (g * 16 + n) * 16, at_v = kPageBytes8 + v8_chunk_offset(wv, g, n);
   auto page_load = [](const char* p) {
     if constexpr (kOnce) return __builtin_nontemporal_load((const u32x4*)p);
     return *(const u32x4*)p;
   };
   // A step past the split's end re-reads a page of the split; its logits are masked and its V operands are zeros.
-  auto load_k_of = [&](const int u, const int t, const int blk) {
+  auto load_k_of = [&](const int t, const int blk) {
     const uint8_t* e = scales + (size_t)(uint32_t)blk * kScaleBytes8;
-    ke[u][t] = e[(uint32_t)n];
-    ve[u][t] = *(const uint32_t*)(e + (uint32_t)(kPage + 4 * g));
+    ke[t] = e[(uint32_t)n];
+    ve[t] = *(const uint32_t*)(e + (uint32_t)(kPage + 4 * g));
     const char* p = base + (size_t)(uint32_t)blk * kBlockBytes8;
 #pragma unroll
-    for (int jj = 0; jj < 4; ++jj) kr[u][2 * jj + t] = page_load(p + at_k + jj * 1024);
+    for (int jj = 0; jj < 4; ++jj) kr[2 * jj + t] = page_load(p + at_k + jj * 1024);
   };
   auto load_v_of = [&](const int s, const int t, const int blk) {
     vr[s][t] = page_load(base + (size_t)(uint32_t)blk * kBlockBytes8 + at_v);
@@ -335,20 +332,21 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
   constexpr int kInlineRounds = kWorkInlinePages / (2 * kRound);
   auto load_k = [&](const int round) {
     if (round < kInlineRounds) {
-      const DescPtr id = wi.rec + 16 + 2 * kRound * round + 2 * kSub * wv;
-#pragma unroll
-      for (int i = 0; i < 2 * kSub; ++i) load_k_of(i >> 1, i & 1, id[i]);
+      const DescPtr id = wi.rec + 16 + 2 * kRound * round + 2 * wv;
+      load_k_of(0, id[0]);
+      load_k_of(1, id[1]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
-#pragma unroll
-      for (int i = 0; i < 2 * kSub; ++i) load_k_of(i >> 1, i & 1, ids[min(2 * kRound * round + 2 * kSub * wv + i, npg - 1)]);
+      const int at = 2 * kRound * round + 2 * wv;
+      load_k_of(0, ids[min(at, npg - 1)]);
+      load_k_of(1, ids[min(at + 1, npg - 1)]);
     }
   };
   auto load_v = [&](const int round) {
     if (round < kInlineRounds) {
       const DescPtr8 id = (DescPtr8)(wi.rec + 16 + 2 * kRound * round);
 #pragma unroll
-      for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, id[i / 8][i % 8]);
+      for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, id[0][i]);
     } else {
       const DescPtr ids = (DescPtr)a.tables + wi.tbl_off + (wi.kv_begin >> 4);
 #pragma unroll
@@ -356,10 +354,8 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     }
   };
   auto load_first_v = [&]() {   // with the ids that came with the record
-    i32x8 more = wi.pages;
-    if constexpr (kSteps > 4) more = ((DescPtr8)wi.rec)[3];
 #pragma unroll
-    for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, i < 8 ? wi.pages[i % 8] : more[i % 8]);
+    for (int i = 0; i < 2 * kSteps; ++i) load_v_of(i >> 1, i & 1, wi.pages[i]);
   };
 
   // The queries first: loads complete in order, so the barrier below waits for them only.  Fragment 2jj+i of a row holds
@@ -384,8 +380,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
         for (int i = 0; i < 2; ++i) sm.q[r][2 * wv + i][lane] = query_sign(a, qtmp[r][i]);
     };
     if (kSteps == 2 && wv >= 2) {
-#pragma unroll
-      for (int u = 0; u < kSub; ++u) ke[u][0] = ke[u][1] = ve[u][0] = ve[u][1] = 0;
+      ke[0] = ke[1] = ve[0] = ve[1] = 0;
       load_first_v();
       store_q();
     } else {
@@ -413,69 +408,62 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     int lane_now = tid & 63;
     asm volatile("" : "+v"(lane_now));
     const int lane = lane_now, n = lane & 15, g = lane >> 4, sub = n >> 3;
-    f32x4 s0[kSub][G], s1[kSub][G];
-    int vb[kSub][8];   // exponent bytes of this lane's values, 0 for keys that are not there
+    f32x4 s0[G], s1[G];
+    int vb[8];   // exponent bytes of this lane's values, 0 for keys that are not there
+    const int pos = wi.kv_begin + 32 * (kRound * round + wv);
+    const int left = wi.kv_end - pos;
+    const bool need_mask = (kLast && left < 32) || pos + 31 > wi.q0;
+    if (kSteps != 2 || wv < 2) {
 #pragma unroll
-    for (int u = 0; u < kSub; ++u) {
-      const int pos = wi.kv_begin + 32 * (kRound * round + kSub * wv + u);
-      const int left = wi.kv_end - pos;
-      const bool need_mask = (kLast && left < 32) || pos + 31 > wi.q0;
-      if (kSteps != 2 || wv < 2) {
+      for (int r = 0; r < G; ++r) s0[r] = s1[r] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      const float ks0 = scale_of(ke[0]), ks1 = scale_of(ke[1]);
 #pragma unroll
-        for (int r = 0; r < G; ++r) s0[u][r] = s1[u][r] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        const float ks0 = scale_of(ke[u][0]), ks1 = scale_of(ke[u][1]);
+      for (int j = 0; j < 8; ++j) {
+        const u32x4 a0 = kr[2 * (j >> 1)], a1 = kr[2 * (j >> 1) + 1];
+        const u32x4 k0 = bf16_operand(a0[2 * (j & 1)], a0[2 * (j & 1) + 1], ks0);
+        const u32x4 k1 = bf16_operand(a1[2 * (j & 1)], a1[2 * (j & 1) + 1], ks1);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const u32x4 a0 = kr[u][2 * (j >> 1)], a1 = kr[u][2 * (j >> 1) + 1];
-          const u32x4 k0 = bf16_operand(a0[2 * (j & 1)], a0[2 * (j & 1) + 1], ks0);
-          const u32x4 k1 = bf16_operand(a1[2 * (j & 1)], a1[2 * (j & 1) + 1], ks1);
-#pragma unroll
-          for (int r = 0; r < G; ++r) {
-            const u32x4 q = sm.q[r][j][lane];
-            s0[u][r] = mfma16(k0, q, s0[u][r]);
-            s1[u][r] = mfma16(k1, q, s1[u][r]);
-          }
+        for (int r = 0; r < G; ++r) {
+          const u32x4 q = sm.q[r][j][lane];
+          s0[r] = mfma16(k0, q, s0[r]);
+          s1[r] = mfma16(k1, q, s1[r]);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vb[u][e] = (int)((ve[u][e >> 2] >> (8 * (e & 3))) & 0xffu);
-        if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
-          int k0 = pos + 4 * g;
-          asm volatile("" : "+v"(k0));   // a branch: as selects the masks are a quarter of a round's instructions
-#pragma unroll
-          for (int r = 0; r < G; ++r) {
-            const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              s0[u][r][e] = e < end ? s0[u][r][e] : ninf;
-              s1[u][r][e] = 16 + e < end ? s1[u][r][e] : ninf;
-            }
-          }
-          // the exponent byte of a slot that was never written may be anything
-#pragma unroll
-          for (int e = 0; e < 8; ++e) vb[u][e] = (e < 4 ? e : 12 + e) < wi.kv_end - k0 ? vb[u][e] : 0;
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < G; ++r) s0[u][r] = s1[u][r] = (f32x4){ninf, ninf, ninf, ninf};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vb[u][e] = 0;
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vb[e] = (int)((ve[e >> 2] >> (8 * (e & 3))) & 0xffu);
+      if (need_mask) {   // wave-uniform: only the end of a split or the causal diagonal
+        int k0 = pos + 4 * g;
+        asm volatile("" : "+v"(k0));   // a branch: as selects the masks are a quarter of a round's instructions
+#pragma unroll
+        for (int r = 0; r < G; ++r) {
+          const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s0[r][e] = e < end ? s0[r][e] : ninf;
+            s1[r][e] = 16 + e < end ? s1[r][e] : ninf;
+          }
+        }
+        // the exponent byte of a slot that was never written may be anything
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vb[e] = (e < 4 ? e : 12 + e) < wi.kv_end - k0 ? vb[e] : 0;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < G; ++r) s0[r] = s1[r] = (f32x4){ninf, ninf, ninf, ninf};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vb[e] = 0;
     }
     {
       float mx[G];
 #pragma unroll
       for (int r = 0; r < G; ++r) {
-        mx[r] = largest8(s0[0][r], s1[0][r]);
-        if constexpr (kSub == 2) mx[r] = fmaxf(mx[r], largest8(s0[kSub - 1][r], s1[kSub - 1][r]));
-        mx[r] *= sl2;
+        mx[r] = largest8(s0[r], s1[r]) * sl2;
       }
       const float mine = row_max4_each(mx);
       if (g < G) sm.mx[g][n][wv] = mine;
       int top = 1;
 #pragma unroll
-      for (int u = 0; u < kSub; ++u)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, vb[u][e]);
+      for (int e = 0; e < 8; ++e) top = max(top, vb[e]);
       top = (int)rows4_largest((uint32_t)top);   // the same in all lanes of 16
       if (lane == 0) sm.top[wv] = top;
     }
@@ -514,20 +502,16 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
         m[r] = up ? mx[r] : m[r];
       }
     }
+    // 2^(exponent - vref + 7); for a key that is not there (P is 0) something finite
+    float factor[8];
 #pragma unroll
-    for (int u = 0; u < kSub; ++u) {
-      // 2^(exponent - vref + 7); for a key that is not there (P is 0) something finite
-      float factor[8];
+    for (int e = 0; e < 8; ++e) factor[e] = __uint_as_float((uint32_t)max((vb[e] << 23) + ((127 + 7 - vref) << 23), 0));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) factor[e] = __uint_as_float((uint32_t)max((vb[u][e] << 23) + ((127 + 7 - vref) << 23), 0));
-#pragma unroll
-      for (int r = 0; r < G; ++r) {
-        u32x4 w;
-        l[r] += weights8(s0[u][r], s1[u][r], sl2, (m[r] == ninf) ? 0.f : m[r], factor, w);
-        sm.p[(kSub * wv + u) * G + r][lane] = w;
-        if constexpr (kLast)
-          if (u == kSub - 1) sm.ls[r][lane][wv] = l[r];
-      }
+    for (int r = 0; r < G; ++r) {
+      u32x4 w;
+      l[r] += weights8(s0[r], s1[r], sl2, (m[r] == ninf) ? 0.f : m[r], factor, w);
+      sm.p[wv * G + r][lane] = w;
+      if constexpr (kLast) sm.ls[r][lane][wv] = l[r];
     }
     __builtin_amdgcn_sched_barrier(0);   // the next K chunks reuse kr[]
     if constexpr (!kLast) load_k(round + 1);
@@ -632,12 +616,8 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
   const int path_word = head[W_PATH];
   if ((path_word & kPathMask) == PATH_NOOP) return;
   const bool few_keys = wi.kv_end - wi.kv_begin <= 64;
-  if (path_word & kPathAppends) {   // one or two tokens on their own pages
-    if (wi.kv_end - wi.kv_begin > 128)
-      path_word & kPathOnce ? attend8<1, true, 8>(a, wi, sm) : attend8<1, false, 8>(a, wi, sm);
-    else
-      path_word & kPathOnce ? attend8<1, true, 4>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
-  }
+  if (path_word & kPathAppends)   // one or two tokens on their own pages
+    path_word & kPathOnce ? attend8<1, true, 4>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
   else if (wi.n_tok > 4)
     few_keys ? attend8<4, false, 2>(a, wi, sm) : attend8<4, false, 4>(a, wi, sm);
   else if (wi.n_tok > 2)

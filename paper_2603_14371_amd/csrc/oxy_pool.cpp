@@ -220,9 +220,12 @@ constexpr int64_t kOnceBytes = 128 << 20;   // see kPathOnce in oxy_batch_build
 // Streaming path on an item's own history.  A history of at most 512 tokens is cut into
 // 128-token work items (one step per wavefront: steps that wait for memory one after the other
 // are what such a launch is made of), a longer one into 256-token work items (two steps per
-// wavefront; halves the work items and split results of a launch that is bound by bytes).
+// wavefront; halves the work items and split results of a launch that is bound by bytes).  In 8 bits one of more than
+// 65536 tokens, which brings work for every CU by itself, into 512-token ones (a layer of one request of 131072 tokens
+// 16.5 us, so 15.6; three 40.8 / 37.8; one of 66000 13.8 / 12.6, four 29.4 / 30.9; one of 40000 9.2, so 11.5).
 int32_t stream_split_for(const oxy_pool_config& c, int32_t len) {
   if (c.stream_split_tokens) return c.stream_split_tokens;
+  if (c.flags & OXY_POOL_KV_FP8 && len > 65536) return 512;
   return len <= 512 ? 128 : 256;
 }
 

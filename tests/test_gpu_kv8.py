@@ -207,7 +207,7 @@ def test_read_back_of_several_layers_is_that_of_each(bits8):
                 assert np.array_equal(rows, want)
                 assert not got[at + n * 512:at + stride].any()
     for bad in (dict(layer_begin=2, layer_end=2), dict(layer_begin=-1, layer_end=2), dict(layer_end=5),
-                dict(stride=100), dict(slots=[64 * 16]), dict(slots=[-1])):
+                dict(stride=100), dict(stride=len(live) * 512 + 8), dict(slots=[64 * 16]), dict(slots=[-1])):
         a = dict(dict(layer_begin=0, layer_end=4, slots=live, stride=len(live) * 512), **bad)
         with pytest.raises(B.OxyError):
             B.oxy_gather_kv_layers(gw.pool, a["layer_begin"], a["layer_end"], a["slots"], k.data_ptr(), v.data_ptr(),
@@ -663,3 +663,126 @@ def test_values_at_the_ends_of_the_range(sizes):
     else:
         assert_o_close_scaled(g["O"][0], o["O"][0], 2.0 ** shift)
     assert_lse_close(g["LSE"][0], o["LSE"][0], sizes)
+
+
+@pytest.mark.parametrize("own", [65536, 65537])
+def test_histories_of_more_than_65536_tokens(own):
+    """Longer ones are cut into splits of 512."""
+    b = _TraceBuilder()
+    d = b.stream(-1, DECODE)
+    b.step([(d, own - 2)], attend=False)
+    b.step([(d, 2)])
+    w = _workload("longer", 23, 1, 4100, b.trace)
+    gw, _ = run_both8(w, poison=True, max_partials=1024)
+    gw.close()
+
+
+@pytest.mark.parametrize("own", [40, 9000], ids=["short", "merged_by_many"])
+def test_a_captured_layer_follows_its_inputs(own):
+    """Turning, storing, attention and read-back captured twice (two graphs of one batch, and a second batch), replayed
+    in turn with eager work and new inputs between: every replay gives what eager calls give."""
+    import torch
+    from paper_2603_14371_amd import binding as B
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    pid = b.prefix(500)
+    act, dec = b.stream(pid, ACTION), b.stream(pid, DECODE)
+    b.step([(dec, own)], attend=False)
+    w = _workload("captured", 3, 2, 800, b.trace)
+    gw = GpuWorld(w, synth.DataSource(3), kv8=True, poison=True, max_q_tokens=64)
+    gw.run(w["trace"])
+    freqs = torch.from_numpy(B.oxy_rotary_freqs(10000.0, 128)[0]).cuda()
+    turn = B.make_rotary(freqs.data_ptr(), 128)
+    batches, buffers, graphs = [], [], []
+    for m in (1, 2):
+        items = [(act, 20), (dec, m)]
+        batches.append(B.oxy_batch_build(gw.pool, items, 0, gw._stream()))
+        n = 20 + m
+        buffers.append(dict(n=n, wide=torch.zeros((n, 10, 256), dtype=torch.bfloat16, device="cuda"),
+                            pos=torch.zeros(n, dtype=torch.int32, device="cuda"),
+                            q=torch.zeros((n, 8, 256), dtype=torch.bfloat16, device="cuda"),
+                            o=torch.zeros((2, n, 8, 256), dtype=torch.bfloat16, device="cuda"),
+                            lse=torch.zeros((2, n, 8), device="cuda"),
+                            kv=torch.zeros((2, 2, n, 256), dtype=torch.bfloat16, device="cuda")))
+
+    def layer_calls(i, s):
+        t, batch = buffers[i], batches[i]
+        wide = t["wide"]
+        slots = B.oxy_batch_slots(batch)
+        B.oxy_rotary(turn, t["pos"].data_ptr(), wide.data_ptr(), 5120, wide.data_ptr(), 5120, t["n"], 1, s)
+        for layer in range(2):
+            B.oxy_rotary_append(gw.pool, batch, layer, turn, t["pos"].data_ptr(), wide.data_ptr(), 5120, t["q"].data_ptr(),
+                                wide[:, 8].data_ptr(), 5120, wide[:, 9].data_ptr(), 5120, s)
+            B.oxy_mixed_attention(gw.pool, batch, layer, t["q"].data_ptr(), t["o"][layer].data_ptr(),
+                                  t["lse"][layer].data_ptr(), 0.0625, s)
+        B.oxy_gather_kv_layers(gw.pool, 0, 2, slots, t["kv"][0].data_ptr(), t["kv"][1].data_ptr(), t["n"] * 512, s)
+
+    def fill(i, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        t = buffers[i]
+        t["wide"].normal_(generator=g)
+        t["pos"].random_(0, 9000, generator=g)
+        for x in ("q", "o", "lse", "kv"):
+            t[x].fill_(7)
+
+    def results(i):
+        torch.cuda.synchronize()
+        return [buffers[i][x].clone() for x in ("wide", "q", "o", "lse", "kv")]
+
+    side = torch.cuda.Stream()
+    for i in (0, 0, 1):
+        fill(i, 0)
+        layer_calls(i, gw._stream())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            layer_calls(i, torch.cuda.current_stream().cuda_stream)
+        graphs.append((i, graph))
+    for seed in range(1, 5):
+        for i, graph in graphs:
+            fill(i, seed)
+            layer_calls(i, gw._stream())
+            want = results(i)
+            fill(i, seed)
+            torch.cuda.synchronize()
+            graph.replay()
+            for x, y in zip(want, results(i)):
+                assert torch.equal(x, y) and torch.isfinite(x).all()
+    del graphs
+    for batch in batches:
+        B.oxy_batch_destroy(batch)
+    gw.close()
+
+
+def test_recordings_on_both_sides_of_the_merge_by_many():
+    """A request whose split results pass 32 while its steps are recorded and replayed."""
+    import torch
+    from paper_2603_14371_amd import binding as B
+    from paper_2603_14371_amd.harness import GpuWorld, bits_of, to_device_bf16
+    b = _TraceBuilder()
+    pid = b.prefix(100)
+    dec = b.stream(pid, DECODE)
+    b.step([(dec, 30 * 32 - 3)], attend=False)
+    w = _workload("passes", 8, 2, 100, b.trace)
+    data = synth.DataSource(8)
+    outs = {}
+    for flags in (0, B.STEP_GRAPH):
+        gw = GpuWorld(w, data, kv8=True, stream_split_tokens=32, max_q_tokens=16)
+        gw.run(w["trace"])
+        s, parts = gw._stream(), []
+        k, v, q = (torch.stack([to_device_bf16(data(b.recipe(1, tag=5), l, x, 1), gw.device) for l in range(2)]) for x in "kvq")
+        o, lse, got = torch.zeros_like(q), torch.zeros((2, 1, 8), device="cuda"), []
+        for step in range(8):
+            batch = B.oxy_batch_build(gw.pool, [(dec, 1)], 0, s)
+            parts.append(B.oxy_batch_info(batch)[3])
+            o.zero_()
+            B.oxy_step_layers(gw.pool, batch, 0, 2, k.data_ptr(), v.data_ptr(), 512, q.data_ptr(), o.data_ptr(), 4096,
+                              lse.data_ptr(), 32, gw.scale, flags, None, s)
+            torch.cuda.synchronize()
+            got.append((bits_of(o), lse.cpu().numpy().copy()))
+            B.oxy_batch_destroy(batch)
+        outs[flags] = got
+        assert min(parts) == 32 and max(parts) == 33
+        gw.close()
+    for a, c in zip(outs[0], outs[B.STEP_GRAPH]):
+        assert np.array_equal(a[0], c[0]) and np.array_equal(a[1], c[1]) and a[0].any()
