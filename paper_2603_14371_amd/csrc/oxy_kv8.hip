@@ -11,11 +11,12 @@
 // was cut into calls.
 //
 // Attention.  The work items, splits, rounds and split results are those of a bf16 cache (see oxy_kernels.hip, `attend`);
-// what differs is what lies in memory: half the bytes, turned into bf16 operands in registers.  The products stay in bf16:
-// the 8-bit matrix instructions round their own sums to about 2^-16 of the products' 2-norm (rms 1.5e-5, up to 5e-5 with
+// what differs is what lies in memory: half the bytes, turned into 16-bit operands in registers, bf16 for the logits
+// (queries are bf16, a value of the cache is a bf16 number) and fp16 for the sums of values (see `attend8`).  The 8-bit
+// matrix instructions round their own sums to about 2^-16 of the products' 2-norm (rms 1.5e-5, up to 5e-5 with
 // products of different size, measured on sums of 128), which a log-sum-exp in 32 bits would show, and queries and
 // probabilities would have to be split into two and three 8-bit parts.  A conversion of two codes takes about 5 cycles
-// of a wavefront: 128 of them a round beside 48 matrix instructions of 16 cycles per 16 query rows.
+// of a wavefront: 128 of them a round of 128 keys, beside 32 matrix instructions of 16 cycles per 16 query rows.
 #include "oxy_kv8_device.h"
 #include "oxy_merge.h"
 
@@ -28,7 +29,8 @@ namespace oxy {
 // ------------------------------------------------------------------------------------------
 // quantised append
 // ------------------------------------------------------------------------------------------
-// One wavefront per token: the first half takes the key, the second the value.
+// One wavefront per token: the first half takes the key, the second the value.  Bound by the chain slot - row - largest
+// element - codes: 58 tokens 2.3 us a launch, 1338 tokens 3.7 (2.1 MB).
 constexpr int kAppendTokens8 = 4;   // wavefronts, and tokens, of a workgroup
 __global__ __launch_bounds__(64 * kAppendTokens8) void append8_kernel(const uint16_t* __restrict__ k_new,
                                                                       const uint16_t* __restrict__ v_new,
@@ -175,7 +177,8 @@ __device__ __forceinline__ void gather_page8(const char* __restrict__ block, con
     store_values16(v_out + at, *(const u32x4*)(&sm.v[key][16 * c]), scale_of(ev));
   }
 }
-// Runs of slots anywhere, one workgroup per run, blockIdx.y = layer.
+// Runs of slots anywhere, one workgroup per run, blockIdx.y = layer.  Bound as an append is: 1338 tokens of 4 histories in
+// 6 layers 5.2 us (12.3 MB).
 __global__ __launch_bounds__(256) void gather8_kernel(const char* __restrict__ blocks, const uint8_t* __restrict__ scales,
                                                       const GatherRuns runs, uint16_t* __restrict__ k_out,
                                                       uint16_t* __restrict__ v_out, size_t out_layer_stride,
@@ -285,8 +288,19 @@ struct __align__(16) WorkLds8 {
 // when vref grows, which a power of two does exactly.
 //
 // A row's arithmetic does not depend on G or on the other rows.
-// kSteps: 32-key steps of a round that are loaded: 4, or 2 for a split of at most 64 keys.
-// kOnce: non-temporal page loads (see kOnceBytes).
+// kSteps: 32-key steps of a round that are loaded: 4, or 2 for a split of at most 64 keys (eight chunks and eight
+// requests on 832 tokens 14.6 us a layer, so 14.3; eight causal chunks of 20 tokens 10.25 / 9.95; eight chunks on 2048
+// tokens 18.7 / 18.95).
+// kOnce: non-temporal page loads (see kOnceBytes; 64 requests on eight prefixes of 2048 tokens 16.35 us a layer, so 15.4;
+// 256 on 32 44.1 / 41.1).
+//
+// What bounds it.  Small launches: the chain record - pages - logits - P - sums, 2.7 us, and the two launches themselves
+// (one chunk and one request 6.85 us a layer, one request 5.7).  Chunks: eight of 64 on 2048 tokens take 18.9 us with
+// the merge, of which the first loads of 512 workgroups are 2.4 us and a SIMD issues vector instructions for 5.4 us
+// (128 conversions and 300 others a round) and matrix ones for 3.6 (128 a round of eight tokens), which overlap little; no phase taken
+// out alone saves more than 1 us.  Bytes where histories are long: 131072 tokens 12.9 us, 5.2 TB/s.
+// Not kept, for the same launches: a group's softmax beside another's products in program order, raised wave
+// priorities, four workgroups per CU (registers spill), rounds of 256 keys.
 template <int G, bool kOnce, int kSteps>
 __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
   constexpr int kLate8 = 5 * 8, kRound = 4;   // steps
@@ -630,11 +644,12 @@ static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "atten
 // ------------------------------------------------------------------------------------------
 // merge of tokens with many split results
 // ------------------------------------------------------------------------------------------
-// A wavefront per token and head takes 0.9 us for every 16 split results behind the first (29 us for the 512 of a history
-// of 131072 tokens: two workgroups read 2 MB in turn).  Here a token of more than kLongParts results takes a workgroup for
-// each head and 64 dims: eight wavefronts share the results out, 64 at a time with everything in flight at once, each with
-// a maximum of its own, and the first one joins the eight.  Tokens of fewer are merged by one wavefront as in every
-// other launch, so that a token's bits do not depend on what else is in the batch.
+// A wavefront per token and head takes 0.9 us for every 16 split results behind the first (29 us for 512: two workgroups
+// read 2 MB in turn).  Here a token of more than kLongParts results takes a workgroup for each head and 64 dims: eight
+// wavefronts share the results out, 64 at a time with everything in flight at once, each with a maximum of its own, and the
+// first one joins the eight (256 results of a history of 131072 tokens 3 us).  Tokens of fewer are merged by one wavefront
+// as in every other launch, so that a token's bits do not depend on what else is in the batch.  us per layer with a limit
+// of 16 / 32 / 64: one history of 6000 tokens 8.3 / 8.6 / 8.9, 16 of 4000 15.1 / 13.9 / 13.9, one of 10000 8.6 / 8.6 / 9.8.
 constexpr int kLongWaves = 8, kLongAhead = 16;   // a wavefront's loads: kLongAhead times four results of 128 bytes
 __global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint16_t* part_acc, const float* part_ml, void* out,
                                                                     float* lse, const int32_t* n_parts,

@@ -690,7 +690,10 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
       int32_t n_new, tile, split;   // new tokens, query tokens per work item, keys per split
     };
     // In 8 bits a chunk's keys are in the pool when the work items run (appends quantise in a launch of their own), so
-    // its own phase is an item like any other: one split, as many tokens as share an item of its prefix.
+    // its own phase is an item like any other: one split, as many tokens as share an item of its prefix (always 8: one
+    // chunk + one request 9.1 us a layer, so 6.85; eight requests and a chunk 9.25 / 7.55; eight chunks the same).  A
+    // causal chunk's items have as many tokens in every launch, because their keys depend on it: 4 (eight of 20 tokens
+    // 9.95 us, two of 50 8.05; 8: 10.05 and 9.25; 2: no faster, and half as many items again).
     int32_t chunk_tile8 = 8;
     auto own_cut = [&](const Plan& pl) {
       OwnCut o;
@@ -745,7 +748,10 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
     // requests on one 10.9 / 12.5 / 15.6, 32 requests on two (336 items of pairs) 16.4 / 12.6 / 16.8,
     // 64 requests on eight 22.9 / 17.1 / 20.1, eight chunks 37.0 / 30.9 / 26.8.  (On a prefix longer
     // than 1024 tokens the width was always 8: with splits of 160 or 192 tokens, five or six steps
-    // in two rounds, small launches took 15.2 us a layer where pairs take 10.9.)
+    // in two rounds, small launches took 15.2 us a layer where pairs take 10.9.)  In 8 bits (pairs / 4 / 8): one chunk +
+    // one request 6.85 / 7.6 / 9.65, four chunks 12.1 / 10.0 / 10.7, eight 18.8 / 14.9 / 14.0; on 2048 tokens eight 25.2 /
+    // 20.4 / 18.9, 64 requests on eight with two chunks 20.8 / 17.5 / 15.1; and pairs for two items a CU on a long prefix
+    // too: 32 requests on two of 2048 tokens 8.05 / 9.1, nine with six drafts each on one 8.65 / 9.75.
     int32_t width = 8;
     {
       int64_t other = 0, pairs = 0, by4 = 0, by8 = 0, limited = 0, for_pairs = 512;
@@ -771,7 +777,7 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
         by4 += ns * ((g.n_tok + 3) / 4);
         by8 += ns * ((g.n_tok + 7) / 8);
         limited += g.px->len <= 1024 ? in_pairs : ns * ((g.n_tok + 7) / 8);
-        if (g.px->len > 1024) for_pairs = 256;
+        if (g.px->len > 1024 && !p->kv8) for_pairs = 256;
       }
       // The limit holds for pairs on a prefix of at most 1024 tokens and for tiles of 8 on a longer
       // one, whatever width the launch ends up with; a narrower form is taken only if it fits too.

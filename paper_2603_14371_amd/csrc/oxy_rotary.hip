@@ -27,8 +27,8 @@ enum RotaryForm { FORM_PAIRS, FORM_HALVES, FORM_HALVES_ANY };
 // Cosine and sine of position * freq times the amplitude, rounded to 32 bits once.  The angle is brought to a fraction of a
 // turn, then to within an eighth of one around the nearest quarter, where the series of the two functions are cut where
 // their next terms are below 1e-11 (a fiftieth of a thousandth of half a unit of the 32-bit result).  20 instructions in 64
-// bits, which run at the rate of 32 (the library's sincospi, whose last bits are rounded off here, takes three times as many: prefill of
-// 8192 tokens 20.7 us, now 17.5).
+// bits, which run at the rate of 32 (with the library's sincospi, whose last bits are rounded off here, three times as
+// many: nine heads of 8192 tokens 20.7 us, with this 17.5).
 __device__ __forceinline__ void turn_of(const double freq, const double amplitude, const int position, float& c, float& s) {
   const double turns = (double)position * freq * 0.15915494309189533577;   // 1 / (2 pi)
   const double part = turns - rint(turns), quarter = rint(4.0 * part);
@@ -111,8 +111,8 @@ __device__ __forceinline__ LaneTurns turns_of_lane(const float* cs, const float*
   }
   return r;
 }
-// By all lanes of a half wavefront.  In a prefill partners come from other lanes (loaded a second time instead: 8192
-// tokens 21.9 us, so 19.9); in a step they are loaded, while the angles are taken (58 tokens 2.85 us; from lanes 3.05).
+// By all lanes of a half wavefront.  In a prefill partners come from other lanes (8192 tokens 19.9 us; loaded a second
+// time 21.9); in a step they are loaded, while the angles are taken (58 tokens 2.85 us; from lanes 3.05).
 template <int kForm, bool kPartners>
 __device__ __forceinline__ u32x4 turned(RowLoad x, const LaneTurns& w, const int rot, const int c) {
 #pragma clang fp contract(off)
@@ -140,7 +140,8 @@ __device__ __forceinline__ u32x4 turned(RowLoad x, const LaneTurns& w, const int
 
 // kTokens of a workgroup: their angles are taken once for all heads, by all threads, and come to the lanes through LDS.
 // With four, two half wavefronts share a token's heads; with one, all eight do.  A half wavefront keeps its cosines and
-// sines, and kRows rows in flight.
+// sines, and kRows rows in flight.  Nine heads of 8192 tokens (75 MB) 18.0 us in halves, 17.0 in pairs: 4.2 and 4.4 TB/s;
+// of 64 tokens 2.6 us.
 template <int kForm, int kTokens>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const char* x, const size_t x_stride, char* out,
                                                      const size_t out_stride, const int32_t n_tokens,
@@ -188,7 +189,8 @@ struct RotaryLate {
   uint8_t* scales;
   double amplitude;
 };
-// One token per workgroup: ten half wavefronts take its eight query rows, its key and its value.  The addresses of the
+// One token per workgroup: ten half wavefronts take its eight query rows, its key and its value (58 tokens 2.8
+// us a launch: the chain position - angle - LDS - row).  The addresses of the
 // first loads are preloaded into scalar registers (see build.py).
 template <int kForm, bool kBits8>
 __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* positions, const char* q, const char* k_new,
@@ -241,6 +243,8 @@ __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* posit
 }
 
 namespace {
+// From here on there are four tokens for every CU's two resident workgroups and more, and four share one's start.  One /
+// four per workgroup, nine heads in halves: 2048 tokens 5.19 / 5.27 us, 3000 6.77 / 6.64, 8192 18.3 / 17.7.
 constexpr int kManyTokens = 2049;
 int form_of(const RotaryArgs& r) {
   return r.pairs ? FORM_PAIRS : (r.rot_dims >> 1) % 8 == 0 ? FORM_HALVES : FORM_HALVES_ANY;
@@ -262,7 +266,6 @@ void launch_append_form(const RotaryAppendArgs& a, hipStream_t s) {
 hipError_t launch_rotary(const RotaryArgs& r, const void* x, size_t x_stride, void* out, size_t out_stride,
                          int32_t n_tokens, int32_t n_heads, hipStream_t s) {
   if (n_tokens <= 0) return hipSuccess;
-  // four tokens share a workgroup's start where there are enough of them for every CU
   const bool many = n_tokens >= kManyTokens;
   const auto launch = [&](auto one, auto four) {
     const dim3 grid(many ? (n_tokens + 3) / 4 : n_tokens);
