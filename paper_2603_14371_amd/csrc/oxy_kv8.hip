@@ -30,8 +30,12 @@ namespace oxy {
 // quantised append
 // ------------------------------------------------------------------------------------------
 // One wavefront per token: the first half takes the key, the second the value.  Bound by the chain slot - row - largest
-// element - codes: 58 tokens 2.3 us a launch, 1338 tokens 3.7 (2.1 MB).
+// element - codes, and for many tokens by the byte stores of V.
 constexpr int kAppendTokens8 = 4;   // wavefronts, and tokens, of a workgroup
+// From here on 16 tokens a workgroup (append_many8_kernel).  One token a wavefront / 16 a workgroup: 58 tokens 2.9 / 4.1 us,
+// 1338 of four requests 3.8 / 3.85, 2048 of 512 4.3 / 4.8, 4096 of one 6.3 / 4.15, 16384 17.5 / 8.5, 131072 107 / 41.6
+// (4.8 TB/s; 48.8 where they start inside a chunk).
+constexpr int kManyAppend8 = 2049;
 __global__ __launch_bounds__(64 * kAppendTokens8) void append8_kernel(const uint16_t* __restrict__ k_new,
                                                                       const uint16_t* __restrict__ v_new,
                                                                       const int32_t* __restrict__ slots,
@@ -96,6 +100,61 @@ __device__ __forceinline__ void append_page8(const uint16_t* __restrict__ k_src,
 #pragma unroll
         for (int c = 0; c < 4; ++c) vp[4 * c + e] = (char)(out[c] >> (8 * e));
       }
+  }
+}
+
+// 16 tokens of any slots by one workgroup, rows as above.  Tokens that follow each other in their slots over four keys of one
+// chunk leave as whole chunks of V, the others byte by byte, a byte per thread.
+__global__ __launch_bounds__(256) void append_many8_kernel(const uint16_t* __restrict__ k_new,
+                                                           const uint16_t* __restrict__ v_new,
+                                                           const int32_t* __restrict__ slots, char* __restrict__ blocks,
+                                                           uint8_t* __restrict__ scales, const int32_t n_tokens) {
+  __shared__ PageLds8 sm;
+  const int tok0 = blockIdx.x * 16, n = min(16, n_tokens - tok0);
+  const int t = threadIdx.x, c = t & 31;
+  u32x4 k[2], v[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const size_t at = (size_t)(tok0 + min((t >> 5) + 8 * i, n - 1)) * kDim + c * 8;
+    k[i] = *(const u32x4*)(k_new + at);
+    v[i] = *(const u32x4*)(v_new + at);
+  }
+  const int j16 = t & 15;
+  const int slot = slots[tok0 + min(j16, n - 1)];   // of token j16, in every 16 lanes
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int j = (t >> 5) + 8 * i;
+    const Row8 rk = quantise_row(k[i]), rv = quantise_row(v[i]);
+    const int mine = __shfl(slot, j);
+    if (j < n) {
+      uint8_t* sc = scales + (size_t)(mine >> 4) * kScaleBytes8;
+      store_key(rk, mine & 15, blocks + (size_t)(mine >> 4) * kBlockBytes8, sc, c);
+      if (c == 0) sc[v8_scale_offset(mine & 15)] = (uint8_t)rv.exponent;
+    }
+    *(u32x2*)(&sm.v[j][8 * c]) = (u32x2){rv.codes[0], rv.codes[1]};
+  }
+  // bit j: token j + 1 has the next slot; token j starts a chunk whose other three follow it
+  const uint32_t next = (uint32_t)__ballot(j16 + 1 < n && __shfl(slot, (j16 + 1) & 15) == slot + 1) & 0xffffu;
+  const uint32_t starts = (uint32_t)__ballot((slot & 3) == 0) & next & (next >> 1) & (next >> 2);
+  uint32_t rest = ((1u << n) - 1u) & ~(starts | starts << 1 | starts << 2 | starts << 3);
+  __syncthreads();
+  {
+    const int wv = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    uint32_t left = starts;   // the (lane >> 4)-th of at most four
+    for (int i = 0; i < (lane >> 4); ++i) left &= left - 1;
+    const int j = left ? __builtin_ctz(left) : 0;
+    const int first = __shfl(slot, j);
+    if (left) {
+      u32x4 rows;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rows[e] = *(const uint32_t*)(&sm.v[j + e][64 * wv + 4 * (lane & 15)]);
+      *(u32x4*)(blocks + (size_t)(first >> 4) * kBlockBytes8 + kPageBytes8 + v8_chunk_offset(wv, (first >> 2) & 3, lane & 15)) =
+          transposed4(rows);
+    }
+  }
+  for (; rest; rest &= rest - 1) {
+    const int j = __builtin_ctz(rest), mine = __builtin_amdgcn_readlane(slot, j);
+    blocks[(size_t)(mine >> 4) * kBlockBytes8 + kPageBytes8 + v8_offset(t, mine & 15)] = (char)sm.v[j][t];
   }
 }
 
@@ -737,8 +796,12 @@ __global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint1
 hipError_t launch_append8(const void* k_new, const void* v_new, const int32_t* d_slots, int32_t n_tokens, Layer8 layer,
                           hipStream_t s) {
   if (n_tokens <= 0) return hipSuccess;
-  append8_kernel<<<(n_tokens + kAppendTokens8 - 1) / kAppendTokens8, 64 * kAppendTokens8, 0, s>>>(
-      (const uint16_t*)k_new, (const uint16_t*)v_new, d_slots, layer.blocks, layer.scales, n_tokens);
+  if (n_tokens >= kManyAppend8)
+    append_many8_kernel<<<(n_tokens + 15) / 16, 256, 0, s>>>((const uint16_t*)k_new, (const uint16_t*)v_new, d_slots,
+                                                             layer.blocks, layer.scales, n_tokens);
+  else
+    append8_kernel<<<(n_tokens + kAppendTokens8 - 1) / kAppendTokens8, 64 * kAppendTokens8, 0, s>>>(
+        (const uint16_t*)k_new, (const uint16_t*)v_new, d_slots, layer.blocks, layer.scales, n_tokens);
   return hipGetLastError();
 }
 

@@ -786,3 +786,49 @@ def test_recordings_on_both_sides_of_the_merge_by_many():
         gw.close()
     for a, c in zip(outs[0], outs[B.STEP_GRAPH]):
         assert np.array_equal(a[0], c[0]) and np.array_equal(a[1], c[1]) and a[0].any()
+
+
+@pytest.mark.parametrize("lens,first", [([2049], [0]), ([2061], [3]), ([1] * 2100, [5]), (None, None)],
+                         ids=["whole", "ragged", "single", "mixed"])
+def test_large_appends_store_what_small_ones_do(lens, first):
+    """More than 2048 tokens go by another kernel; an append that turns by nothing stores the same rows one by one."""
+    import torch
+    from paper_2603_14371_amd import binding as B
+    rng = np.random.default_rng(5)
+    if lens is None:
+        lens = rng.integers(1, 60, 90).tolist()
+        first = rng.integers(0, 30, 90).tolist()
+    first = first * (len(lens) // len(first))
+    n = sum(lens)
+    assert n > 2048
+    x = rng.standard_normal((2, n, 256)) * 2.0 ** rng.integers(-30, 30, (2, n, 1))
+    x[0, 7], x[1, 9], x[0, 11, 3], x[1, 12, 200] = 0, 0, np.inf, np.nan
+    rows = torch.from_numpy(x).cuda().to(torch.bfloat16)
+    positions = torch.zeros(n, dtype=torch.int32, device="cuda")
+    freqs = torch.ones(1, dtype=torch.float64, device="cuda")
+    stored = []
+    for turning in (False, True):
+        blocks = sum((m + f + 15) // 16 for m, f in zip(lens, first))
+        order = np.random.default_rng(1).permutation(blocks).tolist()
+        cfg = B.make_config(2, blocks, flags=B.POOL_KV_FP8, max_q_tokens=16, max_append_tokens=16 * blocks, free_order=order)
+        kv = torch.full((B.oxy_kv_bytes(cfg),), 0x5a, dtype=torch.uint8, device="cuda")
+        ws = torch.empty(B.oxy_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        cfg.kv_base, cfg.kv_bytes, cfg.workspace, cfg.workspace_bytes = kv.data_ptr(), kv.numel(), ws.data_ptr(), ws.numel()
+        pool, s = B.oxy_pool_create(cfg), torch.cuda.current_stream().cuda_stream
+        sids = [B.oxy_stream_create(pool, -1, DECODE) for _ in lens]
+        before = [(sid, f) for sid, f in zip(sids, first) if f]
+        if before:                                   # these rows stay unwritten
+            B.oxy_batch_destroy(B.oxy_batch_build(pool, before, B.BATCH_APPEND_ONLY, s))
+        batch = B.oxy_batch_build(pool, list(zip(sids, lens)), B.BATCH_APPEND_ONLY, s)
+        if turning:
+            B.oxy_rotary_append(pool, batch, 1, B.make_rotary(freqs.data_ptr(), 2), positions.data_ptr(), 0, 0, 0,
+                                rows[0].data_ptr(), 512, rows[1].data_ptr(), 512, s)
+        else:
+            B.oxy_stream_append(pool, batch, 1, rows[0].data_ptr(), rows[1].data_ptr(), s)
+        torch.cuda.synchronize()
+        stored.append(kv.cpu().numpy())
+        B.oxy_batch_destroy(batch)
+        B.oxy_pool_destroy(pool)
+    assert np.array_equal(*stored)
+    half = len(stored[0]) // 2
+    assert (stored[0][:half] == 0x5a).all() and (stored[0][half:] != 0x5a).sum() > 500 * n
