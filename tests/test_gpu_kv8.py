@@ -832,3 +832,58 @@ def test_large_appends_store_what_small_ones_do(lens, first):
     assert np.array_equal(*stored)
     half = len(stored[0]) // 2
     assert (stored[0][:half] == 0x5a).all() and (stored[0][half:] != 0x5a).sum() > 500 * n
+
+
+@pytest.mark.parametrize("seed", range(100, 108))
+def test_random_traces(seed):
+    """Forks, rewinds, releases, chunks, drafts and histories in any order, a pool full of NaN bytes; at the end every
+    live row is read back."""
+    from test_gpu_fuzz import random_trace
+    gw, ow = run_both8(random_trace(seed), layers=[0, 2], poison=True, max_q_tokens=1024, max_append_tokens=4096)
+    assert_pool_contents_equal(gw, ow)
+    gw.close()
+
+
+def test_blocks_beyond_4_gib():
+    """Block ids whose bytes lie past 32 bits, codes and exponents: written by all three appends, read back, attended."""
+    b = _TraceBuilder()
+    pid = b.prefix(333)
+    act, dec = b.stream(pid, ACTION), b.stream(pid, DECODE)
+    b.step([(dec, 3000)], attend=False)
+    b.step([(act, 30), (dec, 1)])
+    n = (9 << 29) // 8192
+    order = np.roll(np.arange(n, dtype=np.int32)[::-1], -3)
+    gw, ow = run_both8(_workload("far", 41, 1, n, b.trace, free_order=order), max_partials=4096)
+    assert gw.prefix_slots(pid)[0] * 512 > 1 << 32
+    assert_pool_contents_equal(gw, ow)
+    gw.close()
+
+
+@pytest.mark.parametrize("hist", [50, 9000], ids=["short", "merged_by_many"])
+def test_kernels_carry_their_events(hist):
+    import ctypes
+    import torch
+    from paper_2603_14371_amd import binding as B
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    dec = b.stream(b.prefix(200), DECODE)
+    b.step([(dec, hist)], attend=False)
+    w = _workload("events", 8, 2, 800, b.trace)
+    gw = GpuWorld(w, synth.DataSource(8), kv8=True, max_q_tokens=16)
+    gw.run(w["trace"])
+    x, s = torch.randn(2, 1, 8, 256, device="cuda").to(torch.bfloat16), gw._stream()
+    outs = [torch.zeros_like(x) for _ in range(2)]
+    events = [torch.cuda.Event(enable_timing=True) for _ in range(8)]
+    for e in events:
+        e.record()                                  # creates the handle
+    raw = (ctypes.c_void_p * 8)(*[e.cuda_event for e in events])
+    batch = B.oxy_batch_build(gw.pool, [(dec, 1)], 0, s)
+    for out, ev in zip(outs, (None, raw)):
+        B.oxy_step_layers(gw.pool, batch, 0, 2, x.data_ptr(), x.data_ptr(), 4096, x.data_ptr(), out.data_ptr(), 4096, 0, 0,
+                          gw.scale, 0, ev, s)
+    torch.cuda.synchronize()
+    for i in range(0, 8, 2):
+        assert 0 < events[i].elapsed_time(events[i + 1]) < 10
+    assert torch.equal(*outs) and outs[0].any()
+    B.oxy_batch_destroy(batch)
+    gw.close()
