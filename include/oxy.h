@@ -74,7 +74,7 @@
  * cut into calls, what else is in its page or what was there before.  Probabilities meet the values in
  * fp16: a value counts to 2^-11 of itself, and to 2^-32 of the largest value among the same few hundred
  * keys.  A key that is not finite makes the outputs of the queries that see it NaN; a value that is not
- * finite the dim, or its 64 dims, of those queries, and of tokens before it in the same chunk of new tokens.
+ * finite the dim, or its 64 dims, of those queries; other queries are as without it.
  * About half the memory
  * (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded up to 256): first
  * the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.

@@ -350,6 +350,7 @@ struct __align__(16) WorkLds8 {
 // kSteps: 32-key steps of a round that are loaded: 4, or 2 for a split of at most 64 keys (eight chunks and eight
 // requests on 832 tokens 14.6 us a layer, so 14.3; eight causal chunks of 20 tokens 10.25 / 9.95; eight chunks on 2048
 // tokens 18.7 / 18.95).
+// kHides: some rows of the item may not see all its keys (new tokens of one request).
 // kOnce: non-temporal page loads (see kOnceBytes; 64 requests on eight prefixes of 2048 tokens 16.35 us a layer, so 15.4;
 // 256 on 32 44.1 / 41.1).
 //
@@ -361,7 +362,7 @@ struct __align__(16) WorkLds8 {
 // 13.5 when traced, 5.0 TB/s.
 // Not kept, for the same launches: a group's softmax beside another's products in program order, raised wave
 // priorities, four workgroups per CU (registers spill), rounds of 256 keys.
-template <int G, bool kOnce, int kSteps>
+template <int G, bool kOnce, int kSteps, bool kHides = true>
 __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
   constexpr int kLate8 = 5 * 8, kRound = 4;   // steps
   AttnArgs8 a = early_args;
@@ -590,6 +591,30 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     __builtin_amdgcn_sched_barrier(0);   // the next K chunks reuse kr[]
     if constexpr (!kLast) load_k(round + 1);
     __builtin_amdgcn_sched_barrier(0);
+    // Some rows do not see all keys: P is 0 there, and 0 times NaN is not.  Codes that are NaN become zeros, and the 64
+    // dims of the rows that do see one NaN.
+    if (kHides && min(wi.kv_end, wi.kv_begin + 32 * kRound * (round + 1)) - 1 > wi.q0) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        u32x4 nan[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) nan[t] = ((vr[s][t] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // bit 7 of a key's byte
+        const uint32_t first = nan[0][0] | nan[0][1] | nan[0][2] | nan[0][3], second = nan[1][0] | nan[1][1] | nan[1][2] | nan[1][3];
+        if (__any(first | second)) {
+          const uint32_t key = first ? 4 * g + (__builtin_ctz(first) >> 3) : second ? 16 + 4 * g + (__builtin_ctz(second) >> 3) : 63;
+          const int lowest = 63 - (int)rows4_largest(lanes16_largest(63 - key));
+          const int at = lowest + wi.kv_begin + 32 * (kRound * round + s);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) vr[s][t] &= ~((nan[t] >> 7) * 0xffu);
+#pragma unroll
+          for (int r = 0; r < G; ++r)
+            if (at < min(wi.kv_end, wi.q0 + 2 * r + sub + 1)) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) acc[r][c] *= __builtin_nanf("");
+            }
+        }
+      }
+    }
     __syncthreads();
     auto operands = [&](const int s, u32x4 (&v)[4]) {
 #pragma unroll
@@ -690,14 +715,17 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
   const int path_word = head[W_PATH];
   if ((path_word & kPathMask) == PATH_NOOP) return;
   const bool few_keys = wi.kv_end - wi.kv_begin <= 64;
-  if (path_word & kPathAppends)   // one or two tokens on their own pages
+  const bool hides = wi.kv_end - 1 > wi.q0;   // the item's first token does not see all keys
+  if (wi.n_tok > 4 && !hides)
+    few_keys ? attend8<4, false, 2, false>(a, wi, sm) : attend8<4, false, 4, false>(a, wi, sm);
+  else if (path_word & kPathAppends)   // one or two tokens on their own pages
     path_word & kPathOnce ? attend8<1, true, 4>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
-  else if (wi.n_tok > 4)
-    few_keys ? attend8<4, false, 2>(a, wi, sm) : attend8<4, false, 4>(a, wi, sm);
-  else if (wi.n_tok > 2)
+  else if (wi.n_tok <= 2)
+    few_keys ? attend8<1, false, 2>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
+  else if (wi.n_tok <= 4)
     few_keys ? attend8<2, false, 2>(a, wi, sm) : attend8<2, false, 4>(a, wi, sm);
   else
-    few_keys ? attend8<1, false, 2>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
+    attend8<4, false, 4>(a, wi, sm);
 }
 static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "attend8 reads the last argument there");
 

@@ -887,3 +887,42 @@ def test_kernels_carry_their_events(hist):
     assert torch.equal(*outs) and outs[0].any()
     B.oxy_batch_destroy(batch)
     gw.close()
+
+
+@pytest.mark.parametrize("n_new,hist,bad", [(2, 0, 1), (3, 0, 2), (8, 0, 4), (13, 5, 6), (5, 125, 3), (6, 253, 4), (13, 250, 1),
+                                            (50, 0, 20), (60, 700, 59), (4, 509, 2), (16, 1000, 1)])
+def test_a_value_that_is_not_finite_does_not_reach_tokens_before_it(n_new, hist, bad):
+    """Of several new tokens, some do not see the value of the token `bad`: their weight of it is zero, and zero times NaN
+    is not."""
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    dec = b.stream(b.prefix(70), DECODE)
+    b.tag = 10
+    if hist:
+        b.step([(dec, hist)], attend=False)
+    b.tag = 20
+    b.step([(dec, n_new)])
+    w = _workload("later", 31, 1, 128, b.trace)
+    src = synth.DataSource(w["seed"])
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "v" and recipe["tag"] == 20:
+            x[bad, 133], x[bad, 200] = 0x7fc0, 0xff80
+        return x
+
+    def without(recipe, layer, what, n):
+        x = planted(recipe, layer, what, n)
+        x = x if what == "q" else kv8.bf16_bits(kv8.cached_values(x))
+        return np.where((x & 0x7fff) > 0x7f80, np.uint16(0), x)
+
+    gw = GpuWorld(w, planted, poison=True, kv8=True)
+    ow = OracleWorld(w["num_blocks"], 1, without, w["scale"])
+    for op in w["trace"]:
+        g, o = gw.apply(op), ow.apply(op)
+    gw.close()
+    got, ref = g["O"][0], o["O"][0]
+    assert_o_close(got[:bad], ref[:bad], "before")
+    assert not np.isfinite(widen_bf16(got[bad:][:, :, [133, 200]])).any()
+    assert_o_close(got[:, :, :128], ref[:, :, :128], "other dims")
+    assert_lse_close(g["LSE"][0], o["LSE"][0], "all")
