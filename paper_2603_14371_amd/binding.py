@@ -180,7 +180,7 @@ def _not_bound(*args):
 
 
 class _Quick:
-    """Calls that a program makes in every layer, through libmarshal.so where it is there: the status, or None
+    """Calls that a program makes in every layer or step, through libmarshal.so where it is there: the status, or None
     where an argument needs ctypes' own conversion (or nothing is bound) and no call was made.  ctypes takes 1.1 us for
     an attention call's arguments and 1.8 for a rotating append's, this 0.3 and 0.4."""
     oxy_mixed_attention = staticmethod(_not_bound)
@@ -189,6 +189,12 @@ class _Quick:
     oxy_append_attention = staticmethod(_not_bound)
     oxy_rotary = staticmethod(_not_bound)
     oxy_rotary_append = staticmethod(_not_bound)
+    # the first two return what they are asked for (a batch's numbers 0.25 us, by ctypes 2.1; 164 slots as a list 1.2 / 7.2,
+    # 1338 12.3 / 19.0), the others take slots as a list (2 us less than by ctypes)
+    oxy_batch_info = staticmethod(_not_bound)
+    oxy_batch_slots = staticmethod(_not_bound)
+    oxy_gather_kv = staticmethod(_not_bound)
+    oxy_gather_kv_layers = staticmethod(_not_bound)
 
 
 _quick = _Quick()
@@ -400,14 +406,22 @@ def _i64(values):
 
 
 def oxy_gather_kv(pool, layer, slots, k_out_ptr, v_out_ptr, stream):
-    arr, ptr, n = _i64(slots)
-    _check(lib().oxy_gather_kv(pool, layer, ptr, n, k_out_ptr, v_out_ptr, stream or None))
+    status = _quick.oxy_gather_kv(pool, layer, slots, k_out_ptr, v_out_ptr, stream)
+    if status is None:
+        arr, ptr, n = _i64(slots)
+        status = lib().oxy_gather_kv(pool, layer, ptr, n, k_out_ptr, v_out_ptr, stream or None)
+    if status:
+        _check(status)
 
 
 def oxy_gather_kv_layers(pool, layer_begin, layer_end, slots, k_out_ptr, v_out_ptr, layer_stride, stream):
-    arr, ptr, n = _i64(slots)
-    _check(lib().oxy_gather_kv_layers(pool, layer_begin, layer_end, ptr, n, k_out_ptr, v_out_ptr, layer_stride,
-                                      stream or None))
+    status = _quick.oxy_gather_kv_layers(pool, layer_begin, layer_end, slots, k_out_ptr, v_out_ptr, layer_stride, stream)
+    if status is None:
+        arr, ptr, n = _i64(slots)
+        status = lib().oxy_gather_kv_layers(pool, layer_begin, layer_end, ptr, n, k_out_ptr, v_out_ptr, layer_stride,
+                                            stream or None)
+    if status:
+        _check(status)
 
 
 def make_rotary(freqs_ptr, rot_dims, layout=ROTARY_HALVES, amplitude=1.0):
@@ -505,6 +519,9 @@ def oxy_free_blocks(pool):
 
 def oxy_batch_info(batch):
     """-> (n_items, n_tokens, n_work, n_partials)"""
+    quick = _quick.oxy_batch_info(batch)
+    if quick is not None:
+        return quick
     a, b, c, d = _i32(), _i32(), _i32(), _i32()
     _check(lib().oxy_batch_info(batch, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c),
                                 ctypes.byref(d)))
@@ -513,6 +530,9 @@ def oxy_batch_info(batch):
 
 def oxy_batch_slots(batch):
     n = oxy_batch_info(batch)[1]
+    quick = _quick.oxy_batch_slots(batch, n)
+    if quick is not None:
+        return quick
     out = np.zeros(n, dtype=np.int64)
     _check(lib().oxy_batch_slots(batch, out.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), n))
     return out.tolist()

@@ -86,9 +86,91 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return call_with((Fn)PyLong_AsVoidPtr(self), args, n);
 }
 
-#define OXY_METHOD(name) {#name, (PyCFunction)(void (*)())call<decltype(&name)>, METH_FASTCALL, nullptr}
+// oxy_batch_info(batch): the four numbers as a tuple, or None where there is no such answer.
+PyObject* call_info(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  const oxy_batch* batch = nullptr;
+  int32_t v[4];
+  if (n != 1 || !convert(args[0], &batch) ||
+      ((decltype(&oxy_batch_info))PyLong_AsVoidPtr(self))(batch, v, v + 1, v + 2, v + 3) != OXY_OK)
+    Py_RETURN_NONE;
+  return Py_BuildValue("(iiii)", v[0], v[1], v[2], v[3]);
+}
+// oxy_batch_slots(batch, n): the slots as a list, or None.
+PyObject* call_slots(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
+  const oxy_batch* batch = nullptr;
+  int32_t n = 0;
+  if (n_args != 2 || !convert(args[0], &batch) || !convert(args[1], &n) || n < 1) Py_RETURN_NONE;
+  int64_t* out = (int64_t*)PyMem_Malloc((size_t)n * sizeof(int64_t));
+  if (!out) Py_RETURN_NONE;
+  PyObject* list = nullptr;
+  if (((decltype(&oxy_batch_slots))PyLong_AsVoidPtr(self))(batch, out, n) == OXY_OK && (list = PyList_New(n))) {
+    for (int32_t i = 0; i < n; ++i) {
+      PyObject* x = PyLong_FromLongLong(out[i]);
+      if (!x) {
+        Py_CLEAR(list);
+        break;
+      }
+      PyList_SET_ITEM(list, i, x);
+    }
+  }
+  PyMem_Free(out);
+  if (list) return list;
+  PyErr_Clear();
+  Py_RETURN_NONE;
+}
+// A list of slots for the length of one call.
+struct Slots {
+  int64_t* v = nullptr;
+  int32_t n = 0;
+  explicit Slots(PyObject* list) {
+    if (!PyList_CheckExact(list) || PyList_GET_SIZE(list) > INT32_MAX) return;
+    n = (int32_t)PyList_GET_SIZE(list);
+    v = (int64_t*)PyMem_Malloc((size_t)n * sizeof(int64_t));
+    if (v && !oxy_ints_of_list(list, v, n)) release();
+  }
+  ~Slots() { release(); }
+  void release() {
+    PyMem_Free(v);
+    v = nullptr;
+  }
+};
+// Read-backs take their slots as a list of ints.
+PyObject* call_gather(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  oxy_pool* pool;
+  int32_t layer, status;
+  void *k, *v, *stream;
+  if (n != 6 || !convert(args[0], &pool) || !convert(args[1], &layer) || !convert(args[3], &k) || !convert(args[4], &v) ||
+      !convert(args[5], &stream))
+    Py_RETURN_NONE;
+  const Slots slots(args[2]);
+  if (!slots.v) Py_RETURN_NONE;
+  Py_BEGIN_ALLOW_THREADS
+  status = ((decltype(&oxy_gather_kv))PyLong_AsVoidPtr(self))(pool, layer, slots.v, slots.n, k, v, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+PyObject* call_gather_layers(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  oxy_pool* pool;
+  int32_t begin, end, status;
+  void *k, *v, *stream;
+  size_t stride;
+  if (n != 8 || !convert(args[0], &pool) || !convert(args[1], &begin) || !convert(args[2], &end) || !convert(args[4], &k) ||
+      !convert(args[5], &v) || !convert(args[6], &stride) || !convert(args[7], &stream))
+    Py_RETURN_NONE;
+  const Slots slots(args[3]);
+  if (!slots.v) Py_RETURN_NONE;
+  Py_BEGIN_ALLOW_THREADS
+  status = ((decltype(&oxy_gather_kv_layers))PyLong_AsVoidPtr(self))(pool, begin, end, slots.v, slots.n, k, v, stride, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+#define OXY_CALL(name, function) {#name, (PyCFunction)(void (*)())function, METH_FASTCALL, nullptr}
+#define OXY_METHOD(name) OXY_CALL(name, call<decltype(&name)>)
 PyMethodDef g_calls[] = {OXY_METHOD(oxy_mixed_attention), OXY_METHOD(oxy_mixed_attention_static), OXY_METHOD(oxy_stream_append),
                          OXY_METHOD(oxy_append_attention), OXY_METHOD(oxy_rotary_append), OXY_METHOD(oxy_rotary),
+                         OXY_CALL(oxy_batch_info, call_info), OXY_CALL(oxy_batch_slots, call_slots),
+                         OXY_CALL(oxy_gather_kv, call_gather), OXY_CALL(oxy_gather_kv_layers, call_gather_layers),
                          {nullptr, nullptr, 0, nullptr}};
 
 // bound(name, address): the call of that name, or None
