@@ -40,6 +40,8 @@
  *    oxy_batch_build at once, without waiting for the device: drive all batches of
  *    a pool on ONE HIP stream (then stream order protects the slot), or order the
  *    next build's stream behind the destroyed batch's last launch yourself.
+ *  - A call works on the calling thread's current device: the pool's buffers, the stream
+ *    and every DEVICE pointer belong to it (one process per GPU; no call sets a device).
  *  - Ids are sequential from 0 and never reused (App. A.2: the id of a request
  *    is the number of requests created before it); prefixes and streams count
  *    separately.
