@@ -439,7 +439,8 @@ def oxy_rotary_freqs(base, rot_dims, kind=ROTARY_PLAIN, factor=1.0, low=0.0, hig
 
 
 def oxy_rotary(rotary, positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream):
-    status = _quick.oxy_rotary(ctypes.addressof(rotary), positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream)
+    status = _quick.oxy_rotary(ctypes.addressof(rotary), positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens,
+                               n_heads, stream)
     if status is None:
         status = lib().oxy_rotary(ctypes.byref(rotary), positions_ptr or None, x_ptr or None, x_stride,
                                   out_ptr or None, out_stride, n_tokens, n_heads, stream or None)

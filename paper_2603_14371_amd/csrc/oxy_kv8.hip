@@ -357,8 +357,8 @@ struct __align__(16) WorkLds8 {
 // What bounds it.  Small launches: the chain record - pages - logits - P - sums, 2.7 us, and the two launches themselves
 // (one chunk and one request 6.85 us a layer, one request 5.7).  Chunks: eight of 50 on 2048 tokens take 18.9 us with
 // the merge, of which the first loads of 512 workgroups are 2.4 us and a SIMD issues vector instructions for 5.4 us
-// (128 conversions and 300 others a round) and matrix ones for 3.6 (128 a round of eight tokens), which overlap little; no phase taken
-// out alone saves more than 1 us.  Bytes where histories are long: 131072 tokens 15.6 us with the merge, the items alone
+// (128 conversions and 300 others a round) and matrix ones for 3.6 (128 a round of eight tokens), which overlap little;
+// no phase taken out alone saves more than 1 us.  Bytes where histories are long: 131072 tokens 15.6 us with the merge, the items alone
 // 13.5 when traced, 5.0 TB/s.
 // Not kept, for the same launches: a group's softmax beside another's products in program order, raised wave
 // priorities, four workgroups per CU (registers spill), rounds of 256 keys.
@@ -599,9 +599,12 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
         u32x4 nan[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) nan[t] = ((vr[s][t] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // bit 7 of a key's byte
-        const uint32_t first = nan[0][0] | nan[0][1] | nan[0][2] | nan[0][3], second = nan[1][0] | nan[1][1] | nan[1][2] | nan[1][3];
+        const uint32_t first = nan[0][0] | nan[0][1] | nan[0][2] | nan[0][3];
+        const uint32_t second = nan[1][0] | nan[1][1] | nan[1][2] | nan[1][3];
         if (__any(first | second)) {
-          const uint32_t key = first ? 4 * g + (__builtin_ctz(first) >> 3) : second ? 16 + 4 * g + (__builtin_ctz(second) >> 3) : 63;
+          const uint32_t key = first    ? 4 * g + (__builtin_ctz(first) >> 3)
+                               : second ? 16 + 4 * g + (__builtin_ctz(second) >> 3)
+                                        : 63;
           const int lowest = 63 - (int)rows4_largest(lanes16_largest(63 - key));
           const int at = lowest + wi.kv_begin + 32 * (kRound * round + s);
 #pragma unroll
@@ -904,7 +907,8 @@ hipError_t launch_merge8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hi
     hipExtLaunchKernelGGL(merge_long_kernel, dim3(4 * kHeads * a.n_q), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc,
                           a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
   else
-    merge_long_kernel<<<4 * kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
+    merge_long_kernel<<<4 * kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts,
+                                                                     a.part_off);
   return hipGetLastError();
 }
 

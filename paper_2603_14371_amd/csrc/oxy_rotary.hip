@@ -146,7 +146,8 @@ template <int kForm, int kTokens>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const char* x, const size_t x_stride, char* out,
                                                      const size_t out_stride, const int32_t n_tokens,
                                                      const int32_t n_heads) {
-  constexpr int kStep = 8 / kTokens, kRows = kForm == FORM_HALVES_ANY ? 1 : kTokens == 1 ? 2 : 3;   // half wavefronts of a token; rows at a time
+  constexpr int kStep = 8 / kTokens;   // half wavefronts of a token
+  constexpr int kRows = kForm == FORM_HALVES_ANY ? 1 : kTokens == 1 ? 2 : 3;   // of each at a time
   __shared__ __align__(16) float cs[kTokens][kMaxPairs], sn[kTokens][kMaxPairs];
   const int tok0 = blockIdx.x * kTokens, here = min(kTokens, n_tokens - tok0);
   const int t = threadIdx.x, c = t & 31, half = r.rot_dims >> 1;
