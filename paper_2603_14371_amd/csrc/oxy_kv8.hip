@@ -295,14 +295,14 @@ __device__ __forceinline__ u32x4 f16_operand(const uint32_t lo, const uint32_t h
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
   return r;
 }
-// Largest of a lane's eight dot products, in four instructions (fmaxf makes every matrix result canonical first: eleven).
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+// Largest of a lane's eight dot products, NaN if one is: four instructions (fmaxf, which passes over a NaN, makes every
+// matrix result canonical first: eleven).  No inline assembly: the compiler does not place the wait states between a
+// matrix instruction and a reader of its result for what stands in such text.
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 __device__ __forceinline__ float largest8(const f32x4 s0, const f32x4 s1) {
-  return max3(max3(max3(s0[0], s0[1], s0[2]), s0[3], s1[0]), max3(s1[1], s1[2], s1[3]), -__builtin_inff());
+  return __builtin_elementwise_maximum(largest3(largest3(largest3(s0[0], s0[1], s0[2]), s0[3], s1[0]), s1[1], s1[2]), s1[3]);
 }
 // first `left` of four bytes
 __device__ __forceinline__ uint32_t byte_mask(const int left) {
