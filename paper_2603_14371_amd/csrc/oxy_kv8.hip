@@ -32,9 +32,11 @@ namespace oxy {
 // One wavefront per token: the first half takes the key, the second the value.  Bound by the chain slot - row - largest
 // element - codes, and for many tokens by the byte stores of V.
 constexpr int kAppendTokens8 = 4;   // wavefronts, and tokens, of a workgroup
-// From here on 16 tokens a workgroup (append_many8_kernel).  One token a wavefront / 16 a workgroup: 58 tokens 2.9 / 4.1 us,
-// 1338 of four requests 3.8 / 3.85, 2048 of 512 4.3 / 4.8, 4096 of one 6.3 / 4.15, 16384 17.5 / 8.5, 131072 107 / 41.6
-// (4.8 TB/s; 48.8 where they start inside a chunk).
+// From here on 16 tokens a workgroup (append_many8_kernel): where the two are equal for tokens of 2100 requests, whose slots do
+// not follow each other; histories gain from about 1300 on.  us a launch, one token a wavefront / 16 a workgroup (the same
+// slots again and again, so mostly in caches): 58 tokens 2.4 / 2.85, 1336 of four requests 3.35 / 3.35, 1536 of 1536 3.75 / 4.4,
+// 2048 of one 3.65 / 3.05, 2100 of 2100 4.8 / 4.65, 4096 of one 5.3 / 3.3, 16384 15.4 / 5.6, 131072 94.7 / 31.3 (6.4 TB/s; 36.6
+// where they start inside a chunk).
 constexpr int kManyAppend8 = 2049;
 __global__ __launch_bounds__(64 * kAppendTokens8) void append8_kernel(const uint16_t* __restrict__ k_new,
                                                                       const uint16_t* __restrict__ v_new,
@@ -134,7 +136,8 @@ __global__ __launch_bounds__(256) void append_many8_kernel(const uint16_t* __res
     *(u32x2*)(&sm.v[j][8 * c]) = (u32x2){rv.codes[0], rv.codes[1]};
   }
   // bit j: token j + 1 has the next slot; token j starts a chunk whose other three follow it
-  const uint32_t next = (uint32_t)__ballot(j16 + 1 < n && __shfl(slot, (j16 + 1) & 15) == slot + 1) & 0xffffu;
+  const int after = __shfl(slot, (j16 + 1) & 15);   // by all lanes: one that is switched off gives nothing
+  const uint32_t next = (uint32_t)__ballot(j16 + 1 < n && after == slot + 1) & 0xffffu;
   const uint32_t starts = (uint32_t)__ballot((slot & 3) == 0) & next & (next >> 1) & (next >> 2);
   uint32_t rest = ((1u << n) - 1u) & ~(starts | starts << 1 | starts << 2 | starts << 3);
   __syncthreads();

@@ -37,3 +37,19 @@ def test_inline_assembly_only_stores(path):
 def test_the_reader_of_inline_assembly_reads():
     code = 'asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r));\nasm volatile("" : "+v"(x));\nasm volatile("a %0\\n\\t"\n "s_nop 1" ::"v"(d));'
     assert asm_texts(code) == ["v_max3_f32 %0, %1, %2, %3", "", "a %0\n s_nop 1"]
+
+
+def conditional_exchanges(code):
+    """Statements in which a lane exchange is computed only where something else is true: to the right of &&, || or ?."""
+    return [s.strip() for s in re.split(r"[;{}]", code) if re.search(r"(&&|\|\||\?).*(__shfl\w*|ds_bpermute)\s*\(", s, re.S)]
+
+
+@pytest.mark.parametrize("path", FILES, ids=os.path.basename)
+def test_lanes_that_are_read_from_take_part(path):
+    """A lane that is switched off gives nothing to one that reads from it."""
+    assert not conditional_exchanges(code_of(path))
+
+
+def test_the_reader_of_exchanges_reads():
+    assert conditional_exchanges("x = __ballot(i + 1 < n &&\n __shfl(s, i + 1) == s + 1) & 0xffu;\ny = a ? __shfl(b, c) : 0;")
+    assert not conditional_exchanges("const int y = __shfl(s, i + 1);\nx = __ballot(i + 1 < n && y == s + 1); if (a && b) { c = __shfl(d, e); }")
