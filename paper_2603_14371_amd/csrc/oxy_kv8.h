@@ -24,6 +24,9 @@ inline size_t layer_bytes8(int32_t num_blocks) {
   return ((size_t)num_blocks * (kBlockBytes8 + kScaleBytes8) + 255) / 256 * 256;
 }
 
+// Tokens from which on an append is made 16 a workgroup, by a kernel of its own: a recording of one is none of the other.
+constexpr int kManyAppend8 = 2049;
+constexpr bool many_append8(int32_t n_tokens) { return n_tokens >= kManyAppend8; }
 // As launch_append and launch_gather_inline, the latter for n_layers layers that lie pool_layer_stride bytes apart
 // (outputs out_layer_stride).
 OXY_WEAK hipError_t launch_append8(const void* k_new, const void* v_new, const int32_t* d_slots, int32_t n_tokens,

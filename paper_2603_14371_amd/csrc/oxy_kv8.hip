@@ -32,12 +32,11 @@ namespace oxy {
 // One wavefront per token: the first half takes the key, the second the value.  Bound by the chain slot - row - largest
 // element - codes, and for many tokens by the byte stores of V.
 constexpr int kAppendTokens8 = 4;   // wavefronts, and tokens, of a workgroup
-// From here on 16 tokens a workgroup (append_many8_kernel): where the two are equal for tokens of 2100 requests, whose slots do
-// not follow each other; histories gain from about 1300 on.  us a launch, one token a wavefront / 16 a workgroup (the same
-// slots again and again, so mostly in caches): 58 tokens 2.4 / 2.85, 1336 of four requests 3.35 / 3.35, 1536 of 1536 3.75 / 4.4,
-// 2048 of one 3.65 / 3.05, 2100 of 2100 4.8 / 4.65, 4096 of one 5.3 / 3.3, 16384 15.4 / 5.6, 131072 94.7 / 31.3 (6.4 TB/s; 36.6
-// where they start inside a chunk).
-constexpr int kManyAppend8 = 2049;
+// From kManyAppend8 tokens on 16 a workgroup (append_many8_kernel): where the two are equal for tokens of as many requests,
+// whose slots do not follow each other; histories gain from about 1300 on.  us a launch, one token a wavefront / 16 a
+// workgroup (the same slots again and again, so mostly in caches): 58 tokens 2.4 / 2.85, 1336 of four requests 3.35 / 3.35,
+// 1536 of 1536 3.75 / 4.4, 2048 of one 3.65 / 3.05, 2100 of 2100 4.8 / 4.65, 4096 of one 5.3 / 3.3, 16384 15.4 / 5.6, 131072
+// 94.7 / 31.3 (6.4 TB/s; 36.6 where they start inside a chunk).
 __global__ __launch_bounds__(64 * kAppendTokens8) void append8_kernel(const uint16_t* __restrict__ k_new,
                                                                       const uint16_t* __restrict__ v_new,
                                                                       const int32_t* __restrict__ slots,
@@ -831,7 +830,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint1
 hipError_t launch_append8(const void* k_new, const void* v_new, const int32_t* d_slots, int32_t n_tokens, Layer8 layer,
                           hipStream_t s) {
   if (n_tokens <= 0) return hipSuccess;
-  if (n_tokens >= kManyAppend8)
+  if (many_append8(n_tokens))
     append_many8_kernel<<<(n_tokens + 15) / 16, 256, 0, s>>>((const uint16_t*)k_new, (const uint16_t*)v_new, d_slots,
                                                              layer.blocks, layer.scales, n_tokens);
   else

@@ -68,7 +68,7 @@ struct StepKey {
   float scale = 0.f;
   int32_t layer_begin = 0, layer_end = 0, mode = 0;   // mode: 0 separate, 1 fused, 2 folded
   int32_t n_work = 0, n_tokens = 0, n_fresh = 0, off_work = 0, off_tables = 0, off_part_off = 0,
-          off_n_parts = 0, write_through = 0, long_merge = 0;
+          off_n_parts = 0, write_through = 0, long_merge = 0, many_append = 0;
   bool operator==(const StepKey& o) const {
     return d_base == o.d_base && k_new == o.k_new && v_new == o.v_new && q == o.q &&
            out == o.out && lse == o.lse && kv_stride == o.kv_stride && q_stride == o.q_stride &&
@@ -83,7 +83,7 @@ struct StepKey {
   bool same_topology(const StepKey& o) const {
     return layer_end - layer_begin == o.layer_end - o.layer_begin && mode == o.mode &&
            oxy::merge_heads(n_tokens) == oxy::merge_heads(o.n_tokens) && (n_fresh > 0) == (o.n_fresh > 0) &&
-           long_merge == o.long_merge;
+           long_merge == o.long_merge && many_append == o.many_append;
   }
 };
 struct StepGraph {
@@ -1372,6 +1372,7 @@ int32_t replay_step(const StepCall& c, hipStream_t s) {
   key.off_n_parts = b->off_n_parts;
   key.write_through = writes_through(b);
   key.long_merge = p->kv8 && b->max_parts > oxy::kLongParts;
+  key.many_append = p->kv8 && oxy::many_append8(b->n_tokens);
   const uint64_t now = ++p->graph_clock;
   StepGraph* hit = nullptr;
   for (StepGraph& g : p->graphs)
