@@ -73,13 +73,13 @@
  *   value_i = code_i * 2^e            (a bf16 number; infinite where |x_i| >= 1.9375 * 2^127 makes it 2^128)
  * Every call takes and returns bf16 as with a bf16 pool; the attention is that of the values, and
  * oxy_gather_kv returns them.  What a row holds depends on that row alone, not on how a history was
- * cut into calls, what else is in its page or what was there before.  Probabilities meet the values in
- * fp16: a value counts to 2^-11 of itself, and to 2^-32 of the largest value among the same few hundred
- * keys.  A key that is not finite makes the outputs of the queries that see it NaN; a value that is not
- * finite the dim, or its 64 dims, of those queries; other queries are as without it.
- * About half the memory
- * (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded up to 256): first
- * the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.
+ * cut into calls, what else is in its page or what was there before.  What a key adds to a query (its
+ * probability times its value) passes through fp16: it counts to 2^-11 of itself, or to 2^-20 of the largest
+ * that any one of the same few hundred keys adds to that query.  A key that is not finite makes the outputs of
+ * the queries that see it NaN; a value that is not finite the dim, or its 64 dims, of those queries; other
+ * queries are as without it.
+ * About half the memory (8224 bytes per block and layer).  Layer l starts at l * (num_blocks * 8224 rounded
+ * up to 256): first the blocks, 8 KiB each (K page 4 KiB, V page 4 KiB), then 32 exponent bytes per block.
  *   K page: 16-byte chunk (jj, g, key), jj<4, g<4, key<16, at ((jj*4+g)*16+key)*16 holds the codes of
  *           K[key][64jj+16g .. +15].
  *   V page: chunk (w, g, n), w<4, g<4, n<16, at ((w*4+g)*16+n)*16 holds those of V[4g..4g+3][d], then of

@@ -269,7 +269,6 @@ __global__ __launch_bounds__(256) void gather_table8_kernel(const char* blocks, 
 // attention work items
 // ------------------------------------------------------------------------------------------
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 // largest of lanes n, n+16, n+32, n+48
 __device__ __forceinline__ uint32_t rows4_largest(uint32_t x) {
   x = swap16_max(x);
@@ -310,6 +309,27 @@ __device__ __forceinline__ float largest8(const f32x4 s0, const f32x4 s1) {
 __device__ __forceinline__ uint32_t byte_mask(const int left) {
   return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 }
+constexpr int kSpread = 12;   // see `attend8`
+// Exponent bytes of a set of values as one word, the largest in the low half, 255 less the smallest in the high half: 0 is
+// the empty set, and the larger half of each is the union.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t span_union(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ uint32_t span_of8(const int (&b)[8]) {
+  int top = b[0], low = b[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) top = max(top, b[e]), low = min(low, b[e]);
+  return (uint32_t)top | (uint32_t)(255 - low) << 16;
+}
+__device__ __forceinline__ uint32_t rows4_span(uint32_t s) {   // of lanes n, n+16, n+32, n+48
+  const auto a = __builtin_amdgcn_permlane16_swap(s, s, false, false);
+  s = span_union(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(s, s, false, false);
+  return span_union(b[0], b[1]);
+}
+__device__ __forceinline__ int span_top(uint32_t s) { return (int)(s & 0xffffu); }
+__device__ __forceinline__ int span_low(uint32_t s) { return 255 - (int)(s >> 16); }
 // P = 2^(sl2 * s - m) of a lane's eight dot products; what meets the value codes is P times its key's factor, as fp16.
 // Returns the sum of P itself.
 __device__ __forceinline__ float weights8(const f32x4 s0, const f32x4 s1, const float sl2, const float m,
@@ -325,13 +345,29 @@ __device__ __forceinline__ float weights8(const f32x4 s0, const f32x4 s1, const 
   return sum;
 }
 
+// The same with a unit of the row's own: P times 2^(its key's exponent byte - unit + 7).
+__device__ __forceinline__ float weights8_by_row(const f32x4 s0, const f32x4 s1, const float sl2, const float m,
+                                                 const int (&vb)[8], const int unit, u32x4& w) {
+  float p[8], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = fast_exp2(__builtin_fmaf(e < 4 ? s0[e & 3] : s1[e & 3], sl2, -m));
+    sum += p[e];
+    p[e] = __builtin_amdgcn_ldexpf(p[e], vb[e] + 7 - unit);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_f16(p[2 * i], p[2 * i + 1]);
+  return sum;
+}
+
 // LDS of a work item: nothing of K and V, only what the four wavefronts exchange.
 struct __align__(16) WorkLds8 {
   u32x4 q[kMaxGroups][8][64];      // query fragments, the same for all wavefronts
   u32x4 p[4 * kMaxGroups][64];     // [32-key step][group]: P of a round's keys
   float mx[kMaxGroups][16][4];     // largest logit of a row among each wavefront's keys
+  float share[kMaxGroups][16][4];  // largest log2 of a weight times its value's power of two, where units go by the row
   int slot[2 * kMaxGroups];        // split result of each token
-  int top[4];                      // largest exponent byte of each wavefront's values
+  uint32_t span[4];                // exponent bytes of each wavefront's values: see span_of8
   float ls[kMaxGroups][64][4];     // sum of a lane's P over each wavefront's keys
 };
 
@@ -343,16 +379,24 @@ struct __align__(16) WorkLds8 {
 //
 // P travels as ONE fp16 number (hi + lo bf16 in a bf16 cache: twice the products, the LDS traffic and the packing).
 // A single bf16 would be too coarse (2^-8 of it at most, for queries that see few keys); fp16 has 2^-11, like the split
-// results behind it, and e4m3 codes are fp16 numbers.  Its range: with `vref` the largest exponent of the values seen so
-// far, P (at most 2^8) times 2^(exponent - vref + 7) is at most 2^15; what contributes 2^-21 of the largest value or more
-// keeps 11 bits, below that the error is 2^-32 of the largest value.  acc is in units of 2^(vref - 7) and rescaled
-// when vref grows, which a power of two does exactly.
+// results behind it, and e4m3 codes are fp16 numbers.  Its range is short, so the number is P times
+// 2^(exponent - unit + 7), acc is in units of 2^(unit - 7), and the unit decides what is left of small ones:
+//  - All tokens of the item see all its keys, and their exponents lie within kSpread of each other: the largest exponent so
+//    far, the same for all rows.  P is at most 2^8 and at least 1 for some key of a row, so what meets the codes is at most
+//    2^15, and at least 2^(7 - kSpread) for the key that adds the most: half a step of the smallest fp16 numbers is 2^-20
+//    of that.  acc is rescaled when the unit grows, which a power of two does exactly.
+//  - kByRow, otherwise: the row's own, by the largest P times 2^exponent among the keys that it sees.  A token's values then
+//    leave no trace in the tokens before it, and a large value that has no weight none in the others.  An item finds out
+//    after its first products and starts again: 10 to 33 % slower (one chunk and one request 7.0 us a layer / 8.0, eight
+//    chunks on 2048 tokens 19.8 / 23.2, 64 requests and two chunks 15.2 / 20.2, 131072 tokens 15.9 / 17.4).  As a branch
+//    of the other form it took the registers of all instances (256, 61 of them spilled: 7.5, 23.2, 18.9 and 16.4 without
+//    ever being taken).
 //
-// A row's arithmetic does not depend on G or on the other rows.
+// A row's arithmetic depends on the split's keys and on whether all tokens of the item see them, not on G or on what the
+// other rows hold.  Returns whether the item is done: false, by all wavefronts, where it has to be done by rows.
 // kSteps: 32-key steps of a round that are loaded: 4, or 2 for a split of at most 64 keys (eight chunks and eight
 // requests on 832 tokens 14.6 us a layer, so 14.3; eight causal chunks of 20 tokens 10.25 / 9.95; eight chunks on 2048
 // tokens 18.7 / 18.95).
-// kHides: some rows of the item may not see all its keys (new tokens of one request).
 // kOnce: non-temporal page loads (see kOnceBytes; 64 requests on eight prefixes of 2048 tokens 16.35 us a layer, so 15.4;
 // 256 on 32 44.1 / 41.1).
 //
@@ -364,8 +408,8 @@ struct __align__(16) WorkLds8 {
 // 13.5 when traced, 5.0 TB/s.
 // Not kept, for the same launches: a group's softmax beside another's products in program order, raised wave
 // priorities, four workgroups per CU (registers spill), rounds of 256 keys.
-template <int G, bool kOnce, int kSteps, bool kHides = true>
-__device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
+template <int G, bool kOnce, int kSteps, bool kByRow>
+__device__ __forceinline__ bool attend8(const AttnArgs8& early_args, const WorkItem& wi, WorkLds8& sm) {
   constexpr int kLate8 = 5 * 8, kRound = 4;   // steps
   AttnArgs8 a = early_args;
   int tid = threadIdx.x;
@@ -471,9 +515,11 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
 
   float m[G], l[G];   // reference max (scaled log2 domain) of this lane's row, and the sum of P
   f32x4 acc[G][4];    // over this wavefront's keys; acc[r][c][e] = dim 64w + 16g + 4e + c
-  int vref = 1;       // exponent byte that acc's unit goes by
+  uint32_t span = 1;   // exponent bytes seen
+  int unit[G];         // acc's unit, as an exponent byte: that of the largest value seen, or the row's own
 #pragma unroll
   for (int r = 0; r < G; ++r) {
+    unit[r] = 1;
     m[r] = ninf;
     l[r] = 0.f;
 #pragma unroll
@@ -486,10 +532,10 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
     asm volatile("" : "+v"(lane_now));
     const int lane = lane_now, n = lane & 15, g = lane >> 4, sub = n >> 3;
     f32x4 s0[G], s1[G];
-    int vb[8];   // exponent bytes of this lane's values, 0 for keys that are not there
+    int vb[8];   // exponent bytes of this lane's values; of keys that are not there, those of others
     const int pos = wi.kv_begin + 32 * (kRound * round + wv);
     const int left = wi.kv_end - pos;
-    const bool need_mask = (kLast && left < 32) || pos + 31 > wi.q0;
+    const bool need_mask = (kLast && left < 32) || (kByRow && pos + 31 > wi.q0);
     if (kSteps != 2 || wv < 2) {
 #pragma unroll
       for (int r = 0; r < G; ++r) s0[r] = s1[r] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -513,7 +559,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
         asm volatile("" : "+v"(k0));   // a branch: as selects the masks are a quarter of a round's instructions
 #pragma unroll
         for (int r = 0; r < G; ++r) {
-          const int end = min(wi.kv_end, wi.q0 + 2 * r + sub + 1) - k0;
+          const int end = (kByRow ? min(wi.kv_end, wi.q0 + 2 * r + sub + 1) : wi.kv_end) - k0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             s0[r][e] = e < end ? s0[r][e] : ninf;
@@ -521,8 +567,9 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
           }
         }
         // the exponent byte of a slot that was never written may be anything
+        const int there = left > 0 ? __builtin_amdgcn_readfirstlane(vb[0]) : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vb[e] = (e < 4 ? e : 12 + e) < wi.kv_end - k0 ? vb[e] : 0;
+        for (int e = 0; e < 8; ++e) vb[e] = (e < 4 ? e : 12 + e) < wi.kv_end - k0 ? vb[e] : there;
       }
     } else {
 #pragma unroll
@@ -538,11 +585,23 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       }
       const float mine = row_max4_each(mx);
       if (g < G) sm.mx[g][n][wv] = mine;
-      int top = 1;
+      if constexpr (kByRow) {   // log2 of the largest share that a key has in its row's sums, up to its codes
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, vb[e]);
-      top = (int)rows4_largest((uint32_t)top);   // the same in all lanes of 16
-      if (lane == 0) sm.top[wv] = top;
+        for (int r = 0; r < G; ++r) {
+          f32x4 c0, c1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            c0[e] = __builtin_fmaf(s0[r][e], sl2, (float)vb[e]);
+            c1[e] = __builtin_fmaf(s1[r][e], sl2, (float)vb[4 + e]);
+          }
+          mx[r] = largest8(c0, c1);
+        }
+        const float share = row_max4_each(mx);
+        if (g < G) sm.share[g][n][wv] = share;
+      } else {
+        const uint32_t sp = left > 0 ? rows4_span(span_of8(vb)) : 0;   // the same in all lanes of 16
+        if (lane == 0) sm.span[wv] = sp;
+      }
     }
     __syncthreads();
     // online softmax with a reference that only moves by more than kGrow: see `attend`
@@ -554,48 +613,75 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       mx[r] = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3]));
       grow |= mx[r] > m[r] + kGrow;
     }
-    const i32x4 tops = *(const i32x4*)sm.top;
-    const int top = __builtin_amdgcn_readfirstlane(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
-    if (top > vref) {   // wave-uniform; acc holds zeros in the first round
-      if (round > 0) {
-        const float down = __builtin_amdgcn_ldexpf(1.f, vref - top);
+    if constexpr (kByRow) {
+#pragma unroll
+      for (int r = 0; r < G; ++r) {
+        const f32x4 cw = *(const f32x4*)sm.share[r][n];
+        const float share = fmaxf(fmaxf(cw[0], cw[1]), fmaxf(cw[2], cw[3]));
+        const bool up = mx[r] > m[r] + kGrow;
+        const float to = up ? mx[r] : m[r];
+        const float alpha = up ? fast_exp2(m[r] - to) : 1.f;
+        // the unit that the sums have by the new reference, or that of a larger share
+        const float want = fmaxf(share - to, up ? (float)unit[r] + (m[r] - to) : (float)unit[r]);
+        const int fits = (int)ceilf(fminf(fmaxf(want, 1.f), 254.f));
+        l[r] = rescaled(l[r], alpha);
+        if (round > 0) {
+          const float down = __builtin_amdgcn_ldexpf(alpha, unit[r] - fits);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[r][c] *= down;
+        }
+        m[r] = to;
+        unit[r] = fits;
+      }
+    } else {
+      const u32x4 spans = *(const u32x4*)sm.span;
+      const uint32_t seen = __builtin_amdgcn_readfirstlane(
+          span_union(span, span_union(span_union(spans[0], spans[1]), span_union(spans[2], spans[3]))));
+      const int top = span_top(seen);
+      if (top - span_low(seen) > kSpread) return false;   // all four wavefronts
+      if (top > span_top(span) && round > 0) {   // wave-uniform; acc holds zeros in the first round
+        const float down = __builtin_amdgcn_ldexpf(1.f, span_top(span) - top);
 #pragma unroll
         for (int r = 0; r < G; ++r)
 #pragma unroll
           for (int c = 0; c < 4; ++c) acc[r][c] *= down;
       }
-      vref = top;
-    }
-    if (__any(grow)) {
+      span = seen;
+      if (__any(grow)) {
 #pragma unroll
-      for (int r = 0; r < G; ++r) {
-        const bool up = mx[r] > m[r] + kGrow;
-        const float alpha = up ? fast_exp2(m[r] - mx[r]) : 1.f;
-        l[r] = rescaled(l[r], alpha);
-        if (round > 0) {
+        for (int r = 0; r < G; ++r) {
+          const bool up = mx[r] > m[r] + kGrow;
+          const float alpha = up ? fast_exp2(m[r] - mx[r]) : 1.f;
+          l[r] = rescaled(l[r], alpha);
+          if (round > 0) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) acc[r][c] *= alpha;
+            for (int c = 0; c < 4; ++c) acc[r][c] *= alpha;
+          }
+          m[r] = up ? mx[r] : m[r];
         }
-        m[r] = up ? mx[r] : m[r];
       }
     }
-    // 2^(exponent - vref + 7); for a key that is not there (P is 0) something finite
+    // 2^(exponent - unit + 7); for a key that is not there (P is 0) something finite
     float factor[8];
+    if constexpr (!kByRow) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) factor[e] = __uint_as_float((uint32_t)max((vb[e] << 23) + ((127 + 7 - vref) << 23), 0));
+      for (int e = 0; e < 8; ++e)
+        factor[e] = __uint_as_float((uint32_t)max((vb[e] << 23) + ((127 + 7 - span_top(span)) << 23), 0));
+    }
 #pragma unroll
     for (int r = 0; r < G; ++r) {
       u32x4 w;
-      l[r] += weights8(s0[r], s1[r], sl2, (m[r] == ninf) ? 0.f : m[r], factor, w);
+      const float ref = (m[r] == ninf) ? 0.f : m[r];
+      l[r] += kByRow ? weights8_by_row(s0[r], s1[r], sl2, ref, vb, unit[r], w) : weights8(s0[r], s1[r], sl2, ref, factor, w);
       sm.p[wv * G + r][lane] = w;
       if constexpr (kLast) sm.ls[r][lane][wv] = l[r];
     }
     __builtin_amdgcn_sched_barrier(0);   // the next K chunks reuse kr[]
     if constexpr (!kLast) load_k(round + 1);
     __builtin_amdgcn_sched_barrier(0);
-    // Some rows do not see all keys: P is 0 there, and 0 times NaN is not.  Codes that are NaN become zeros, and the 64
+    // Some rows may not see all keys: P is 0 there, and 0 times NaN is not.  Codes that are NaN become zeros, and the 64
     // dims of the rows that do see one NaN.
-    if (kHides && min(wi.kv_end, wi.kv_begin + 32 * kRound * (round + 1)) - 1 > wi.q0) {
+    if (kByRow && min(wi.kv_end, wi.kv_begin + 32 * kRound * (round + 1)) - 1 > wi.q0) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         u32x4 nan[2];
@@ -653,7 +739,7 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
       };
       auto finish_group = [&](const int r) {
         const int slot = sm.slot[2 * r + sub];
-        store_part<(G >= 4), true>(a, wi, slot, acc[r], r, wv, lane, vref - 127 - 7);
+        store_part<(G >= 4), true>(a, wi, slot, acc[r], r, wv, lane, (kByRow ? unit[r] : span_top(span)) - 127 - 7);
         if (wv == r) {   // wave-uniform: the sums of the groups are shared out
           const f32x4 lw = *(const f32x4*)sm.ls[r][lane];
           const float total = row_sum4((lw[0] + lw[1]) + (lw[2] + lw[3]));
@@ -689,10 +775,12 @@ __device__ __forceinline__ void attend8(const AttnArgs8& early_args, const WorkI
         }
       }
     }
+    return true;
   };
   if constexpr (kSteps != 2)
-    for (int round = 0; round + 1 < rounds; ++round) round_body(round, std::false_type());
-  round_body(kSteps != 2 ? rounds - 1 : 0, std::true_type());
+    for (int round = 0; round + 1 < rounds; ++round)
+      if (!round_body(round, std::false_type())) return false;
+  return round_body(kSteps != 2 ? rounds - 1 : 0, std::true_type());
 }
 
 __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_kernel(
@@ -706,31 +794,43 @@ __global__ __attribute__((aligned(4096))) __launch_bounds__(256, 2) void attn8_k
   a.part_off = work + part_off;
   a.scale = scale;
   WorkItem wi;
-  wi.rec = (DescPtr)work + (size_t)blockIdx.x * kWorkWords;
-  const i32x8 head = ((DescPtr8)wi.rec)[0];
-  wi.toks = ((DescPtr8)wi.rec)[1];
-  wi.pages = ((DescPtr8)wi.rec)[2];
-  asm volatile("" ::"s"(head), "s"(wi.toks), "s"(wi.pages));
-  wi.n_tok = head[W_N_TOK];
-  wi.tbl_off = head[W_TBL_OFF];
-  wi.kv_begin = head[W_KV_BEGIN];
-  wi.kv_end = head[W_KV_END];
-  wi.q0 = head[W_CAUSAL_Q0];
-  wi.part_idx = head[W_PART_IDX];
-  const int path_word = head[W_PATH];
+  int path_word;
+  auto read_item = [&]() {
+    wi.rec = (DescPtr)work + (size_t)blockIdx.x * kWorkWords;
+    const i32x8 head = ((DescPtr8)wi.rec)[0];
+    wi.toks = ((DescPtr8)wi.rec)[1];
+    wi.pages = ((DescPtr8)wi.rec)[2];
+    asm volatile("" ::"s"(head), "s"(wi.toks), "s"(wi.pages));
+    wi.n_tok = head[W_N_TOK];
+    wi.tbl_off = head[W_TBL_OFF];
+    wi.kv_begin = head[W_KV_BEGIN];
+    wi.kv_end = head[W_KV_END];
+    wi.q0 = head[W_CAUSAL_Q0];
+    wi.part_idx = head[W_PART_IDX];
+    path_word = head[W_PATH];
+  };
+  read_item();
   if ((path_word & kPathMask) == PATH_NOOP) return;
   const bool few_keys = wi.kv_end - wi.kv_begin <= 64;
-  const bool hides = wi.kv_end - 1 > wi.q0;   // the item's first token does not see all keys
-  if (wi.n_tok > 4 && !hides)
-    few_keys ? attend8<4, false, 2, false>(a, wi, sm) : attend8<4, false, 4, false>(a, wi, sm);
-  else if (path_word & kPathAppends)   // one or two tokens on their own pages
-    path_word & kPathOnce ? attend8<1, true, 4>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
-  else if (wi.n_tok <= 2)
-    few_keys ? attend8<1, false, 2>(a, wi, sm) : attend8<1, false, 4>(a, wi, sm);
+  if (wi.kv_end - 1 <= wi.q0) {   // the item's first token sees all keys, and so do the others
+    bool done;
+    if (wi.n_tok > 4)
+      done = few_keys ? attend8<4, false, 2, false>(a, wi, sm) : attend8<4, false, 4, false>(a, wi, sm);
+    else if (path_word & kPathAppends)   // one or two tokens on their own pages
+      done = path_word & kPathOnce ? attend8<1, true, 4, false>(a, wi, sm) : attend8<1, false, 4, false>(a, wi, sm);
+    else if (wi.n_tok <= 2)
+      done = few_keys ? attend8<1, false, 2, false>(a, wi, sm) : attend8<1, false, 4, false>(a, wi, sm);
+    else
+      done = few_keys ? attend8<2, false, 2, false>(a, wi, sm) : attend8<2, false, 4, false>(a, wi, sm);
+    if (done) return;
+    read_item();   // nothing of it is kept for this
+  }
+  if (wi.n_tok <= 2)
+    attend8<1, false, 4, true>(a, wi, sm);
   else if (wi.n_tok <= 4)
-    few_keys ? attend8<2, false, 2>(a, wi, sm) : attend8<2, false, 4>(a, wi, sm);
+    few_keys ? attend8<2, false, 2, true>(a, wi, sm) : attend8<2, false, 4, true>(a, wi, sm);
   else
-    attend8<4, false, 4>(a, wi, sm);
+    attend8<4, false, 4, true>(a, wi, sm);
 }
 static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "attend8 reads the last argument there");
 

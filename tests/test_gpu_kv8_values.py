@@ -1,0 +1,160 @@
+"""Values of very different size in a pool in 8 bits: what a query does not see, or gives no weight, leaves its output alone.
+
+Tolerances.  A key's weight times the power of two of its value is held as one fp16 number, whose unit goes by the largest
+that any one key adds to the query: off by 2^-11 of itself or 2^-20 of that largest (at most 2^-12 for 256 keys).  A split's
+sums are stored as fp16, off by 2^-11 of themselves or of the largest of 64 dims.  The output is rounded to bf16, 2^-8.
+Where outputs are of the order of one these are within 2e-3 + 1e-2 |ref|, the bound of all attention tests; where they are
+not, the same is asked in units of the row's largest output."""
+import numpy as np
+import pytest
+
+from oracle import kv8
+from oracle.attention import widen_bf16
+from oracle.replay import OracleWorld
+from paper_2603_14371_amd import synth
+from paper_2603_14371_amd.synth import ACTION, DECODE, _TraceBuilder, _workload
+from parity_util import assert_lse_close, assert_o_close
+
+pytestmark = pytest.mark.gpu
+LOWEST = 0xFF7F                      # of bf16
+
+
+def scaled(bits, power):
+    """bf16 numbers times 2^power, as far as they stay normal."""
+    e = ((bits >> 7) & 0xff).astype(np.int32)
+    return np.where(e == 0, bits, (bits & 0x807f) | (np.clip(e + power, 1, 254) << 7)).astype(np.uint16)
+
+
+def outputs(w, source):
+    """The last step's bits and log-sum-exps, and the oracle's on what the pool holds."""
+    from paper_2603_14371_amd.harness import GpuWorld
+    gw = GpuWorld(w, source, poison=True, kv8=True, max_partials=4096)
+    ow = OracleWorld(w["num_blocks"], 1, kv8.cached_source(source), w["scale"])
+    for op in w["trace"]:
+        g, o = gw.apply(op), ow.apply(op)
+    gw.close()
+    return g["O"][0], g["LSE"][0], o["O"][0], o["LSE"][0]
+
+
+def assert_close_by_row(bits, ref):
+    unit = np.abs(ref).max(axis=-1, keepdims=True)
+    assert np.all(np.abs(widen_bf16(bits) / unit - ref / unit) <= 2e-3 + 1e-2 * np.abs(ref / unit))
+
+
+@pytest.mark.parametrize("size", [21, 28, 40, 100, "lowest", -60])
+@pytest.mark.parametrize("n_new,hist,bad", [(2, 0, 1), (3, 0, 2), (8, 0, 4), (13, 5, 6), (5, 125, 3), (6, 253, 4), (13, 250, 1),
+                                            (50, 0, 20), (60, 700, 59), (4, 509, 2), (16, 1000, 1)])
+def test_a_finite_value_does_not_reach_tokens_before_it(n_new, hist, bad, size):
+    """Of several new tokens those before `bad` do not see its value: their outputs are, bit for bit, what they are beside
+    any other value there."""
+    b = _TraceBuilder()
+    dec = b.stream(b.prefix(70), DECODE)
+    b.tag = 10
+    if hist:
+        b.step([(dec, hist)], attend=False)
+    b.tag = 20
+    b.step([(dec, n_new)])
+    w = _workload("later", 31, 1, 128, b.trace)
+    src = synth.DataSource(w["seed"])
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "v" and recipe["tag"] == 20:
+            x[bad] = LOWEST if size == "lowest" else scaled(x[bad], size)
+        return x
+
+    got, lse, ref, ref_lse = outputs(w, planted)
+    assert_o_close(got[:bad], ref[:bad], "before")
+    if size != "lowest":             # its values are held as infinite
+        assert_close_by_row(got, ref)
+    assert_lse_close(lse, ref_lse, "all")
+    plain = outputs(w, src)
+    assert np.array_equal(got[:bad], plain[0][:bad]) and np.array_equal(lse, plain[1])
+
+
+@pytest.mark.parametrize("size", [13, 25, 40, 90])
+@pytest.mark.parametrize("where", ["prefix", "chunk", "history", "new"])
+def test_a_large_value_of_no_weight_leaves_the_others(where, size):
+    """One key, at a logit 2^-size and far less behind the others', has values 2^size as large."""
+    b = _TraceBuilder()
+    pid = b.prefix(420, b.recipe(420, tag=100))
+    act, dec, few = b.stream(pid, ACTION), b.stream(pid, DECODE), b.stream(pid, DECODE)
+    b.tag = 10
+    b.step([(dec, 700)], attend=False)                 # tag 10
+    b.step([(act, 50), (dec, 1), (few, 5)])            # tag 11
+    w = _workload("no_weight", 17, 1, 512, b.trace)
+    src = synth.DataSource(w["seed"])
+    tag, row = {"prefix": (100, 130), "chunk": (11, 9), "history": (10, 300), "new": (11, 52)}[where]
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "q":
+            x[:, :, 0] = 0x4200                        # 32: a key's first element counts twice in the logit
+        if what == "k":
+            x[:, 0] = 0
+        if recipe["tag"] == tag and row - recipe["tok0"] < n:
+            if what == "k":
+                x[row - recipe["tok0"], 0] = 0xC2C8    # -100: a weight of 2^-288
+            if what == "v":
+                x[row - recipe["tok0"]] = scaled(x[row - recipe["tok0"]], size)
+        return x
+
+    got, lse, ref, ref_lse = outputs(w, planted)
+    assert_o_close(got, ref, where)
+    assert_lse_close(lse, ref_lse, where)
+
+
+@pytest.mark.parametrize("logit", [-20, -60, -80])
+@pytest.mark.parametrize("first", [True, False], ids=["before", "behind"])
+def test_a_small_weight_and_a_large_value_count_by_their_product(logit, first):
+    """A key at e^logit of the others' weight, with values that make up for it: its share of the output is that of the
+    others together, whichever round of keys comes first."""
+    power = int(round(-logit / np.log(2)))
+    b = _TraceBuilder()
+    pid = b.prefix(300, b.recipe(300, tag=100))
+    act, dec = b.stream(pid, ACTION), b.stream(pid, DECODE)
+    b.step([(act, 50), (dec, 3)])
+    w = _workload("product", 19, 1, 128, b.trace)
+    src = synth.DataSource(w["seed"])
+    row = 3 if first else 297
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "q":
+            x[:, :, 0] = 0x4180                        # 16: a key's first element is its logit's
+        if what == "k":
+            x[:, 0] = 0
+        if recipe["tag"] == 100 and what != "q":
+            if what == "k":
+                x[row, 0] = (np.float32(logit).view(np.uint32) >> 16).astype(np.uint16)
+            else:
+                x[row] = scaled(x[row], power + 6)
+        return x
+
+    got, lse, ref, ref_lse = outputs(w, planted)
+    assert_close_by_row(got, ref)
+    assert_lse_close(lse, ref_lse, "all")
+
+
+@pytest.mark.parametrize("spread", [10, 12, 13, 14, 24])
+def test_sizes_that_differ_within_a_split(spread):
+    """Rows of two sizes in turn, on both sides of where units go by the row; zeros among them."""
+    b = _TraceBuilder()
+    pid = b.prefix(333, b.recipe(333, tag=100))
+    act, dec, few = b.stream(pid, ACTION), b.stream(pid, DECODE), b.stream(pid, DECODE)
+    b.step([(dec, 400)], attend=False)
+    b.step([(act, 50), (dec, 1), (few, 7)])
+    w = _workload("two_sizes", 29, 1, 128, b.trace)
+    src = synth.DataSource(w["seed"])
+
+    def planted(recipe, layer, what, n):
+        x = src(recipe, layer, what, n).copy()
+        if what == "v":
+            at = np.arange(n) + recipe["tok0"]
+            x[at % 3 == 1] = scaled(x[at % 3 == 1], -spread)
+            x[at % 50 == 7] = 0
+        return x
+
+    got, lse, ref, ref_lse = outputs(w, planted)
+    assert_o_close(got, ref, "all")
+    assert_lse_close(lse, ref_lse, "all")
