@@ -331,8 +331,8 @@ typedef struct {
 int32_t oxy_rotary_freqs(const oxy_rotary_scaling *scaling, double *freqs, double *amplitude);
 /* Rows of n_tokens tokens (0: nothing to do), n_heads of them side by side per token: row (t, h) at
  * x + t * x_stride + h * 512 -> out + t * out_stride + h * 512, DEVICE bf16, strides in bytes, all
- * 16-byte aligned.  positions: DEVICE int32 [n_tokens].  out may be x with the same stride; other
- * overlaps of rows are not allowed. */
+ * 16-byte aligned (without tokens: anything, null too).  positions: DEVICE int32 [n_tokens].  out may be x
+ * with the same stride; other overlaps of rows are not allowed. */
 int32_t oxy_rotary(const oxy_rotary_config *cfg, const int32_t *positions, const void *x,
                    size_t x_stride, void *out, size_t out_stride, int32_t n_tokens,
                    int32_t n_heads, void *hip_stream);

@@ -340,11 +340,12 @@ int32_t oxy_rotary_freqs(const oxy_rotary_scaling* sc, double* freqs, double* am
 
 int32_t oxy_rotary(const oxy_rotary_config* c, const int32_t* positions, const void* x, size_t x_stride, void* out,
                    size_t out_stride, int32_t n_tokens, int32_t n_heads, void* hip_stream) {
-  if (!c || !c->freqs || !positions || !x || !out) return refuse("rotary: null argument");
+  if (!c || !c->freqs || (n_tokens != 0 && (!positions || !x || !out))) return refuse("rotary: null argument");
   if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2) return refuse("rotary: rot_dims must be even, 2 to 256");
   if (c->layout != OXY_ROTARY_HALVES && c->layout != OXY_ROTARY_PAIRS) return refuse("rotary: unknown layout");
   if (n_tokens < 0 || n_tokens > OXY_ROTARY_MAX_TOKENS || n_heads < 1 || n_heads > OXY_ROTARY_MAX_HEADS)
     return refuse("rotary: n_tokens or n_heads");
+  if (n_tokens == 0) return OXY_OK;   // what holds no rows may lie anywhere
   const size_t row = (size_t)n_heads * oxy::kDim * 2;
   if (((uintptr_t)x | (uintptr_t)out | x_stride | out_stride) & 15) return refuse("rotary: rows must be 16-byte aligned");
   if (n_tokens > 1 && (x_stride < row || out_stride < row)) return refuse("rotary: stride below n_heads rows");
