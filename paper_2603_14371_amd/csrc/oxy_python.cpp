@@ -3,6 +3,7 @@
 #include <Python.h>
 
 #include <cstdint>
+#include <cstring>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -25,10 +26,11 @@ extern "C" int32_t oxy_ints_of_list(PyObject* list, int64_t* out, int64_t n) {
 
 namespace {
 
-PyObject* g_value;   // the attribute's name
+PyObject* g_value;      // the attribute's name
+PyObject* g_void_p;     // ctypes.c_void_p
 
-// An address: an int, None, or an object with an int or None as its `value` (ctypes.c_void_p).  False, with no exception
-// set, for anything else.
+// An address: an int, None, or a ctypes.c_void_p.  False, with no exception set, for anything else (ctypes refuses other
+// objects that have a value, numbers of its own kinds among them).
 bool address_of(PyObject* o, uint64_t* out) {
   if (o == Py_None) return *out = 0, true;
   if (PyLong_CheckExact(o)) {
@@ -37,7 +39,7 @@ bool address_of(PyObject* o, uint64_t* out) {
     PyErr_Clear();
     return false;
   }
-  if (PyFloat_Check(o) || PyLong_Check(o)) return false;
+  if ((PyObject*)Py_TYPE(o) != g_void_p) return false;
   PyObject* v = PyObject_GetAttr(o, g_value);
   if (!v) return PyErr_Clear(), false;
   const bool ok = (v == Py_None || PyLong_CheckExact(v)) && address_of(v, out);
@@ -188,6 +190,10 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "libmarshal", nullptr, -1, g_meth
 }  // namespace
 
 PyMODINIT_FUNC PyInit_libmarshal(void) {
+  PyObject* ctypes = PyImport_ImportModule("ctypes");
+  if (!ctypes) return nullptr;
+  g_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
+  Py_DECREF(ctypes);
   g_value = PyUnicode_InternFromString("value");
-  return g_value ? PyModule_Create(&g_module) : nullptr;
+  return g_void_p && g_value ? PyModule_Create(&g_module) : nullptr;
 }
