@@ -29,6 +29,19 @@ TOKEN_BYTES = 1024          # K + V of one token in one layer: 2 * 256 * 2 B
 QO_BYTES = 2 * 8 * 256 * 2  # one query token read + one output token written
 
 
+# what the measured launches are compiled from
+KERNEL_SOURCES = ["oxy_kernels.hip", "oxy_merge.h", "oxy_device.h", "oxy_internal.h"]
+
+
+def kernel_source_hash():
+    import hashlib
+    h = hashlib.sha256()
+    for name in KERNEL_SOURCES:
+        with open(os.path.join(ROOT, "paper_2603_14371_amd", "csrc", name), "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()[:16]
+
+
 def _build_state(workload, device, split_tokens, stream_split_tokens=0, max_partials=16384):
     """Replays the set-up part of a trace (everything before its first attended step) with
     random resident data; returns the world and the remaining steps."""
@@ -916,10 +929,8 @@ def main():
         out["host_us_per_step_recorded_graph"] = round(s["host_us_per_step_graph"], 1)
     traffic_file = os.path.join(ROOT, "profiles", "pmc_traffic_stress.json")
     if os.path.exists(traffic_file):
-        import hashlib
         t = json.load(open(traffic_file))
-        src = os.path.join(ROOT, "paper_2603_14371_amd", "csrc", "oxy_kernels.hip")
-        now = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+        now = kernel_source_hash()
         out["roofline"]["traffic"] = t["hbm_bytes_per_launch"]
         out["roofline"]["traffic_source"] = "profiles/pmc_traffic_stress.json (rocprofv3 --pmc " \
                                             "FETCH_SIZE / WRITE_SIZE, scaled by a copy of known size)"
