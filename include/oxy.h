@@ -291,7 +291,8 @@ int32_t oxy_batch_destroy(oxy_batch *batch);
 int32_t oxy_gather_kv(oxy_pool *pool, int32_t layer, const int64_t *slots, int32_t n,
                       void *k_out, void *v_out, void *hip_stream);
 /* The same of layers [layer_begin, layer_end): layer l's rows go to k_out + (l - layer_begin) * layer_stride
- * and v_out likewise (bytes, at least n * 512, a multiple of 16).  On a pool in 8 bits one launch serves all the layers. */
+ * and v_out likewise (bytes, at least n * 512, a multiple of 16).  On a pool in 8 bits a launch serves all the
+ * layers; a long or scattered list takes several. */
 int32_t oxy_gather_kv_layers(oxy_pool *pool, int32_t layer_begin, int32_t layer_end,
                              const int64_t *slots, int32_t n, void *k_out, void *v_out,
                              size_t layer_stride, void *hip_stream);

@@ -1519,7 +1519,9 @@ int32_t gather_impl(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const i
     if (slots[i] < 0 || slots[i] >= n_slots)
       return fail(OXY_ERR_INVALID_ARG, "%s: slot %lld out of range", who, (long long)slots[i]);
   // consecutive slots of one block travel as one run (see launch_gather_inline); in 8 bits consecutive tokens of one table
-  // as its block ids (see Table8), where there are more than a few blocks of them
+  // as its block ids (see Table8), where the list ends with them or they would fill a launch of runs: before that a table is
+  // one launch more.  us for six layers, blocks in runs / as a table, five slots elsewhere behind them: 8 blocks 3.1 / 4.95, 64
+  // 4.4 / 6.2, 128 5.9 / 7.8, 256 11.3 / 11.4, 512 20.6 / 17.0, 1500 56.3 / 40.
   const oxy::Table8 table = table8(p, layer_begin, layers, layer_stride);
   int32_t ids[oxy::max_table_blocks(true)];
   for (int32_t done = 0; done < n;) {
@@ -1537,7 +1539,7 @@ int32_t gather_impl(oxy_pool* p, int32_t layer_begin, int32_t layer_end, const i
         at += len;
         if ((slot & (kPage - 1)) + len < kPage) break;
       }
-      if (at == n || n_ids >= 64) {
+      if (at == n || n_ids >= oxy::kMaxGatherRows / kPage) {
         hipError_t e = oxy::launch_gather_table8((char*)k_out + (size_t)done * oxy::kDim * 2,
                                                  (char*)v_out + (size_t)done * oxy::kDim * 2, table, ids, offset,
                                                  at - done, (hipStream_t)hip_stream);
