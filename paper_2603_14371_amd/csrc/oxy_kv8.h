@@ -51,6 +51,8 @@ OXY_WEAK hipError_t launch_gather_inline8(Layer8 layer, const GatherRuns& runs, 
 struct AttnArgs8 : AttnArgs {
   const uint8_t* scales;    // layer_base and scales: those of the Layer8
   int32_t max_parts;        // most split results of a token
+  const int32_t* long_toks; // [n_long]: the tokens of more than kLongParts
+  int32_t n_long;
 };
 // As launch_attention_work.
 OXY_WEAK hipError_t launch_attention_work8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop);

@@ -840,23 +840,30 @@ static_assert(Params<decltype(&attn8_kernel)>::offset_of_last() == 5 * 8, "atten
 // A wavefront per token and head takes 0.9 us for every 16 split results behind the first (29 us for 512: two workgroups
 // read 2 MB in turn).  Here a token of more than kLongParts results takes a workgroup for each head and 64 dims: eight
 // wavefronts share the results out, 64 at a time with everything in flight at once, each with a maximum of its own, and the
-// first one joins the eight (256 results of a history of 131072 tokens 3 us).  Tokens of fewer are merged by one wavefront
-// as in every other launch, so that a token's bits do not depend on what else is in the batch.  us per layer with a limit
-// of 16 / 32 / 64: one history of 6000 tokens 8.3 / 8.6 / 8.9, 16 of 4000 15.1 / 13.9 / 13.9, one of 10000 8.6 / 8.6 / 9.8.
+// first one joins the eight (256 results of a history of 131072 tokens 3 us).  These workgroups come first (long_toks); behind
+// them every other token is one workgroup, merged by a wavefront for each head as in every other launch, so that a token's bits
+// do not depend on what else is in the batch (eight chunks of 50 on 832 tokens beside a history of 9000 15.7 us a layer, of
+// 131072 26.6; with 32 workgroups for every token 23.7 and 37.1, with a wavefront a head for every token 18.0 and 46.9).  us
+// per layer with a limit of 16 / 32 / 64: one history of 6000 tokens 8.3 / 8.6 / 8.9, 16 of 4000 15.1 / 13.9 / 13.9, one of
+// 10000 8.6 / 8.6 / 9.8.
 constexpr int kLongWaves = 8, kLongAhead = 16;   // a wavefront's loads: kLongAhead times four results of 128 bytes
 __global__ __launch_bounds__(64 * kLongWaves) void merge_long_kernel(const uint16_t* part_acc, const float* part_ml, void* out,
                                                                     float* lse, const int32_t* n_parts,
-                                                                    const int32_t* part_off) {
+                                                                    const int32_t* part_off, const int32_t* long_toks,
+                                                                    const int32_t n_long) {
+  static_assert(kLongWaves == kHeads, "a short token takes a wavefront for each head");
   __shared__ f32x4 os[kLongWaves][16];
   __shared__ float bigs[kLongWaves], totals[kLongWaves];
-  const int tok = blockIdx.x / (4 * kHeads), h = (blockIdx.x >> 2) % kHeads, part = blockIdx.x & 3;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n_first = 4 * kHeads * n_long, bid = blockIdx.x;
+  const int tok = bid < n_first ? ((DescPtr)long_toks)[bid / (4 * kHeads)] : bid - n_first;
   const int np = ((DescPtr)n_parts)[tok];
   const size_t base = (size_t)((DescPtr)part_off)[tok];
-  if (np <= kLongParts) {
-    if (wv == 0 && part == 0) merge_any({part_acc, part_ml, out, lse, n_parts, part_off}, base, np, tok, h, lane);
+  if (bid >= n_first) {   // the tokens in turn, but those above
+    if (np <= kLongParts) merge_any({part_acc, part_ml, out, lse, n_parts, part_off}, base, np, tok, wv, lane);
     return;
   }
+  const int h = (bid >> 2) % kHeads, part = bid & 3;
   const int i = lane & 15, p = lane >> 4;   // dims 64 * part + 4i..+3 of every fourth result
   const char* ml = (const char*)(part_ml + (base * kHeads + h) * 4);
   const char* acc = (const char*)(part_acc + (base * kHeads + h) * kDim + 64 * part + 4 * i);
@@ -1003,14 +1010,15 @@ hipError_t launch_attention_work8(const AttnArgs8& a, hipStream_t s, hipEvent_t 
 }
 
 hipError_t launch_merge8(const AttnArgs8& a, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
-  if (a.max_parts <= kLongParts) return launch_merge_append(a, nullptr, s, start, stop);
-  if (a.n_q <= 0) return hipErrorInvalidValue;
+  if (a.n_long <= 0) return launch_merge_append(a, nullptr, s, start, stop);
+  if (a.n_q < a.n_long) return hipErrorInvalidValue;
+  const int32_t grid = 4 * kHeads * a.n_long + (a.n_long < a.n_q ? a.n_q : 0);
   if (start || stop)
-    hipExtLaunchKernelGGL(merge_long_kernel, dim3(4 * kHeads * a.n_q), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc,
-                          a.part_ml, a.out, a.lse, a.n_parts, a.part_off);
+    hipExtLaunchKernelGGL(merge_long_kernel, dim3(grid), dim3(64 * kLongWaves), 0, s, start, stop, 0, a.part_acc, a.part_ml,
+                          a.out, a.lse, a.n_parts, a.part_off, a.long_toks, a.n_long);
   else
-    merge_long_kernel<<<4 * kHeads * a.n_q, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts,
-                                                                     a.part_off);
+    merge_long_kernel<<<grid, 64 * kLongWaves, 0, s>>>(a.part_acc, a.part_ml, a.out, a.lse, a.n_parts, a.part_off, a.long_toks,
+                                                       a.n_long);
   return hipGetLastError();
 }
 

@@ -68,7 +68,7 @@ struct StepKey {
   float scale = 0.f;
   int32_t layer_begin = 0, layer_end = 0, mode = 0;   // mode: 0 separate, 1 fused, 2 folded
   int32_t n_work = 0, n_tokens = 0, n_fresh = 0, off_work = 0, off_tables = 0, off_part_off = 0,
-          off_n_parts = 0, write_through = 0, long_merge = 0, many_append = 0;
+          off_n_parts = 0, write_through = 0, n_long = 0, many_append = 0;
   bool operator==(const StepKey& o) const {
     return d_base == o.d_base && k_new == o.k_new && v_new == o.v_new && q == o.q &&
            out == o.out && lse == o.lse && kv_stride == o.kv_stride && q_stride == o.q_stride &&
@@ -76,14 +76,14 @@ struct StepKey {
            layer_end == o.layer_end && mode == o.mode && n_work == o.n_work &&
            n_tokens == o.n_tokens && n_fresh == o.n_fresh && off_work == o.off_work && off_tables == o.off_tables &&
            off_part_off == o.off_part_off && off_n_parts == o.off_n_parts &&
-           write_through == o.write_through && long_merge == o.long_merge;
+           write_through == o.write_through && n_long == o.n_long;
   }
   // same number and kernels of launches in the same order: an instantiated graph can be updated
   // in place from a recording of the other
   bool same_topology(const StepKey& o) const {
     return layer_end - layer_begin == o.layer_end - o.layer_begin && mode == o.mode &&
            oxy::merge_heads(n_tokens) == oxy::merge_heads(o.n_tokens) && (n_fresh > 0) == (o.n_fresh > 0) &&
-           long_merge == o.long_merge && many_append == o.many_append;
+           (n_long > 0) == (o.n_long > 0) && many_append == o.many_append;
   }
 };
 struct StepGraph {
@@ -127,6 +127,8 @@ struct oxy_batch {
   int32_t n_fresh = 0;    // blocks of items whose own-phase tiles read k_new / v_new (folded append)
   int32_t off_fresh = 0;
   int32_t max_parts = 0;  // most split results of a token
+  int32_t n_long = 0;     // in 8 bits: tokens of more than kLongParts
+  int32_t off_long = 0;
   bool decodes = false;           // some item has <= 2 new tokens
   bool append_foldable = false;   // every item has <= 2 new tokens or an empty own history
   // word offsets inside the descriptor
@@ -291,6 +293,8 @@ oxy::AttnArgs8 attn_args(const oxy_pool* p, const oxy_batch* b, int32_t layer, c
   a.d_slots = nullptr;
   a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
   a.max_parts = b->max_parts;
+  a.long_toks = d + b->off_long;
+  a.n_long = b->n_long;
   return a;
 }
 
@@ -1101,8 +1105,11 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
   b->n_partials = (int32_t)n_partials;
   b->decodes = decodes;
   for (int32_t n : n_parts) b->max_parts = std::max(b->max_parts, n);
+  if (p->kv8 && b->max_parts > oxy::kLongParts)
+    b->n_long = (int32_t)std::count_if(n_parts.begin(), n_parts.end(), [](int32_t n) { return n > oxy::kLongParts; });
   b->append_foldable = foldable;
-  // Sections in the order work | slots | part_off | n_parts | fresh runs | token lists | tables: the block
+  // Sections in the order work | slots | part_off | n_parts | fresh runs (in 8 bits, where there are none: the
+  // tokens of many split results) | token lists | tables: the block
   // tables, whose size changes whenever a stream takes a new block, come last, so that the
   // device addresses of all sections stay the same from step to step while the shape of the
   // batch (tokens, work items, tile token lists) does -- a recorded launch sequence
@@ -1117,7 +1124,8 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
   b->off_n_parts = b->off_part_off + (int32_t)part_off.size();
   b->n_fresh = (int32_t)fresh_runs.size();
   b->off_fresh = b->off_n_parts + (int32_t)n_parts.size();
-  b->off_toks = b->off_fresh + b->n_fresh;
+  b->off_long = b->off_fresh + b->n_fresh;
+  b->off_toks = b->off_long + b->n_long;
   b->off_tables = b->off_toks + (int32_t)toks.size();
   std::vector<int32_t>& h = b->host;
   h.resize((size_t)b->off_tables + tbl_words);
@@ -1146,6 +1154,8 @@ int32_t oxy_batch_build(oxy_pool* p, const oxy_item* items, int32_t n_items, int
   std::copy(fresh_runs.begin(), fresh_runs.end(), h.begin() + b->off_fresh);
   std::copy(part_off.begin(), part_off.end(), h.begin() + b->off_part_off);
   std::copy(n_parts.begin(), n_parts.end(), h.begin() + b->off_n_parts);
+  for (int32_t t = 0, at = b->off_long; t < (int32_t)n_parts.size() && at < b->off_toks; ++t)
+    if (n_parts[t] > oxy::kLongParts) h[at++] = t;
   std::vector<char> is_wide(wide_tiles.empty() ? 0 : (size_t)n_items_of_list);
   for (int32_t i : wide_tiles) is_wide[i] = 1;
   // Work records, 128 bytes each: header, then inline copies of the tile's token ids and of the
@@ -1371,7 +1381,7 @@ int32_t replay_step(const StepCall& c, hipStream_t s) {
   key.off_part_off = b->off_part_off;
   key.off_n_parts = b->off_n_parts;
   key.write_through = writes_through(b);
-  key.long_merge = p->kv8 && b->max_parts > oxy::kLongParts;
+  key.n_long = b->n_long;
   key.many_append = p->kv8 && oxy::many_append8(b->n_tokens);
   const uint64_t now = ++p->graph_clock;
   StepGraph* hit = nullptr;
