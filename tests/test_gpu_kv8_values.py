@@ -158,3 +158,40 @@ def test_sizes_that_differ_within_a_split(spread):
     got, lse, ref, ref_lse = outputs(w, planted)
     assert_o_close(got, ref, "all")
     assert_lse_close(lse, ref_lse, "all")
+
+
+@pytest.mark.parametrize("n_new", [1, 3, 9])
+@pytest.mark.parametrize("keys", [1, 2, 3, 5, 17, 64, 100, 300, 700])
+def test_outputs_within_what_each_rounding_may_cost(keys, n_new):
+    """Element by element, also where the terms of a sum cancel.  With A = sum P |v| / sum P and M the largest A of the 64 dims
+    that share an exponent: weights in fp16 cost 2^-11 A, split results 2^-11 M (the two together at most 2^-20 M more), the
+    output 2^-8 |ref|.  Logits below 16 in 32 bits, eight products of 32 dims after one another: 16 * 8 * 2^-24 of each
+    weight, and as much of their sum, 2^-16 A together."""
+    import torch
+    from test_gpu_kv8 import Cache
+    c = Cache(n_layers=1, blocks=80)
+    rng = np.random.default_rng(keys)
+    bits = lambda *shape: (rng.standard_normal(shape).astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)  # noqa: E731
+    pk, pv, nk, nv, q = bits(keys, 256), bits(keys, 256), bits(n_new, 256), bits(n_new, 256), bits(n_new, 8, 256)
+    up = [c.up(x) for x in (pk, pv, nk, nv, q)]
+    pid = c.B.oxy_prefix_create(c.pool)
+    c.B.oxy_prefix_append(c.pool, pid, 0, up[0].data_ptr(), up[1].data_ptr(), keys, 0, c.stream)
+    sid = c.B.oxy_stream_create(c.pool, pid, DECODE)
+    batch = c.B.oxy_batch_build(c.pool, [(sid, n_new)], 0, c.stream)
+    c.B.oxy_stream_append(c.pool, batch, 0, up[2].data_ptr(), up[3].data_ptr(), c.stream)
+    out = torch.zeros_like(up[4])
+    c.B.oxy_mixed_attention(c.pool, batch, 0, up[4].data_ptr(), out.data_ptr(), 0, 1.0 / 16, c.stream)
+    got = widen_bf16(c.back(out))
+    c.B.oxy_batch_destroy(batch)
+    c.close()
+    k, v = (kv8.cached_values(np.concatenate(x)) for x in ((pk, nk), (pv, nv)))
+    for t in range(n_new):
+        n = keys + t + 1
+        s = widen_bf16(q[t]) @ k[:n].T / 16
+        assert np.abs(s).max() < 16
+        p = np.exp(s - s.max(axis=1, keepdims=True))
+        p /= p.sum(axis=1, keepdims=True)
+        ref, a = p @ v[:n], p @ np.abs(v[:n])
+        m = np.repeat(a.reshape(8, 4, 64).max(axis=2), 64, axis=1)
+        bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -16) * a + (2.0 ** -11 + 2.0 ** -20) * m
+        assert np.all(np.abs(got[t] - ref) <= bound), (np.abs(got[t] - ref) / bound).max()
