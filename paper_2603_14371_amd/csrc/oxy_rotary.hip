@@ -25,10 +25,11 @@ constexpr int kMaxPairs = kDim / 2;
 enum RotaryForm { FORM_PAIRS, FORM_HALVES, FORM_HALVES_ANY };
 
 // Cosine and sine of position * freq times the amplitude, rounded to 32 bits once.  The angle is brought to a fraction of a
-// turn, then to within an eighth of one around the nearest quarter, where the series of the two functions are cut where
-// their next terms are below 1e-11 (a fiftieth of a thousandth of half a unit of the 32-bit result).  20 instructions in 64
-// bits, which run at the rate of 32 (with the library's sincospi, whose last bits are rounded off here, three times as
-// many: nine heads of 8192 tokens 20.7 us, with this 17.5).
+// turn, then to within an eighth of one around the nearest quarter, where the series of the two functions are cut behind
+// x^13 / 13! and x^14 / 14!: the next terms are at most 2e-14 and 1e-15, a millionth of half a unit of the 32-bit result (2^-25
+// near one), so the rounding is that of the exact value but for one in a million.  20 instructions in 64 bits, which run at the
+// rate of 32 (with the library's sincospi, whose last bits are rounded off here, three times as many: nine heads of 8192
+// tokens 20.7 us, with this 17.5).
 __device__ __forceinline__ void turn_of(const double freq, const double amplitude, const int position, float& c, float& s) {
   const double turns = (double)position * freq * 0.15915494309189533577;   // 1 / (2 pi)
   const double part = turns - rint(turns), quarter = rint(4.0 * part);
@@ -141,7 +142,7 @@ __device__ __forceinline__ u32x4 turned(RowLoad x, const LaneTurns& w, const int
 // kTokens of a workgroup: their angles are taken once for all heads, by all threads, and come to the lanes through LDS.
 // With four, two half wavefronts share a token's heads; with one, all eight do.  A half wavefront keeps its cosines and
 // sines, and kRows rows in flight.  Nine heads of 8192 tokens (75 MB) 18.0 us in halves, 17.0 in pairs: 4.2 and 4.4 TB/s;
-// of 64 tokens 2.6 us.
+// in halves that are not whole chunks, whose partners are loaded one by one, 29; of 64 tokens 2.6 us.
 template <int kForm, int kTokens>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const char* x, const size_t x_stride, char* out,
                                                      const size_t out_stride, const int32_t n_tokens,
@@ -245,7 +246,8 @@ __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* posit
 
 namespace {
 // From here on there are four tokens for every CU's two resident workgroups and more, and four share one's start.  One /
-// four per workgroup, nine heads in halves: 2048 tokens 5.19 / 5.27 us, 3000 6.77 / 6.64, 8192 18.3 / 17.7.
+// four per workgroup, nine heads in halves: 2048 tokens 5.19 / 5.27 us, 3000 6.77 / 6.64, 8192 18.3 / 17.7; in halves that are
+// not whole chunks 2048 tokens 11.9 / 9.7.
 constexpr int kManyTokens = 2049;
 int form_of(const RotaryArgs& r) {
   return r.pairs ? FORM_PAIRS : (r.rot_dims >> 1) % 8 == 0 ? FORM_HALVES : FORM_HALVES_ANY;
