@@ -401,11 +401,12 @@ struct __align__(16) WorkLds8 {
 // 256 on 32 44.1 / 41.1).
 //
 // What bounds it.  Small launches: the chain record - pages - logits - P - sums, 2.7 us, and the two launches themselves
-// (one chunk and one request 6.85 us a layer, one request 5.7).  Chunks: eight of 50 on 2048 tokens take 18.9 us with
-// the merge, of which the first loads of 512 workgroups are 2.4 us and a SIMD issues vector instructions for 5.4 us
-// (128 conversions and 300 others a round) and matrix ones for 3.6 (128 a round of eight tokens), which overlap little;
-// no phase taken out alone saves more than 1 us.  Bytes where histories are long: 131072 tokens 15.6 us with the merge, the items alone
-// 13.5 when traced, 5.0 TB/s.
+// (one chunk and one request 7.0 us a layer, one request 5.8).  Chunks: eight of 50 on 2048 tokens take 19.8 us with the
+// merge, of which the items are 16.3 when traced.  A SIMD issues vector instructions for 31 % of those (128 conversions and 300
+// others a round) and matrix ones for 17 % (128 a round of eight tokens), which overlap little; the first loads of 512
+// workgroups are 2.4 us, 15.2 MB of split results are written, and no phase taken out alone saves more than 1 us.  Seven items
+// of a chunk convert the same codes.  Bytes where histories are long: 131072 tokens 15.9 us with the merge, the items alone
+// 13.6 when traced, 5.0 TB/s.
 // Not kept, for the same launches: a group's softmax beside another's products in program order, raised wave
 // priorities, four workgroups per CU (registers spill), rounds of 256 keys.
 template <int G, bool kOnce, int kSteps, bool kByRow>
