@@ -195,3 +195,74 @@ def test_outputs_within_what_each_rounding_may_cost(keys, n_new):
         m = np.repeat(a.reshape(8, 4, 64).max(axis=2), 64, axis=1)
         bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -16) * a + (2.0 ** -11 + 2.0 ** -20) * m
         assert np.all(np.abs(got[t] - ref) <= bound), (np.abs(got[t] - ref) / bound).max()
+
+
+def _sized(data):
+    """Values of sizes up to 2^45 apart, by their own bits, so that a row is the same in any batch."""
+    def read(recipe, layer, what, n):
+        x = data(recipe, layer, what, n)
+        if what != "v":
+            return x
+        x = x.copy()
+        for rest, power in ((0, 25), (1, -20)):
+            rows = x[:, 1] % 7 == rest
+            x[rows] = scaled(x[rows], power)
+        x[x[:, 1] % 61 == 3] = 0
+        return x
+    return read
+
+
+def _outputs_of(me, others, prefixes):
+    """Items are (prefix, kind, history, new tokens, tag).  `me`'s outputs in one step with `others` before and behind it, and
+    the oracle's; how many query tokens the widest record of the launch has."""
+    from oracle.attention import attend_item
+    from paper_2603_14371_amd import binding as B
+    from paper_2603_14371_amd.harness import GpuWorld
+    b = _TraceBuilder()
+    pids = [b.prefix(n, b.recipe(n, tag=30 + i)) for i, n in enumerate(prefixes)]
+    half = len(others) // 2
+    items = []
+    for p, kind, hist, n, tag in others[:half] + [me] + others[half:]:
+        sid = b.stream(pids[p], kind)
+        if hist:
+            b.step([(sid, hist)], attend=False, recipe={"tag": 500 + tag, "tok0": 0, "n_total": hist})
+        items.append((sid, n, tag))
+    w = _workload("sized", 4, 1, 3000, b.trace)
+    data = _sized(synth.DataSource(4))
+    gw = GpuWorld(w, data, kv8=True, poison=True, max_q_tokens=2048, max_append_tokens=32768, max_partials=40000)
+    gw.run(w["trace"])
+    gw.data_fn = lambda recipe, layer, what, n: np.concatenate(
+        [data({"tag": 900 + tag, "tok0": 0, "n_total": m}, layer, what, m) for _, m, tag in items])
+    batch = B.oxy_batch_build(gw.pool, [(s, n) for s, n, _ in items], 0, gw._stream())
+    widest = max(r[1] for r in B.oxy_batch_records(batch))
+    B.oxy_batch_destroy(batch)
+    for (sid, n, tag), it in zip(items, others[:half] + [me] + others[half:]):
+        if it[1] == DECODE:
+            B.oxy_stream_rewind(gw.pool, sid, it[2])
+    r = gw.step({"op": "step", "items": [(s, n) for s, n, _ in items], "attend": True, "data": None})
+    gw.close()
+    at = sum(n for _, n, _ in items[:half])
+    p, kind, hist, n, tag = me
+    got = r["O"][0][at:at + n], r["LSE"][0][at:at + n]
+    rec = lambda t, m: {"tag": t, "tok0": 0, "n_total": m}  # noqa: E731
+    held = lambda t, m, what: kv8.bf16_bits(kv8.cached_values(data(rec(t, m), 0, what, m)))  # noqa: E731
+    own = [np.concatenate([held(500 + tag, hist, x), held(900 + tag, n, x)]) if hist else held(900 + tag, n, x) for x in "kv"]
+    ref = attend_item(0 if kind == ACTION else 1, data(rec(900 + tag, n), 0, "q", n), held(30 + p, prefixes[p], "k"),
+                      held(30 + p, prefixes[p], "v"), own[0], own[1], w["scale"])
+    return got, ref, widest
+
+
+@pytest.mark.parametrize("me,prefix", [((0, ACTION, 0, 50, 7), 2048), ((0, ACTION, 0, 13, 7), 300), ((0, DECODE, 40, 1, 7), 900),
+                                       ((0, DECODE, 1100, 30, 7), 300), ((0, DECODE, 0, 6, 7), 900)], ids=str)
+def test_sizes_in_items_of_every_width(me, prefix):
+    """The same bits whatever shares the launch, and as the oracle says; among many an item has eight query tokens."""
+    chunks = [(i % 8, ACTION, 0, 50, 100 + i) for i in range(8)]
+    alone, ref, _ = _outputs_of(me, [], [prefix])
+    assert_close_by_row(alone[0], ref[0])
+    assert_lse_close(alone[1], ref[1], "alone")
+    widths = set()
+    for others in (chunks[1:4], chunks[1:] + [(0, DECODE, 20 * i, 1, 20 + i) for i in range(20)]):
+        got, _, widest = _outputs_of(me, others, [prefix] + [2048] * 7)
+        widths.add(int(widest))
+        assert np.array_equal(got[0], alone[0]) and np.array_equal(got[1], alone[1])
+    assert 8 in widths
