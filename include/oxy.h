@@ -145,13 +145,15 @@ typedef struct {
                                launches tiles of 4 or 8 tokens) and the own phase of
                                action chunks and multi-token decode.  Multiple of 32, <= 1024.
                                0 -> chosen from the length of the KV source alone: about an
-                               eighth of it, within [64, 256]; 32 for a chunk of at most 64
-                               tokens on an empty own history (an action chunk)             */
+                               eighth of it, within [64, 256]; 32 (a pool in 8 bits: 64) for a
+                               chunk of at most 64 tokens on an empty own history (an action
+                               chunk)                                                        */
   int32_t stream_split_tokens; /* KV tokens per work item of the decode streaming path, multiple
                                of 32, <= 1024 (0 -> split_tokens; if that is 0 too: 128 for an own
-                               history of at most 512 tokens, else 256).  Both depend
-                               only on the pool and the item, so an item's arithmetic never
-                               depends on its batch mates                                    */
+                               history of at most 512 tokens, else 256; in a pool in 8 bits
+                               512 for one of more than 65536).  Both depend only on the pool
+                               and the item, so an item's arithmetic never depends on its
+                               batch mates                                                   */
   int32_t flags;
 } oxy_pool_config;
 
