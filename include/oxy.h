@@ -288,6 +288,50 @@ int32_t oxy_append_attention(oxy_pool *pool, const oxy_batch *batch, int32_t lay
                              float *lse, float scale, void *hip_stream);
 int32_t oxy_batch_destroy(oxy_batch *batch);
 
+/* --- prefill: many query tokens of a prefix, or of a whole prompt, at once --------------- */
+/* Visible set of a query at position p of an item of `len` tokens: those at positions
+ * j < min(len, max(p + 1, n_full)).  n_full = 0: causal; len or more: every token sees every token; between:
+ * what the item begins with (an observation's images and instruction, Eq. 1) sees itself whole, what follows
+ * is causal.  A row of outputs depends on its queries and on the tokens that it sees, up to rounding: how keys are cut
+ * into parts goes by all items of the batch.  Values that a query does not see do not reach it, whatever they are; a key
+ * that is not finite makes the outputs of the queries that see it NaN, a value that is not finite its dim, or the 64 dims
+ * that it is among, of theirs NaN or infinite. */
+typedef struct {
+  int32_t prefix_id;
+  int32_t n_new;  /* >= 1 tokens appended behind the prefix's length AND queried */
+  int32_t n_full; /* >= 0, see above */
+} oxy_prefix_item;
+/* New tokens of prefixes (a prefill, or the next part of one; also behind what a fork shares): extends
+ * every listed prefix by n_new tokens, taking blocks in item order, and builds a batch as oxy_batch_build does, on a
+ * descriptor slot like that one's, with flags like that one's.  A prefix is listed once, is not sealed and still has
+ * its creator's reference.  The rows are stored, layer by layer, by oxy_stream_append, oxy_rotary_append or
+ * oxy_rotary_axes_append with this batch, then attended over by oxy_prefix_attention; oxy_batch_slots and
+ * oxy_batch_info serve it too, the calls of a step of streams do not (OXY_ERR_INVALID_ARG).  At most max_q_tokens
+ * (with OXY_BATCH_APPEND_ONLY max_append_tokens) new tokens. */
+int32_t oxy_prefix_batch_build(oxy_pool *pool, const oxy_prefix_item *items, int32_t n_items,
+                               int32_t flags, void *hip_stream, oxy_batch **out);
+/* q, out: DEVICE bf16, token t's eight rows of 256 at q + t * q_stride and out + t * out_stride (bytes; 16-byte
+ * aligned, at least 4096), tokens in batch order, so a projection's output is taken as it is.  lse: DEVICE float
+ * [n][8] or NULL.  Any scale.  Must be enqueued behind what stores the new rows of this layer.  out must not overlap q. */
+int32_t oxy_prefix_attention(oxy_pool *pool, const oxy_batch *batch, int32_t layer, const void *q,
+                             size_t q_stride, void *out, size_t out_stride, float *lse, float scale,
+                             void *hip_stream);
+/* Whole prompts side by side, with keys and values in the rows that a projection wrote and nothing in the cache (of
+ * a pool of either form: it lends its workspace). */
+typedef struct {
+  int32_t n_tokens; /* 0 or more */
+  int32_t n_full;   /* >= 0, see above */
+} oxy_prompt;
+/* The work list of prompts of these lengths; it serves every layer.  At most max_q_tokens tokens in all. */
+int32_t oxy_prompt_batch_build(oxy_pool *pool, const oxy_prompt *prompts, int32_t n_prompts,
+                               void *hip_stream, oxy_batch **out);
+/* q, out, lse, scale as oxy_prefix_attention; token t's key and value, 256 bf16 each, at k + t * k_stride and
+ * v + t * v_stride (DEVICE; bytes, 16-byte aligned, at least 512).  Without tokens nothing is done, whatever the pointers
+ * are.  out must not overlap q, k or v. */
+int32_t oxy_prompt_attention(oxy_pool *pool, const oxy_batch *batch, const void *q, size_t q_stride,
+                             const void *k, size_t k_stride, const void *v, size_t v_stride, void *out,
+                             size_t out_stride, float *lse, float scale, void *hip_stream);
+
 /* Reads K/V rows back in natural order: slots HOST int64 [n] (block*16+offset);
  * k_out, v_out: DEVICE bf16 [n][256]. */
 int32_t oxy_gather_kv(oxy_pool *pool, int32_t layer, const int64_t *slots, int32_t n,
@@ -349,6 +393,23 @@ int32_t oxy_rotary_append(oxy_pool *pool, const oxy_batch *batch, int32_t layer,
                           const oxy_rotary_config *cfg, const int32_t *positions, const void *q,
                           size_t q_stride, void *q_out, const void *k_new, size_t k_stride,
                           const void *v_new, size_t v_stride, void *hip_stream);
+/* Positions with several axes (time, height, width of images and video; words have one position on all of them): pair i is
+ * turned by positions[axis_of_pair[i]][token] * freqs[i], everything else is as above. */
+enum { OXY_ROTARY_MAX_AXES = 4 };
+typedef struct {
+  int32_t n_axes;              /* 1..4                                                                           */
+  const uint8_t *axis_of_pair; /* HOST [rot_dims / 2], each below n_axes: sections side by side, or axes in turn */
+} oxy_rotary_axis_map;
+/* oxy_rotary; positions: DEVICE int32 [n_axes][n_tokens]. */
+int32_t oxy_rotary_axes(const oxy_rotary_config *cfg, const oxy_rotary_axis_map *axes,
+                        const int32_t *positions, const void *x, size_t x_stride, void *out,
+                        size_t out_stride, int32_t n_tokens, int32_t n_heads, void *hip_stream);
+/* oxy_rotary_append; positions: DEVICE int32 [n_axes][tokens of the batch]. */
+int32_t oxy_rotary_axes_append(oxy_pool *pool, const oxy_batch *batch, int32_t layer,
+                               const oxy_rotary_config *cfg, const oxy_rotary_axis_map *axes,
+                               const int32_t *positions, const void *q, size_t q_stride, void *q_out,
+                               const void *k_new, size_t k_stride, const void *v_new, size_t v_stride,
+                               void *hip_stream);
 
 /* --- introspection (HOST outputs; these are the indexing results compared bit-exactly) -- */
 int32_t oxy_stream_info(oxy_pool *pool, int32_t stream_id, int32_t *prefix_id, int32_t *kind,

@@ -14,6 +14,7 @@ pool_model  the indexing oracle: free stack, refcounts, block tables, slots.
 replay      runs an operation trace through pool_model + attention.
 kv8         what a cache in 8 bits holds for a row.
 rotary      rotation of rows by their tokens' positions, and the frequencies.
+prefill     attention of many queries of one item, rotation by positions with several axes.
 schedule    the per-frame execution flow (Alg. 1) under arbitrary arrivals, and the
             ablation variants, as a plain simulation.
 

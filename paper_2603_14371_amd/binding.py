@@ -27,6 +27,7 @@ STEP_FUSE_ACROSS_LAYERS = 1
 STEP_FOLD_APPEND = 2
 STEP_GRAPH = 4
 ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+MAX_ROTARY_PAIRS = 128
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = 0, 1, 2, 3, 4
 SCHED_BATCHED, SCHED_UNBATCHED, SCHED_UPPER_BOUND = 0, 1, 2
 
@@ -39,8 +40,9 @@ EXPORTS = [
     "oxy_stream_append", "oxy_mixed_attention", "oxy_mixed_attention_static", "oxy_step_layers", "oxy_step_graph_stats",
     "oxy_append_attention",
     "oxy_batch_destroy",
+    "oxy_prefix_batch_build", "oxy_prefix_attention", "oxy_prompt_batch_build", "oxy_prompt_attention",
     "oxy_gather_kv", "oxy_gather_kv_layers",
-    "oxy_rotary_freqs", "oxy_rotary", "oxy_rotary_append",
+    "oxy_rotary_freqs", "oxy_rotary", "oxy_rotary_append", "oxy_rotary_axes", "oxy_rotary_axes_append",
     "oxy_stream_info", "oxy_stream_blocks", "oxy_prefix_info", "oxy_prefix_blocks",
     "oxy_block_refcounts", "oxy_free_blocks", "oxy_pool_stats", "oxy_batch_info",
     "oxy_batch_slots", "oxy_batch_work", "oxy_batch_records",
@@ -80,6 +82,10 @@ class RotaryConfig(ctypes.Structure):
                 ("amplitude", ctypes.c_double)]
 
 
+class RotaryAxisMap(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("axis_of_pair", ctypes.c_void_p)]
+
+
 class RotaryScaling(ctypes.Structure):
     _fields_ = [("base", ctypes.c_double), ("rot_dims", ctypes.c_int32), ("kind", ctypes.c_int32),
                 ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
@@ -88,6 +94,14 @@ class RotaryScaling(ctypes.Structure):
 
 class Item(ctypes.Structure):
     _fields_ = [("stream_id", ctypes.c_int32), ("n_new", ctypes.c_int32)]
+
+
+class PrefixItem(ctypes.Structure):
+    _fields_ = [("prefix_id", ctypes.c_int32), ("n_new", ctypes.c_int32), ("n_full", ctypes.c_int32)]
+
+
+class Prompt(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("n_full", ctypes.c_int32)]
 
 
 _lib = None
@@ -136,6 +150,11 @@ def lib():
             "oxy_step_graph_stats": [vp, pi32, pi32, pi32],
             "oxy_append_attention": [vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp],
             "oxy_batch_destroy": [vp],
+            "oxy_prefix_batch_build": [vp, ctypes.POINTER(PrefixItem), i32, i32, vp, ctypes.POINTER(vp)],
+            "oxy_prefix_attention": [vp, vp, i32, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp, ctypes.c_float, vp],
+            "oxy_prompt_batch_build": [vp, ctypes.POINTER(Prompt), i32, vp, ctypes.POINTER(vp)],
+            "oxy_prompt_attention": [vp, vp, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp,
+                                     ctypes.c_size_t, vp, ctypes.c_float, vp],
             "oxy_gather_kv": [vp, i32, vp, i32, vp, vp, vp],
             "oxy_gather_kv_layers": [vp, i32, i32, vp, i32, vp, vp, ctypes.c_size_t, vp],
             "oxy_rotary_freqs": [ctypes.POINTER(RotaryScaling), ctypes.POINTER(ctypes.c_double),
@@ -144,6 +163,10 @@ def lib():
                            i32, vp],
             "oxy_rotary_append": [vp, vp, i32, ctypes.POINTER(RotaryConfig), vp, vp, ctypes.c_size_t, vp, vp,
                                   ctypes.c_size_t, vp, ctypes.c_size_t, vp],
+            "oxy_rotary_axes": [ctypes.POINTER(RotaryConfig), ctypes.POINTER(RotaryAxisMap), vp, vp, ctypes.c_size_t, vp,
+                                ctypes.c_size_t, i32, i32, vp],
+            "oxy_rotary_axes_append": [vp, vp, i32, ctypes.POINTER(RotaryConfig), ctypes.POINTER(RotaryAxisMap), vp, vp,
+                                       ctypes.c_size_t, vp, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp],
             "oxy_stream_info": [vp, i32, pi32, pi32, pi32, pi32],
             "oxy_stream_blocks": [vp, i32, pi32, i32],
             "oxy_prefix_info": [vp, i32, pi32, pi32, pi32, pi32],
@@ -189,6 +212,10 @@ class _Quick:
     oxy_append_attention = staticmethod(_not_bound)
     oxy_rotary = staticmethod(_not_bound)
     oxy_rotary_append = staticmethod(_not_bound)
+    oxy_rotary_axes = staticmethod(_not_bound)
+    oxy_rotary_axes_append = staticmethod(_not_bound)
+    oxy_prefix_attention = staticmethod(_not_bound)
+    oxy_prompt_attention = staticmethod(_not_bound)
     # the first two return what they are asked for (a batch's numbers 0.25 us, by ctypes 2.1; 164 slots as a list 1.2 / 7.2,
     # 1338 12.3 / 19.0), the others take slots as a list (2 us less than by ctypes)
     oxy_batch_info = staticmethod(_not_bound)
@@ -383,6 +410,43 @@ def oxy_batch_destroy(batch):
     _check(lib().oxy_batch_destroy(batch))
 
 
+def oxy_prefix_batch_build(pool, items, flags, stream):
+    """items: (prefix_id, n_new, n_full) each."""
+    arr = (PrefixItem * len(items))(*[PrefixItem(int(p), int(n), int(f)) for p, n, f in items])
+    out = ctypes.c_void_p()
+    _check(lib().oxy_prefix_batch_build(pool, arr, len(items), flags, stream or None, ctypes.byref(out)))
+    return out
+
+
+def oxy_prefix_attention(pool, batch, layer, q_ptr, q_stride, out_ptr, out_stride, lse_ptr, scale, stream):
+    status = _quick.oxy_prefix_attention(pool, batch, layer, q_ptr, q_stride, out_ptr, out_stride, lse_ptr, scale, stream)
+    if status is None:
+        status = lib().oxy_prefix_attention(pool, batch, layer, q_ptr or None, q_stride, out_ptr or None, out_stride,
+                                            lse_ptr or None, ctypes.c_float(scale), stream or None)
+    if status:
+        _check(status)
+
+
+def oxy_prompt_batch_build(pool, prompts, stream):
+    """prompts: (n_tokens, n_full) each."""
+    arr = (Prompt * len(prompts))(*[Prompt(int(n), int(f)) for n, f in prompts])
+    out = ctypes.c_void_p()
+    _check(lib().oxy_prompt_batch_build(pool, arr, len(prompts), stream or None, ctypes.byref(out)))
+    return out
+
+
+def oxy_prompt_attention(pool, batch, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride, lse_ptr,
+                         scale, stream):
+    status = _quick.oxy_prompt_attention(pool, batch, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride,
+                                         lse_ptr, scale, stream)
+    if status is None:
+        status = lib().oxy_prompt_attention(pool, batch, q_ptr or None, q_stride, k_ptr or None, k_stride, v_ptr or None,
+                                            v_stride, out_ptr or None, out_stride, lse_ptr or None,
+                                            ctypes.c_float(scale), stream or None)
+    if status:
+        _check(status)
+
+
 def _i64(values):
     """(array, address, length) of a sequence of integers."""
     # a list of Python ints, as oxy_batch_slots returns it, is converted natively: 1338 slots take
@@ -456,6 +520,37 @@ def oxy_rotary_append(pool, batch, layer, rotary, positions_ptr, q_ptr, q_stride
         status = lib().oxy_rotary_append(pool, batch, layer, ctypes.byref(rotary), positions_ptr or None,
                                          q_ptr or None, q_stride, q_out_ptr or None, k_ptr or None, k_stride,
                                          v_ptr or None, v_stride, stream or None)
+    if status:
+        _check(status)
+
+
+def make_rotary_axes(axis_of_pair, n_axes):
+    """axis_of_pair: the axis of each of rot_dims / 2 pairs, below n_axes."""
+    pairs = (ctypes.c_uint8 * max(len(axis_of_pair), MAX_ROTARY_PAIRS))(*axis_of_pair)
+    axes = RotaryAxisMap(n_axes, ctypes.addressof(pairs))
+    axes._keep = pairs
+    return axes
+
+
+def oxy_rotary_axes(rotary, axes, positions_ptr, x_ptr, x_stride, out_ptr, out_stride, n_tokens, n_heads, stream):
+    status = _quick.oxy_rotary_axes(ctypes.addressof(rotary), ctypes.addressof(axes), positions_ptr, x_ptr, x_stride,
+                                    out_ptr, out_stride, n_tokens, n_heads, stream)
+    if status is None:
+        status = lib().oxy_rotary_axes(ctypes.byref(rotary), ctypes.byref(axes), positions_ptr or None, x_ptr or None,
+                                       x_stride, out_ptr or None, out_stride, n_tokens, n_heads, stream or None)
+    if status:
+        _check(status)
+
+
+def oxy_rotary_axes_append(pool, batch, layer, rotary, axes, positions_ptr, q_ptr, q_stride, q_out_ptr, k_ptr, k_stride,
+                           v_ptr, v_stride, stream):
+    status = _quick.oxy_rotary_axes_append(pool, batch, layer, ctypes.addressof(rotary), ctypes.addressof(axes),
+                                           positions_ptr, q_ptr, q_stride, q_out_ptr, k_ptr, k_stride, v_ptr, v_stride,
+                                           stream)
+    if status is None:
+        status = lib().oxy_rotary_axes_append(pool, batch, layer, ctypes.byref(rotary), ctypes.byref(axes),
+                                              positions_ptr or None, q_ptr or None, q_stride, q_out_ptr or None,
+                                              k_ptr or None, k_stride, v_ptr or None, v_stride, stream or None)
     if status:
         _check(status)
 

@@ -8,7 +8,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboxy.so")
-SOURCES = ["oxy_kernels.hip", "oxy_kv8.hip", "oxy_rotary.hip", "oxy_pool.cpp", "oxy_sched.cpp"]
+SOURCES = ["oxy_kernels.hip", "oxy_kv8.hip", "oxy_rotary.hip", "oxy_prefill.hip", "oxy_pool.cpp", "oxy_sched.cpp"]
 # packed fp32 VALU forms are switched off for device code on purpose; the first eight arguments of a
 # kernel (at most 14 words, none from a struct on) are preloaded into scalar registers
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -2,6 +2,7 @@
 // (oxy_rotary.hip).  The launchers are weak: host code that is linked without these kernels refuses the calls that
 // need them.
 #pragma once
+#include "../../include/oxy.h"
 #include "oxy_internal.h"
 
 #define OXY_WEAK __attribute__((weak))
@@ -68,9 +69,29 @@ struct RotaryArgs {
   int32_t rot_dims;
   int32_t pairs;               // pairs (2i, 2i + 1), else (i, i + rot_dims / 2)
 };
+// Several axes: the position of token t on axis i is positions[i * n_tokens + t], pair i turns on axis
+// (of_pairs[i / 16] >> 2 (i % 16)) & 3.
+struct RotaryAxes {
+  int32_t n_axes;              // 1..4
+  uint32_t of_pairs[8];
+};
+// Null, or what is wrong with the map.
+inline const char* read_axes(const oxy_rotary_config* c, const oxy_rotary_axis_map* map, RotaryAxes* out) {
+  if (!c || !map || !map->axis_of_pair) return "null argument";
+  if (c->rot_dims < 2 || c->rot_dims > kDim || c->rot_dims % 2) return "rot_dims must be even, 2 to 256";
+  if (map->n_axes < 1 || map->n_axes > OXY_ROTARY_MAX_AXES) return "n_axes must be 1 to 4";
+  *out = {map->n_axes, {}};
+  for (int32_t i = 0; i < c->rot_dims / 2; ++i) {
+    const uint32_t axis = map->axis_of_pair[i];
+    if (axis >= (uint32_t)map->n_axes) return "a pair's axis is not below n_axes";
+    out->of_pairs[i / 16] |= axis << (2 * (i % 16));
+  }
+  return nullptr;
+}
 // Rows of n_tokens tokens, n_heads each: x + token * x_stride + head * 512 -> out + token * out_stride + head * 512.
-OXY_WEAK hipError_t launch_rotary(const RotaryArgs& r, const void* x, size_t x_stride, void* out, size_t out_stride,
-                                  int32_t n_tokens, int32_t n_heads, hipStream_t s);
+// axes: null, or those of several positions a token.
+OXY_WEAK hipError_t launch_rotary(const RotaryArgs& r, const RotaryAxes* axes, const void* x, size_t x_stride, void* out,
+                                  size_t out_stride, int32_t n_tokens, int32_t n_heads, hipStream_t s);
 struct RotaryAppendArgs {
   RotaryArgs rotary;
   const void* q;               // null: no queries
@@ -81,6 +102,7 @@ struct RotaryAppendArgs {
   void* layer_base;            // of a bf16 layer, or the blocks of one in 8 bits
   uint8_t* scales;             // null: bf16
   int32_t n_tokens;
+  const RotaryAxes* axes;      // HOST; null: one position a token
 };
 OXY_WEAK hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s);
 

@@ -6,6 +6,7 @@
 #include "../../include/oxy.h"
 #include "oxy_internal.h"
 #include "oxy_kv8.h"
+#include "oxy_prefill.h"
 
 #include <algorithm>
 #include <cstdarg>
@@ -41,6 +42,7 @@ struct Prefix {
   bool handle = true;  // creator's reference still held
   int32_t n_streams = 0;
   int32_t frozen = 0;  // tokens below this position are shared with a fork: read-only
+  uint64_t stamp = 0;  // last batch build that listed this prefix
 };
 
 struct Stream {
@@ -118,8 +120,12 @@ struct oxy_pool {
   int32_t graph_instantiations = 0, graph_updates = 0, graph_replays = 0;
 };
 
+// What a batch describes: a step of streams, new tokens of prefixes, or whole prompts.
+enum BatchKind { BATCH_STEP, BATCH_PREFIX, BATCH_PROMPT };
+
 struct oxy_batch {
   oxy_pool* pool = nullptr;
+  BatchKind kind = BATCH_STEP;
   int32_t slot = -1;
   int32_t flags = 0;
   int32_t n_items = 0, n_tokens = 0, n_work = 0, n_partials = 0;
@@ -129,6 +135,8 @@ struct oxy_batch {
   int32_t max_parts = 0;  // most split results of a token
   int32_t n_long = 0;     // in 8 bits: tokens of more than kLongParts
   int32_t off_long = 0;
+  int32_t n_merge = 0;    // of a prefill: tokens with split results
+  int32_t off_merges = 0;
   bool decodes = false;           // some item has <= 2 new tokens
   bool append_foldable = false;   // every item has <= 2 new tokens or an empty own history
   // word offsets inside the descriptor
@@ -1229,6 +1237,7 @@ int32_t oxy_stream_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
                           const void* v_new, void* hip_stream) {
   if (!p || !b || b->pool != p || !k_new || !v_new || p->host_only)
     return fail(OXY_ERR_INVALID_ARG, "stream_append: null argument, foreign batch or host-only pool");
+  if (b->kind == BATCH_PROMPT) return fail(OXY_ERR_INVALID_ARG, "stream_append: whole prompts have no place in the cache");
   if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "stream_append: layer %d", layer);
   const int32_t* d_desc = (const int32_t*)p->slots[b->slot].d_base;
   hipError_t e = append_rows(p, layer, k_new, v_new, d_desc + b->off_slots, b->n_tokens, (hipStream_t)hip_stream);
@@ -1243,6 +1252,7 @@ int32_t oxy_mixed_attention(oxy_pool* p, const oxy_batch* b, int32_t layer, cons
   if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "mixed_attention: layer %d", layer);
   if (b->flags & OXY_BATCH_APPEND_ONLY)
     return fail(OXY_ERR_INVALID_ARG, "mixed_attention: batch was built append-only");
+  if (b->kind != BATCH_STEP) return fail(OXY_ERR_INVALID_ARG, "mixed_attention: the batch is a prefill's");
   hipError_t e = attention(p, attn_args(p, b, layer, q, out, lse, scale), (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_fail(e, "mixed_attention: launch");
   return OXY_OK;
@@ -1257,6 +1267,7 @@ int32_t oxy_mixed_attention_static(oxy_pool* p, const oxy_batch* b, int32_t laye
     return fail(OXY_ERR_INVALID_ARG, "mixed_attention_static: layer %d", layer);
   if (b->flags & OXY_BATCH_APPEND_ONLY)
     return fail(OXY_ERR_INVALID_ARG, "mixed_attention_static: batch was built append-only");
+  if (b->kind != BATCH_STEP) return fail(OXY_ERR_INVALID_ARG, "mixed_attention_static: the batch is a prefill's");
   if (b->n_partials > oxy::kStaticMaxPartials)
     return fail(OXY_ERR_WORKSPACE,
                 "mixed_attention_static: the batch has %d split results, the static buffer holds %d",
@@ -1468,6 +1479,7 @@ int32_t oxy_step_layers(oxy_pool* p, const oxy_batch* b, int32_t layer_begin, in
     return fail(OXY_ERR_INVALID_ARG, "step_layers: layers [%d, %d)", layer_begin, layer_end);
   if (b->flags & OXY_BATCH_APPEND_ONLY)
     return fail(OXY_ERR_INVALID_ARG, "step_layers: batch was built append-only");
+  if (b->kind != BATCH_STEP) return fail(OXY_ERR_INVALID_ARG, "step_layers: the batch is a prefill's");
   if ((flags & OXY_STEP_GRAPH) && events)
     return fail(OXY_ERR_INVALID_ARG, "step_layers: timing events cannot go into a recorded step");
   StepCall c;
@@ -1599,11 +1611,13 @@ int32_t oxy_gather_kv_layers(oxy_pool* p, int32_t layer_begin, int32_t layer_end
 }
 
 // ---- rotary positions ------------------------------------------------------------------
-int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const oxy_rotary_config* c,
-                          const int32_t* positions, const void* q, size_t q_stride, void* q_out, const void* k_new,
-                          size_t k_stride, const void* v_new, size_t v_stride, void* hip_stream) {
+namespace {
+int32_t rotary_append_impl(oxy_pool* p, const oxy_batch* b, int32_t layer, const oxy_rotary_config* c, const oxy::RotaryAxes* axes,
+                           const int32_t* positions, const void* q, size_t q_stride, void* q_out, const void* k_new,
+                           size_t k_stride, const void* v_new, size_t v_stride, void* hip_stream) {
   if (!p || !b || b->pool != p || !c || !c->freqs || !positions || !k_new || !v_new || (q && !q_out) || p->host_only)
     return fail(OXY_ERR_INVALID_ARG, "rotary_append: null argument, foreign batch or host-only pool");
+  if (b->kind == BATCH_PROMPT) return fail(OXY_ERR_INVALID_ARG, "rotary_append: whole prompts have no place in the cache");
   if (!oxy::launch_rotary_append) return fail(OXY_ERR_INVALID_ARG, "rotary_append: this build has no kernels for it");
   if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "rotary_append: layer %d", layer);
   if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2)
@@ -1634,9 +1648,364 @@ int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const 
   a.layer_base = layer_base(p, layer);
   a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
   a.n_tokens = b->n_tokens;
+  a.axes = axes;
   hipError_t e = oxy::launch_rotary_append(a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_fail(e, "rotary_append: launch");
   return OXY_OK;
+}
+}  // namespace
+
+int32_t oxy_rotary_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const oxy_rotary_config* c,
+                          const int32_t* positions, const void* q, size_t q_stride, void* q_out, const void* k_new,
+                          size_t k_stride, const void* v_new, size_t v_stride, void* hip_stream) {
+  return rotary_append_impl(p, b, layer, c, nullptr, positions, q, q_stride, q_out, k_new, k_stride, v_new, v_stride, hip_stream);
+}
+
+int32_t oxy_rotary_axes_append(oxy_pool* p, const oxy_batch* b, int32_t layer, const oxy_rotary_config* c,
+                               const oxy_rotary_axis_map* map, const int32_t* positions, const void* q, size_t q_stride,
+                               void* q_out, const void* k_new, size_t k_stride, const void* v_new, size_t v_stride,
+                               void* hip_stream) {
+  oxy::RotaryAxes axes;
+  if (const char* why = oxy::read_axes(c, map, &axes)) return fail(OXY_ERR_INVALID_ARG, "rotary_axes_append: %s", why);
+  return rotary_append_impl(p, b, layer, c, &axes, positions, q, q_stride, q_out, k_new, k_stride, v_new, v_stride, hip_stream);
+}
+
+// ---- prefill ----------------------------------------------------------------------------
+namespace {
+
+// New tokens of a prefix, or a whole prompt, in a prefill's batch.
+struct PrefillItem {
+  int32_t tok0, past, n_new, full, len;
+  int32_t src;   // F_SRC of its records
+};
+
+// Work list of a prefill: records in `work`, tokens with split results in `merges`; returns how many split results there are.
+//
+// A record is up to 16 query tokens of an item and a part of the keys that they see.  kSlots workgroups are resident, two on each of 256 CUs.
+int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
+                     std::vector<int32_t>* merges) {
+  constexpr int32_t kSlots = 512, kStepKeys = 32, kLeastSteps = 4;
+  struct Tile {
+    const PrefillItem* it;
+    int32_t first, n, keys, parts;   // tokens of the item, keys that the last of them sees
+  };
+  std::vector<Tile> tiles;
+  int64_t steps = 0;
+  for (const PrefillItem& it : items)
+    for (int32_t t = 0; t < it.n_new; t += oxy::kPrefillTokens) {
+      const int32_t n = std::min(oxy::kPrefillTokens, it.n_new - t);
+      const int32_t keys = std::min(it.len, std::max(it.past + t + n, it.full));
+      tiles.push_back({&it, t, n, keys, 1});
+      steps += (keys + kStepKeys - 1) / kStepKeys;
+    }
+  int64_t partials = 0;
+  for (int64_t most = std::max<int64_t>(kLeastSteps, (steps + kSlots - 1) / kSlots);; most *= 2) {
+    int64_t records = 0;
+    bool split = false;
+    partials = 0;
+    for (Tile& t : tiles) {
+      const int32_t n = (t.keys + kStepKeys - 1) / kStepKeys;
+      t.parts = (int32_t)((n + most - 1) / most);
+      records += t.parts;
+      if (t.parts > 1) partials += (int64_t)t.parts * t.n, split = true;
+    }
+    if (!split || (records <= c.max_work_items && partials <= c.max_partials)) break;
+  }
+  struct Order {
+    int32_t steps, tile, part;
+  };
+  std::vector<Order> order;
+  for (size_t i = 0; i < tiles.size(); ++i)
+    for (int32_t k = 0; k < tiles[i].parts; ++k)
+      order.push_back({(tiles[i].keys + kStepKeys - 1) / kStepKeys / tiles[i].parts, (int32_t)i, k});
+  // the longest first: what a launch ends with is short
+  std::stable_sort(order.begin(), order.end(), [](const Order& x, const Order& y) { return x.steps > y.steps; });
+  std::vector<int32_t> part0(tiles.size(), -1);
+  int32_t next = 0;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const Tile& t = tiles[i];
+    if (t.parts == 1) continue;
+    part0[i] = next;
+    for (int32_t k = 0; k < t.n; ++k) {
+      const int32_t m[oxy::kMergeWords] = {t.it->tok0 + t.first + k, next, t.parts};
+      merges->insert(merges->end(), m, m + oxy::kMergeWords);
+      next += t.parts;
+    }
+  }
+  for (const Order& o : order) {
+    const Tile& t = tiles[o.tile];
+    const int64_t n = (t.keys + kStepKeys - 1) / kStepKeys;
+    const int32_t begin = (int32_t)(n * o.part / t.parts) * kStepKeys;
+    const int32_t end = std::min(t.keys, (int32_t)(n * (o.part + 1) / t.parts) * kStepKeys);
+    int32_t w[oxy::kPrefillWords] = {};
+    w[oxy::F_TOK0] = t.it->tok0 + t.first;
+    w[oxy::F_N_TOK] = t.n;
+    w[oxy::F_POS] = t.it->past + t.first;
+    w[oxy::F_FULL] = t.it->full;
+    w[oxy::F_BEGIN] = begin;
+    w[oxy::F_END] = end;
+    w[oxy::F_SRC] = t.it->src;
+    w[oxy::F_PART] = t.parts > 1 ? part0[o.tile] + o.part : -1;
+    w[oxy::F_N_PARTS] = t.parts;
+    w[oxy::F_LEN] = t.it->len;
+    work->insert(work->end(), w, w + oxy::kPrefillWords);
+  }
+  return partials;
+}
+
+// A batch of a prefill on a free descriptor slot: work list | slots | merges | tables, uploaded.
+struct PrefillDesc {
+  std::vector<int32_t> work, slots, merges, tables;
+  int64_t n_partials = 0;
+};
+int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_items, int32_t n_tokens, PrefillDesc& d,
+                      void* hip_stream, const char* who, oxy_batch** out) {
+  int32_t slot = -1;
+  for (int32_t i = 0; i < (int32_t)p->slots.size() && slot < 0; ++i)
+    if (!p->slots[i].in_use) slot = i;
+  if (slot < 0) return fail(OXY_ERR_BUSY, "%s: %d batches alive (max_live_batches)", who, p->live_batches);
+  const int64_t n_work = (int64_t)d.work.size() / oxy::kPrefillWords;
+  if (n_work > p->cfg.max_work_items || d.n_partials > p->cfg.max_partials)
+    return fail(OXY_ERR_WORKSPACE, "%s: %lld work items (max_work_items %d), %lld split results (max_partials %d)", who,
+                (long long)n_work, p->cfg.max_work_items, (long long)d.n_partials, p->cfg.max_partials);
+  if (d.tables.size() > table_words_of(p->cfg))
+    return fail(OXY_ERR_WORKSPACE, "%s: the block tables list %zu entries > %zu (forked prefixes list shared blocks once each)",
+                who, d.tables.size(), table_words_of(p->cfg));
+  oxy_batch* b = new oxy_batch();
+  b->pool = p;
+  b->kind = kind;
+  b->slot = slot;
+  b->flags = flags;
+  b->n_items = n_items;
+  b->n_tokens = n_tokens;
+  b->n_work = b->n_launch = (int32_t)n_work;
+  b->n_partials = (int32_t)d.n_partials;
+  b->n_merge = (int32_t)(d.merges.size() / oxy::kMergeWords);
+  b->off_slots = (int32_t)d.work.size();
+  b->off_merges = b->off_slots + (int32_t)d.slots.size();
+  b->off_tables = b->off_merges + (int32_t)d.merges.size();
+  try {
+    b->host = std::move(d.work);
+    for (const std::vector<int32_t>* x : {&d.slots, &d.merges, &d.tables}) b->host.insert(b->host.end(), x->begin(), x->end());
+  } catch (...) {
+    delete b;
+    throw;
+  }
+  if (b->host.size() > p->desc_words) {   // cannot happen: every section was bounded above
+    delete b;
+    return fail(OXY_ERR_WORKSPACE, "%s: descriptor overflow (internal)", who);
+  }
+  DescSlot& ds = p->slots[slot];
+  if (!p->host_only && !b->host.empty()) {
+    if (ds.event_pending) {
+      (void)hipEventSynchronize(ds.uploaded);
+      ds.event_pending = false;
+    }
+    memcpy(ds.staging, b->host.data(), b->host.size() * 4);
+    const hipError_t e = oxy::launch_upload(ds.staging, (int32_t*)ds.d_base, (int32_t)b->host.size(),
+                                            (hipStream_t)hip_stream, ds.uploaded);
+    if (e != hipSuccess) {
+      delete b;
+      return hip_fail(e, who);
+    }
+    ds.event_pending = true;
+  }
+  ds.in_use = true;
+  p->live_batches++;
+  *out = b;
+  return OXY_OK;
+}
+
+int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_items, int32_t flags, void* hip_stream,
+                          oxy_batch** out) {
+  const oxy_pool_config& c = p->cfg;
+  const bool append_only = (flags & OXY_BATCH_APPEND_ONLY) != 0;
+  struct Plan {
+    Prefix* px;
+    int32_t n_new, full, old_len, need;
+  };
+  std::vector<Plan> plan;
+  plan.reserve(n_items);
+  const uint64_t stamp = ++p->build_seq;
+  int64_t need_total = 0, n_tokens = 0;
+  for (int32_t i = 0; i < n_items; ++i) {
+    const oxy_prefix_item& it = items[i];
+    auto at = p->prefixes.find(it.prefix_id);
+    if (at == p->prefixes.end() || !at->second.handle)
+      return fail(OXY_ERR_BAD_ID, "prefix_batch_build: no prefix %d", it.prefix_id);
+    Prefix& px = at->second;
+    if (it.n_new < 1 || it.n_full < 0 || px.stamp == stamp)
+      return fail(OXY_ERR_INVALID_ARG, "prefix_batch_build: item %d: n_new %d, n_full %d or duplicate prefix", i, it.n_new,
+                  it.n_full);
+    px.stamp = stamp;
+    if (px.sealed) return fail(OXY_ERR_SEALED, "prefix_batch_build: prefix %d has streams attached", it.prefix_id);
+    if ((int64_t)px.len + it.n_new > (int64_t)kPage * c.num_blocks)
+      return fail(OXY_ERR_NO_BLOCKS, "prefix_batch_build: prefix %d would exceed the pool", it.prefix_id);
+    const int32_t need = std::max(0, blocks_for(px.len + it.n_new) - (int32_t)px.blocks.size());
+    plan.push_back({&px, it.n_new, it.n_full, px.len, need});
+    need_total += need;
+    n_tokens += it.n_new;
+  }
+  if (need_total > (int64_t)p->free_stack.size())
+    return fail(OXY_ERR_NO_BLOCKS, "prefix_batch_build: need %lld blocks, %zu free", (long long)need_total,
+                p->free_stack.size());
+  if (n_tokens > c.max_append_tokens || (!append_only && n_tokens > c.max_q_tokens))
+    return fail(OXY_ERR_WORKSPACE, "prefix_batch_build: %lld new tokens (max_append_tokens %d, max_q_tokens %d)",
+                (long long)n_tokens, c.max_append_tokens, c.max_q_tokens);
+  PrefillDesc d;
+  std::vector<PrefillItem> work;
+  int32_t tok0 = 0, words = 0;
+  for (const Plan& pl : plan) {
+    const int32_t len = pl.old_len + pl.n_new;
+    work.push_back({tok0, pl.old_len, pl.n_new, std::min(pl.full, len), len, words});
+    tok0 += pl.n_new;
+    words += blocks_for(len);
+  }
+  if (!append_only) d.n_partials = plan_prefill(c, work, &d.work, &d.merges);
+  d.slots.reserve(n_tokens);
+  // blocks are taken in item order; what fails from here on gives them back in reverse order of their pops
+  size_t done = 0;
+  auto roll_back = [&]() {
+    while (done > 0) {
+      Plan& pl = plan[--done];
+      for (; pl.need > 0; --pl.need) {
+        p->ref[pl.px->blocks.back()] = 0;
+        p->free_stack.push_back(pl.px->blocks.back());
+        pl.px->blocks.pop_back();
+      }
+      pl.px->len = pl.old_len;
+    }
+  };
+  int32_t status;
+  try {
+    for (Plan& pl : plan) pl.px->blocks.reserve(pl.px->blocks.size() + pl.need);
+    for (Plan& pl : plan) {
+      for (int32_t i = 0; i < pl.need; ++i) {
+        const int32_t blk = p->free_stack.back();
+        p->free_stack.pop_back();
+        p->ref[blk] = 1;
+        pl.px->blocks.push_back(blk);
+      }
+      pl.px->len = pl.old_len + pl.n_new;
+      ++done;
+      for (int32_t t = pl.old_len; t < pl.px->len; ++t) d.slots.push_back(pl.px->blocks[t / kPage] * kPage + t % kPage);
+      if (!append_only)
+        d.tables.insert(d.tables.end(), pl.px->blocks.begin(), pl.px->blocks.begin() + blocks_for(pl.px->len));
+    }
+    status = prefill_batch(p, BATCH_PREFIX, flags, n_items, (int32_t)n_tokens, d, hip_stream, "prefix_batch_build", out);
+  } catch (...) {
+    roll_back();
+    throw;
+  }
+  if (status != OXY_OK) roll_back();
+  return status;
+}
+
+int32_t prompt_batch_impl(oxy_pool* p, const oxy_prompt* prompts, int32_t n_prompts, void* hip_stream, oxy_batch** out) {
+  PrefillDesc d;
+  std::vector<PrefillItem> work;
+  int64_t n_tokens = 0;
+  for (int32_t i = 0; i < n_prompts; ++i) {
+    const oxy_prompt& it = prompts[i];
+    if (it.n_tokens < 0 || it.n_full < 0)
+      return fail(OXY_ERR_INVALID_ARG, "prompt_batch_build: prompt %d: n_tokens %d, n_full %d", i, it.n_tokens, it.n_full);
+    if (n_tokens + it.n_tokens > p->cfg.max_q_tokens)
+      return fail(OXY_ERR_WORKSPACE, "prompt_batch_build: more than max_q_tokens %d tokens", p->cfg.max_q_tokens);
+    const int32_t at = (int32_t)n_tokens;
+    work.push_back({at, 0, it.n_tokens, std::min(it.n_full, it.n_tokens), it.n_tokens, at});
+    n_tokens += it.n_tokens;
+  }
+  d.n_partials = plan_prefill(p->cfg, work, &d.work, &d.merges);
+  return prefill_batch(p, BATCH_PROMPT, 0, n_prompts, (int32_t)n_tokens, d, hip_stream, "prompt_batch_build", out);
+}
+
+oxy::PrefillArgs prefill_args(const oxy_pool* p, const oxy_batch* b, const void* q, size_t q_stride, void* out,
+                              size_t out_stride, float* lse, float scale) {
+  const DescSlot& ds = p->slots[b->slot];
+  const int32_t* d = (const int32_t*)ds.d_base;
+  oxy::PrefillArgs a = {};
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.work = d;
+  a.tables = d + b->off_tables;
+  a.merges = d + b->off_merges;
+  a.part_acc = (uint16_t*)(ds.d_base + p->acc_offset);
+  a.part_ml = (float*)(ds.d_base + p->ml_offset);
+  a.n_work = b->n_launch;
+  a.n_merge = b->n_merge;
+  a.scale = scale;
+  return a;
+}
+// Rows of a token side by side: `rows` of 512 bytes at `at`, the next token's `stride` bytes on.
+bool bad_rows(const void* at, size_t stride, int32_t rows, int32_t n_tokens) {
+  return ((uintptr_t)at | stride) & 15 || (n_tokens > 1 && stride < (size_t)rows * oxy::kDim * 2);
+}
+}  // namespace
+
+int32_t oxy_prefix_batch_build(oxy_pool* p, const oxy_prefix_item* items, int32_t n_items, int32_t flags, void* hip_stream,
+                               oxy_batch** out) {
+  if (!p || !items || !out || n_items < 1)
+    return fail(OXY_ERR_INVALID_ARG, "prefix_batch_build: null argument or no items");
+  *out = nullptr;
+  if (flags & ~OXY_BATCH_APPEND_ONLY) return fail(OXY_ERR_INVALID_ARG, "prefix_batch_build: flags");
+  try {
+    return prefix_batch_impl(p, items, n_items, flags, hip_stream, out);
+  } catch (const std::bad_alloc&) {
+    return fail(OXY_ERR_INVALID_ARG, "prefix_batch_build: out of host memory");
+  }
+}
+
+int32_t oxy_prompt_batch_build(oxy_pool* p, const oxy_prompt* prompts, int32_t n_prompts, void* hip_stream, oxy_batch** out) {
+  if (!p || !prompts || !out || n_prompts < 1)
+    return fail(OXY_ERR_INVALID_ARG, "prompt_batch_build: null argument or no prompts");
+  *out = nullptr;
+  try {
+    return prompt_batch_impl(p, prompts, n_prompts, hip_stream, out);
+  } catch (const std::bad_alloc&) {
+    return fail(OXY_ERR_INVALID_ARG, "prompt_batch_build: out of host memory");
+  }
+}
+
+int32_t oxy_prefix_attention(oxy_pool* p, const oxy_batch* b, int32_t layer, const void* q, size_t q_stride, void* out,
+                             size_t out_stride, float* lse, float scale, void* hip_stream) {
+  if (!p || !b || b->pool != p || !q || !out || p->host_only)
+    return fail(OXY_ERR_INVALID_ARG, "prefix_attention: null argument, foreign batch or host-only pool");
+  if (b->kind != BATCH_PREFIX) return fail(OXY_ERR_INVALID_ARG, "prefix_attention: not a batch of oxy_prefix_batch_build");
+  if (!oxy::launch_prefill) return fail(OXY_ERR_INVALID_ARG, "prefix_attention: this build has no kernels for it");
+  if (layer < 0 || layer >= p->cfg.n_layers) return fail(OXY_ERR_INVALID_ARG, "prefix_attention: layer %d", layer);
+  if (b->flags & OXY_BATCH_APPEND_ONLY)
+    return fail(OXY_ERR_INVALID_ARG, "prefix_attention: batch was built append-only");
+  if (bad_rows(q, q_stride, oxy::kHeads, b->n_tokens) || bad_rows(out, out_stride, oxy::kHeads, b->n_tokens))
+    return fail(OXY_ERR_INVALID_ARG, "prefix_attention: rows must be 16-byte aligned, strides at least a token's rows");
+  oxy::PrefillArgs a = prefill_args(p, b, q, q_stride, out, out_stride, lse, scale);
+  a.layer_base = layer_base(p, layer);
+  a.scales = p->kv8 ? layer8(p, layer).scales : nullptr;
+  const hipError_t e = oxy::launch_prefill(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? OXY_OK : hip_fail(e, "prefix_attention: launch");
+}
+
+int32_t oxy_prompt_attention(oxy_pool* p, const oxy_batch* b, const void* q, size_t q_stride, const void* k, size_t k_stride,
+                             const void* v, size_t v_stride, void* out, size_t out_stride, float* lse, float scale,
+                             void* hip_stream) {
+  if (!p || !b || b->pool != p || p->host_only)
+    return fail(OXY_ERR_INVALID_ARG, "prompt_attention: null argument, foreign batch or host-only pool");
+  if (b->kind != BATCH_PROMPT) return fail(OXY_ERR_INVALID_ARG, "prompt_attention: not a batch of oxy_prompt_batch_build");
+  if (!oxy::launch_prefill) return fail(OXY_ERR_INVALID_ARG, "prompt_attention: this build has no kernels for it");
+  if (b->n_tokens == 0) return OXY_OK;   // what holds no rows may lie anywhere
+  if (!q || !k || !v || !out) return fail(OXY_ERR_INVALID_ARG, "prompt_attention: null argument");
+  if (bad_rows(q, q_stride, oxy::kHeads, b->n_tokens) || bad_rows(out, out_stride, oxy::kHeads, b->n_tokens) ||
+      bad_rows(k, k_stride, 1, b->n_tokens) || bad_rows(v, v_stride, 1, b->n_tokens))
+    return fail(OXY_ERR_INVALID_ARG, "prompt_attention: rows must be 16-byte aligned, strides at least a token's rows");
+  oxy::PrefillArgs a = prefill_args(p, b, q, q_stride, out, out_stride, lse, scale);
+  a.k = (const char*)k;
+  a.v = (const char*)v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  const hipError_t e = oxy::launch_prefill(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? OXY_OK : hip_fail(e, "prompt_attention: launch");
 }
 
 // ---- introspection ------------------------------------------------------------------------
@@ -1715,12 +2084,14 @@ int32_t oxy_batch_info(const oxy_batch* b, int32_t* n_items, int32_t* n_tokens, 
 
 int32_t oxy_batch_slots(const oxy_batch* b, int64_t* out, int32_t cap) {
   if (!b || !out || cap < b->n_tokens) return fail(OXY_ERR_INVALID_ARG, "batch_slots: cap");
+  if (b->kind == BATCH_PROMPT) return fail(OXY_ERR_INVALID_ARG, "batch_slots: whole prompts have no place in the cache");
   for (int32_t i = 0; i < b->n_tokens; ++i) out[i] = b->host[b->off_slots + i];
   return OXY_OK;
 }
 
 int32_t oxy_batch_work(const oxy_batch* b, int32_t* out, int32_t cap_items) {
   if (!b || !out || cap_items < b->n_work) return fail(OXY_ERR_INVALID_ARG, "batch_work: cap");
+  if (b->kind != BATCH_STEP) return fail(OXY_ERR_INVALID_ARG, "batch_work: the batch is a prefill's");
   size_t shared = 0, second = 0;
   for (int32_t i = 0, rec = 0; i < b->n_work; ++rec) {   // the eight header words of each record
     if (second < b->second_records.size() && b->second_records[second] == rec) {
@@ -1739,6 +2110,7 @@ int32_t oxy_batch_work(const oxy_batch* b, int32_t* out, int32_t cap_items) {
 
 int32_t oxy_batch_records(const oxy_batch* b, int32_t* out, int32_t cap_records, int32_t* n_records) {
   if (!b || !n_records) return fail(OXY_ERR_INVALID_ARG, "batch_records: null argument");
+  if (b->kind != BATCH_STEP) return fail(OXY_ERR_INVALID_ARG, "batch_records: the batch is a prefill's");
   *n_records = b->n_launch;
   if (!out && cap_records == 0) return OXY_OK;
   if (!out || cap_records < b->n_launch) return fail(OXY_ERR_INVALID_ARG, "batch_records: cap");

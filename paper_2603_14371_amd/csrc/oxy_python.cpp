@@ -171,6 +171,7 @@ PyObject* call_gather_layers(PyObject* self, PyObject* const* args, Py_ssize_t n
 #define OXY_METHOD(name) OXY_CALL(name, call<decltype(&name)>)
 PyMethodDef g_calls[] = {OXY_METHOD(oxy_mixed_attention), OXY_METHOD(oxy_mixed_attention_static), OXY_METHOD(oxy_stream_append),
                          OXY_METHOD(oxy_append_attention), OXY_METHOD(oxy_rotary_append), OXY_METHOD(oxy_rotary),
+                         OXY_METHOD(oxy_rotary_axes), OXY_METHOD(oxy_rotary_axes_append), OXY_METHOD(oxy_prefix_attention), OXY_METHOD(oxy_prompt_attention),
                          OXY_CALL(oxy_batch_info, call_info), OXY_CALL(oxy_batch_slots, call_slots),
                          OXY_CALL(oxy_gather_kv, call_gather), OXY_CALL(oxy_gather_kv_layers, call_gather_layers),
                          {nullptr, nullptr, 0, nullptr}};

@@ -14,12 +14,17 @@
 
 #include <cmath>
 #include <cstdio>
+#include <string>
 
 extern "C" __attribute__((visibility("hidden"))) void oxy_internal_set_error(const char* msg);
 
 namespace oxy {
 
 constexpr int kMaxPairs = kDim / 2;
+
+__device__ __forceinline__ int axis_of(const RotaryAxes& axes, const int pair) {
+  return (axes.of_pairs[pair >> 4] >> (2 * (pair & 15))) & 3;
+}
 
 // How a lane finds its dims' partners: pairs lie side by side; halves a whole number of 16-byte chunks apart; or not.
 enum RotaryForm { FORM_PAIRS, FORM_HALVES, FORM_HALVES_ANY };
@@ -143,10 +148,11 @@ __device__ __forceinline__ u32x4 turned(RowLoad x, const LaneTurns& w, const int
 // With four, two half wavefronts share a token's heads; with one, all eight do.  A half wavefront keeps its cosines and
 // sines, and kRows rows in flight.  Nine heads of 8192 tokens (75 MB) 18.0 us in halves, 17.0 in pairs: 4.2 and 4.4 TB/s;
 // in halves that are not whole chunks, whose partners are loaded one by one, 29; of 64 tokens 2.6 us.
-template <int kForm, int kTokens>
+// Axes: nothing, or a RotaryAxes: each pair is then turned by its own axis' position.
+template <int kForm, int kTokens, class... Axes>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const char* x, const size_t x_stride, char* out,
                                                      const size_t out_stride, const int32_t n_tokens,
-                                                     const int32_t n_heads) {
+                                                     const int32_t n_heads, const Axes... axes) {
   constexpr int kStep = 8 / kTokens;   // half wavefronts of a token
   constexpr int kRows = kForm == FORM_HALVES_ANY ? 1 : kTokens == 1 ? 2 : 3;   // of each at a time
   __shared__ __align__(16) float cs[kTokens][kMaxPairs], sn[kTokens][kMaxPairs];
@@ -164,7 +170,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs r, const c
   load(head0);   // on their way while the angles are taken
   for (int k = t; k < here * half; k += 256) {
     const int at = k / half, pair = k - at * half;
-    turn_of(r.freqs[pair], r.amplitude, r.positions[tok0 + at], cs[at][pair], sn[at][pair]);
+    const int32_t* positions = r.positions + tok0 + at;
+    if constexpr (sizeof...(Axes) > 0) positions += ((size_t)(axis_of(axes, pair) * n_tokens) + ...);
+    turn_of(r.freqs[pair], r.amplitude, *positions, cs[at][pair], sn[at][pair]);
   }
   __syncthreads();
   const LaneTurns w = turns_of_lane<kForm>(cs[tok], sn[tok], r.rot_dims, c);
@@ -194,11 +202,11 @@ struct RotaryLate {
 // One token per workgroup: ten half wavefronts take its eight query rows, its key and its value (58 tokens 2.8
 // us a launch: the chain position - angle - LDS - row).  The addresses of the
 // first loads are preloaded into scalar registers (see build.py).
-template <int kForm, bool kBits8>
+template <int kForm, bool kBits8, class... Axes>
 __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* positions, const char* q, const char* k_new,
                                                             const char* v_new, const uint32_t q_stride,
                                                             const uint32_t k_stride, const uint32_t v_stride,
-                                                            const int32_t rot, const RotaryLate a) {
+                                                            const int32_t rot, const RotaryLate a, const Axes... axes) {
   __shared__ __align__(16) float cs[kMaxPairs], sn[kMaxPairs];
   const int t = threadIdx.x, c = t & 31, row = t >> 5;
   const size_t tok = blockIdx.x;
@@ -206,7 +214,11 @@ __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* posit
   const char* src = is_q ? q + tok * q_stride + row * (kDim * 2) : is_v ? v_new + tok * v_stride : k_new + tok * k_stride;
   RowLoad x = {};
   const bool live = !is_q || q;
-  const int32_t position = ((DescPtr)positions)[tok];
+  // a token's positions on all axes come by scalar loads, and its pairs choose among them
+  int32_t on_axis[4] = {((DescPtr)positions)[tok]};
+  if constexpr (sizeof...(Axes) > 0)
+#pragma unroll
+    for (int i = 1; i < 4; ++i) on_axis[i] = ((DescPtr)positions)[tok + (((size_t)min(i, axes.n_axes - 1) * gridDim.x) + ...)];
   if (live) {
     if (is_v)
       x.own = *(const u32x4*)((const uint16_t*)src + 8 * c);
@@ -214,7 +226,14 @@ __global__ __launch_bounds__(320) void rotary_append_kernel(const int32_t* posit
       x = load_turning<kForm, true>((const uint16_t*)src, rot, c);
   }
   const int32_t slot = ((DescPtr)a.d_slots)[tok];
-  if (t < rot >> 1) turn_of(a.freqs[t], a.amplitude, position, cs[t], sn[t]);
+  if (t < rot >> 1) {
+    int32_t position = on_axis[0];
+    if constexpr (sizeof...(Axes) > 0) {
+      const int axis = (axis_of(axes, t) + ...);
+      position = axis & 2 ? (axis & 1 ? on_axis[3] : on_axis[2]) : axis ? on_axis[1] : on_axis[0];
+    }
+    turn_of(a.freqs[t], a.amplitude, position, cs[t], sn[t]);
+  }
   __syncthreads();
   u32x4 y = x.own;
   if (!is_v) y = turned<kForm, true>(x, turns_of_lane<kForm>(cs, sn, rot, c), rot, c);
@@ -252,44 +271,54 @@ constexpr int kManyTokens = 2049;
 int form_of(const RotaryArgs& r) {
   return r.pairs ? FORM_PAIRS : (r.rot_dims >> 1) % 8 == 0 ? FORM_HALVES : FORM_HALVES_ANY;
 }
-template <int kForm>
-void launch_append_form(const RotaryAppendArgs& a, hipStream_t s) {
+template <int kForm, class... Axes>
+void launch_append_form(const RotaryAppendArgs& a, hipStream_t s, const Axes&... axes) {
   const RotaryLate late = {a.rotary.freqs, a.d_slots, a.q_out, a.layer_base, a.scales, a.rotary.amplitude};
   const auto launch = [&](auto kernel) {
     kernel<<<a.n_tokens, 320, 0, s>>>(a.rotary.positions, (const char*)a.q, (const char*)a.k_new, (const char*)a.v_new,
-                                      a.q_stride, a.k_stride, a.v_stride, a.rotary.rot_dims, late);
+                                      a.q_stride, a.k_stride, a.v_stride, a.rotary.rot_dims, late, axes...);
   };
   if (a.scales)
-    launch(rotary_append_kernel<kForm, true>);
+    launch(rotary_append_kernel<kForm, true, Axes...>);
   else
-    launch(rotary_append_kernel<kForm, false>);
+    launch(rotary_append_kernel<kForm, false, Axes...>);
 }
-}  // namespace
-
-hipError_t launch_rotary(const RotaryArgs& r, const void* x, size_t x_stride, void* out, size_t out_stride,
-                         int32_t n_tokens, int32_t n_heads, hipStream_t s) {
+template <class... Axes>
+hipError_t launch_append_any(const RotaryAppendArgs& a, hipStream_t s, const Axes&... axes) {
+  if (a.n_tokens <= 0) return hipSuccess;
+  switch (form_of(a.rotary)) {
+    case FORM_PAIRS: launch_append_form<FORM_PAIRS>(a, s, axes...); break;
+    case FORM_HALVES: launch_append_form<FORM_HALVES>(a, s, axes...); break;
+    default: launch_append_form<FORM_HALVES_ANY>(a, s, axes...);
+  }
+  return hipGetLastError();
+}
+template <class... Axes>
+hipError_t launch_any(const RotaryArgs& r, const void* x, size_t x_stride, void* out, size_t out_stride, int32_t n_tokens,
+                      int32_t n_heads, hipStream_t s, const Axes&... axes) {
   if (n_tokens <= 0) return hipSuccess;
   const bool many = n_tokens >= kManyTokens;
   const auto launch = [&](auto one, auto four) {
     const dim3 grid(many ? (n_tokens + 3) / 4 : n_tokens);
-    (many ? four : one)<<<grid, 256, 0, s>>>(r, (const char*)x, x_stride, (char*)out, out_stride, n_tokens, n_heads);
+    (many ? four : one)<<<grid, 256, 0, s>>>(r, (const char*)x, x_stride, (char*)out, out_stride, n_tokens, n_heads, axes...);
   };
   switch (form_of(r)) {
-    case FORM_PAIRS: launch(rotary_kernel<FORM_PAIRS, 1>, rotary_kernel<FORM_PAIRS, 4>); break;
-    case FORM_HALVES: launch(rotary_kernel<FORM_HALVES, 1>, rotary_kernel<FORM_HALVES, 4>); break;
-    default: launch(rotary_kernel<FORM_HALVES_ANY, 1>, rotary_kernel<FORM_HALVES_ANY, 4>);
+    case FORM_PAIRS: launch(rotary_kernel<FORM_PAIRS, 1, Axes...>, rotary_kernel<FORM_PAIRS, 4, Axes...>); break;
+    case FORM_HALVES: launch(rotary_kernel<FORM_HALVES, 1, Axes...>, rotary_kernel<FORM_HALVES, 4, Axes...>); break;
+    default: launch(rotary_kernel<FORM_HALVES_ANY, 1, Axes...>, rotary_kernel<FORM_HALVES_ANY, 4, Axes...>);
   }
   return hipGetLastError();
 }
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& r, const RotaryAxes* axes, const void* x, size_t x_stride, void* out,
+                         size_t out_stride, int32_t n_tokens, int32_t n_heads, hipStream_t s) {
+  return axes ? launch_any(r, x, x_stride, out, out_stride, n_tokens, n_heads, s, *axes)
+              : launch_any(r, x, x_stride, out, out_stride, n_tokens, n_heads, s);
+}
 
 hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s) {
-  if (a.n_tokens <= 0) return hipSuccess;
-  switch (form_of(a.rotary)) {
-    case FORM_PAIRS: launch_append_form<FORM_PAIRS>(a, s); break;
-    case FORM_HALVES: launch_append_form<FORM_HALVES>(a, s); break;
-    default: launch_append_form<FORM_HALVES_ANY>(a, s);
-  }
-  return hipGetLastError();
+  return a.axes ? launch_append_any(a, s, *a.axes) : launch_append_any(a, s);
 }
 
 }  // namespace oxy
@@ -298,6 +327,30 @@ namespace {
 int32_t refuse(const char* what) {
   oxy_internal_set_error(what);
   return OXY_ERR_INVALID_ARG;
+}
+
+int32_t rotary_impl(const oxy_rotary_config* c, const oxy::RotaryAxes* axes, const int32_t* positions, const void* x,
+                    size_t x_stride, void* out, size_t out_stride, int32_t n_tokens, int32_t n_heads, void* hip_stream) {
+  if (!c || !c->freqs || (n_tokens != 0 && (!positions || !x || !out))) return refuse("rotary: null argument");
+  if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2) return refuse("rotary: rot_dims must be even, 2 to 256");
+  if (c->layout != OXY_ROTARY_HALVES && c->layout != OXY_ROTARY_PAIRS) return refuse("rotary: unknown layout");
+  if (n_tokens < 0 || n_tokens > OXY_ROTARY_MAX_TOKENS || n_heads < 1 || n_heads > OXY_ROTARY_MAX_HEADS)
+    return refuse("rotary: n_tokens or n_heads");
+  if (n_tokens == 0) return OXY_OK;   // what holds no rows may lie anywhere
+  const size_t row = (size_t)n_heads * oxy::kDim * 2;
+  if (((uintptr_t)x | (uintptr_t)out | x_stride | out_stride) & 15) return refuse("rotary: rows must be 16-byte aligned");
+  if (n_tokens > 1 && (x_stride < row || out_stride < row)) return refuse("rotary: stride below n_heads rows");
+  if (n_tokens > 1 && x == out && x_stride != out_stride) return refuse("rotary: in place with two strides");
+  const oxy::RotaryArgs r = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};
+  const hipError_t e =
+      oxy::launch_rotary(r, axes, x, x_stride, out, out_stride, n_tokens, n_heads, (hipStream_t)hip_stream);
+  if (e != hipSuccess) {
+    char msg[160];
+    snprintf(msg, sizeof(msg), "rotary: launch: %s", hipGetErrorString(e));
+    oxy_internal_set_error(msg);
+    return OXY_ERR_DEVICE;
+  }
+  return OXY_OK;
 }
 }  // namespace
 
@@ -342,25 +395,17 @@ int32_t oxy_rotary_freqs(const oxy_rotary_scaling* sc, double* freqs, double* am
 
 int32_t oxy_rotary(const oxy_rotary_config* c, const int32_t* positions, const void* x, size_t x_stride, void* out,
                    size_t out_stride, int32_t n_tokens, int32_t n_heads, void* hip_stream) {
-  if (!c || !c->freqs || (n_tokens != 0 && (!positions || !x || !out))) return refuse("rotary: null argument");
-  if (c->rot_dims < 2 || c->rot_dims > oxy::kDim || c->rot_dims % 2) return refuse("rotary: rot_dims must be even, 2 to 256");
-  if (c->layout != OXY_ROTARY_HALVES && c->layout != OXY_ROTARY_PAIRS) return refuse("rotary: unknown layout");
-  if (n_tokens < 0 || n_tokens > OXY_ROTARY_MAX_TOKENS || n_heads < 1 || n_heads > OXY_ROTARY_MAX_HEADS)
-    return refuse("rotary: n_tokens or n_heads");
-  if (n_tokens == 0) return OXY_OK;   // what holds no rows may lie anywhere
-  const size_t row = (size_t)n_heads * oxy::kDim * 2;
-  if (((uintptr_t)x | (uintptr_t)out | x_stride | out_stride) & 15) return refuse("rotary: rows must be 16-byte aligned");
-  if (n_tokens > 1 && (x_stride < row || out_stride < row)) return refuse("rotary: stride below n_heads rows");
-  if (n_tokens > 1 && x == out && x_stride != out_stride) return refuse("rotary: in place with two strides");
-  const oxy::RotaryArgs r = {c->freqs, positions, c->amplitude, c->rot_dims, c->layout == OXY_ROTARY_PAIRS};
-  const hipError_t e = oxy::launch_rotary(r, x, x_stride, out, out_stride, n_tokens, n_heads, (hipStream_t)hip_stream);
-  if (e != hipSuccess) {
-    char msg[160];
-    snprintf(msg, sizeof(msg), "rotary: launch: %s", hipGetErrorString(e));
-    oxy_internal_set_error(msg);
-    return OXY_ERR_DEVICE;
+  return rotary_impl(c, nullptr, positions, x, x_stride, out, out_stride, n_tokens, n_heads, hip_stream);
+}
+
+int32_t oxy_rotary_axes(const oxy_rotary_config* c, const oxy_rotary_axis_map* map, const int32_t* positions, const void* x,
+                        size_t x_stride, void* out, size_t out_stride, int32_t n_tokens, int32_t n_heads, void* hip_stream) {
+  oxy::RotaryAxes axes;
+  if (const char* why = oxy::read_axes(c, map, &axes)) {
+    oxy_internal_set_error((std::string("rotary_axes: ") + why).c_str());
+    return OXY_ERR_INVALID_ARG;
   }
-  return OXY_OK;
+  return rotary_impl(c, &axes, positions, x, x_stride, out, out_stride, n_tokens, n_heads, hip_stream);
 }
 
 }  // extern "C"

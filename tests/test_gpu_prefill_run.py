@@ -1,0 +1,246 @@
+"""Operators of a prefill used together, as a program uses them: on other streams, recorded, repeated, and with rows that are
+not finite."""
+import numpy as np
+import pytest
+
+from oracle import prefill
+from oracle.attention import widen_bf16
+from prefill_util import HALF16, Pool, bits, check, down, held, up
+
+pytestmark = pytest.mark.gpu
+SCALE = 1.0 / 16
+FORMS = pytest.mark.parametrize("kv8", [False, True], ids=["bf16", "fp8"])
+
+
+def _positions(n, side, first):
+    """(time, height, width) of images of side x side tokens, then words."""
+    views = n * 3 // 4 // (side * side)
+    out = []
+    for t in range(n):
+        v, at = divmod(t, side * side)
+        out.append((first + v, first + at // side, first + at % side) if v < views
+                   else (first + side + t - views * side * side,) * 3)
+    return np.array(out, dtype=np.int32).T.copy()
+
+
+@FORMS
+def test_prefill_in_two_parts_then_decode(kv8):
+    """An observation's images, then its words behind them, layer by layer; then a request on the prefix.  The words' rows
+    and the request see what the first part stored."""
+    import torch
+    from paper_2603_14371_amd import binding as B
+    rng = np.random.default_rng(5)
+    sizes, L = (150, 37), 2
+    pool = Pool(L, 40, kv8, seed=3, max_q_tokens=256)
+    freqs = torch.from_numpy(B.oxy_rotary_freqs(10000.0, 256)[0]).cuda()
+    cfg = B.make_rotary(freqs.data_ptr(), 256)
+    axis = np.repeat([0, 1, 2], [32, 48, 48])
+    axes = B.make_rotary_axes(axis.tolist(), 3)
+    pid = B.oxy_prefix_create(pool.p)
+    keys, values = [[] for _ in range(L)], [[] for _ in range(L)]
+    past = 0
+    try:
+        for n in sizes:
+            full = 150
+            batch = B.oxy_prefix_batch_build(pool.p, [(pid, n, full)], 0, pool.stream)
+            pos = _positions(n, 6, past)
+            dpos = torch.from_numpy(pos).cuda()
+            for l in range(L):
+                x = bits(rng, n, 10, 256)
+                d = up(x)
+                q, out = (torch.zeros((n, 8, 256), dtype=torch.int16, device="cuda") for _ in range(2))
+                z = torch.zeros((n, 8), device="cuda")
+                a = d.data_ptr()
+                B.oxy_rotary_axes_append(pool.p, batch, l, cfg, axes, dpos.data_ptr(), a, 5120, q.data_ptr(), a + 4096, 5120,
+                                         a + 4608, 5120, pool.stream)
+                B.oxy_prefix_attention(pool.p, batch, l, q.data_ptr(), 4096, out.data_ptr(), 4096, z.data_ptr(), SCALE,
+                                       pool.stream)
+                ref = prefill.turned(widen_bf16(x[:, :8]), pos, axis, freqs.cpu().numpy(), "halves")
+                got_q = down(q)
+                assert np.all(np.abs(widen_bf16(got_q) - ref) <= HALF16 * np.abs(ref) + 2.0 ** -18)
+                turned = torch.zeros((n, 1, 256), dtype=torch.int16, device="cuda")
+                B.oxy_rotary_axes(cfg, axes, dpos.data_ptr(), a + 4096, 5120, turned.data_ptr(), 512, n, 1, pool.stream)
+                keys[l].append(down(turned)[:, 0])
+                values[l].append(x[:, 9])
+                check(down(out), z.cpu().numpy().astype(np.float64), got_q, held(np.concatenate(keys[l]), kv8),
+                      held(np.concatenate(values[l]), kv8), past, full, SCALE, "layer %d" % l)
+            B.oxy_batch_destroy(batch)
+            past += n
+        sid = B.oxy_stream_create(pool.p, pid, B.KIND_DECODE)
+        with pytest.raises(B.OxyError) as e:
+            B.oxy_prefix_batch_build(pool.p, [(pid, 1, 0)], 0, pool.stream)
+        assert e.value.code == B.ERR_SEALED
+        batch = B.oxy_batch_build(pool.p, [(sid, 2)], 0, pool.stream)
+        for l in range(L):
+            q, k, v = bits(rng, 2, 8, 256), bits(rng, 2, 256), bits(rng, 2, 256)
+            dq, dk, dv = up(q), up(k), up(v)
+            out = torch.zeros((2, 8, 256), dtype=torch.int16, device="cuda")
+            B.oxy_stream_append(pool.p, batch, l, dk.data_ptr(), dv.data_ptr(), pool.stream)
+            B.oxy_mixed_attention(pool.p, batch, l, dq.data_ptr(), out.data_ptr(), 0, SCALE, pool.stream)
+            check(down(out), None, q, held(np.concatenate(keys[l] + [k]), kv8), held(np.concatenate(values[l] + [v]), kv8),
+                  past, 0, SCALE, "request, layer %d" % l)
+        B.oxy_batch_destroy(batch)
+    finally:
+        pool.close()
+
+
+class Calls:
+    """A prefix batch and a prompt batch with resident inputs, both with split results."""
+
+    def __init__(self, kv8):
+        import torch
+        rng = np.random.default_rng(8)
+        self.n = 50
+        self.pool = Pool(1, 80, kv8, seed=1, max_q_tokens=1024)
+        B = self.B = self.pool.B
+        pid = self.pool.prefix(bits(rng, 900, 256), bits(rng, 900, 256))
+        self.prefix = B.oxy_prefix_batch_build(self.pool.p, [(pid, self.n, 0)], 0, self.pool.stream)
+        k, v = up(bits(rng, self.n, 256)), up(bits(rng, self.n, 256))
+        B.oxy_stream_append(self.pool.p, self.prefix, 0, k.data_ptr(), v.data_ptr(), self.pool.stream)
+        self.prompt = B.oxy_prompt_batch_build(self.pool.p, [(700, 0), (44, 44)], self.pool.stream)
+        assert B.oxy_batch_info(self.prefix)[3] > 0 and B.oxy_batch_info(self.prompt)[3] > 0
+        self.q = up(bits(rng, 744, 8, 256))
+        self.x = up(bits(rng, 744, 2, 256))
+        self.out = [torch.zeros((m, 8, 256), dtype=torch.int16, device="cuda") for m in (self.n, 744)]
+        self.lse = [torch.zeros((m, 8), device="cuda") for m in (self.n, 744)]
+        torch.cuda.synchronize()
+
+    def run(self):
+        import torch
+        s = torch.cuda.current_stream().cuda_stream
+        self.B.oxy_prefix_attention(self.pool.p, self.prefix, 0, self.q.data_ptr(), 4096, self.out[0].data_ptr(), 4096,
+                                    self.lse[0].data_ptr(), SCALE, s)
+        a = self.x.data_ptr()
+        self.B.oxy_prompt_attention(self.pool.p, self.prompt, self.q.data_ptr(), 4096, a, 1024, a + 512, 1024,
+                                    self.out[1].data_ptr(), 4096, self.lse[1].data_ptr(), SCALE, s)
+
+    def taken(self):
+        got = [down(o) for o in self.out] + [z.cpu().numpy() for z in self.lse]
+        for t in self.out + self.lse:
+            t.zero_()
+        return got
+
+    def close(self):
+        import torch
+        torch.cuda.synchronize()
+        self.B.oxy_batch_destroy(self.prefix)
+        self.B.oxy_batch_destroy(self.prompt)
+        self.pool.close()
+
+
+@FORMS
+def test_recorded_and_replayed_on_another_stream(kv8):
+    import torch
+    c = Calls(kv8)
+    try:
+        c.run()
+        want = c.taken()
+        c.run()
+        assert all(np.array_equal(a, b) for a, b in zip(want, c.taken()))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            c.run()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(a, b) for a, b in zip(want, c.taken()))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.run()
+        for i in range(4):
+            graph.replay()
+            assert all(np.array_equal(a, b) for a, b in zip(want, c.taken())), i
+            c.run()
+            assert all(np.array_equal(a, b) for a, b in zip(want, c.taken())), i
+        other = up(bits(np.random.default_rng(9), 744, 8, 256))
+        c.q.copy_(other)                # new inputs at the same addresses
+        graph.replay()
+        got = c.taken()
+        c.run()
+        assert all(np.array_equal(a, b) for a, b in zip(got, c.taken()))
+        assert not np.array_equal(got[0], want[0])
+    finally:
+        c.close()
+
+
+@FORMS
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan], ids=str)
+@pytest.mark.parametrize("at", [0, 16, 35, 63, 64, 71])
+def test_values_that_are_not_finite(at, bad, kv8):
+    """A value of one token: queries before it are as without it, those that see it lose its dim or the 64 it is among."""
+    _odd_row(at, bad, kv8, value=True)
+
+
+@FORMS
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan], ids=str)
+@pytest.mark.parametrize("at", [0, 35, 71])
+def test_keys_that_are_not_finite(at, bad, kv8):
+    """A key of one token: queries before it are as without it, those that see it are NaN (or, where a logit is infinite
+    and negative, as without the token)."""
+    _odd_row(at, bad, kv8, value=False)
+
+
+def _odd_row(at, bad, kv8, value):
+    import torch
+    rng = np.random.default_rng(at)
+    n, dim = 72, 130
+    odd = np.float32(bad).view(np.uint32) >> 16
+    q, k, v = bits(rng, n, 8, 256), bits(rng, n, 256), bits(rng, n, 256)
+    q[:, :, dim] = 0x3f80           # 1: the sign of an infinite logit is that of the key
+    got = {}
+    for way in ("pages", "rows"):
+        for with_it in (False, True):
+            kk, vv = k.copy(), v.copy()
+            (vv if value else kk)[at, dim] = odd if with_it else 0
+            pool = Pool(1, 16, kv8, seed=2, max_q_tokens=128)
+            B = pool.B
+            dq, dk, dv = up(q), up(kk), up(vv)
+            out = torch.zeros((n, 8, 256), dtype=torch.int16, device="cuda")
+            try:
+                if way == "pages":
+                    pid = B.oxy_prefix_create(pool.p)
+                    b = B.oxy_prefix_batch_build(pool.p, [(pid, n, 0)], 0, pool.stream)
+                    B.oxy_stream_append(pool.p, b, 0, dk.data_ptr(), dv.data_ptr(), pool.stream)
+                    B.oxy_prefix_attention(pool.p, b, 0, dq.data_ptr(), 4096, out.data_ptr(), 4096, 0, SCALE, pool.stream)
+                else:
+                    b = B.oxy_prompt_batch_build(pool.p, [(n, 0)], pool.stream)
+                    B.oxy_prompt_attention(pool.p, b, dq.data_ptr(), 4096, dk.data_ptr(), 512, dv.data_ptr(), 512,
+                                           out.data_ptr(), 4096, 0, SCALE, pool.stream)
+                got[with_it] = widen_bf16(down(out))
+                B.oxy_batch_destroy(b)
+            finally:
+                pool.close()
+        a, b = got[False], got[True]
+        assert np.array_equal(a[:at], b[:at]) and np.all(np.isfinite(b[:at]))
+        if value:
+            others = np.r_[0:128, 192:256]
+            assert not np.any(np.isfinite(b[at:, :, dim])) and np.array_equal(a[at:][..., others], b[at:][..., others])
+        elif bad == -np.inf and (way == "rows" or not kv8):     # in 8 bits an infinity is NaN
+            # a weight of 0, but for the first token, whose only key it may be
+            assert np.all(np.isfinite(b[at + 1:])) or at == 0
+        else:
+            assert np.all(np.isnan(b[at:]))
+
+
+@pytest.mark.parametrize("tail", [0xff, 0x7f])
+def test_stale_rows_behind_the_end(tail):
+    """Slots that nothing was written to hold NaN (or 8-bit exponents of infinity): they reach nothing.  Lengths that end
+    inside a page and inside a tile."""
+    import torch
+    from paper_2603_14371_amd import binding as B
+    for kv8 in (False, True):
+        for n in (1, 7, 17, 33, 47):
+            pool = Pool(1, 4, kv8, max_q_tokens=64)
+            pool.kv.fill_(tail)
+            rng = np.random.default_rng(n)
+            q, k, v = bits(rng, n, 8, 256), bits(rng, n, 256), bits(rng, n, 256)
+            dq, dk, dv = up(q), up(k), up(v)
+            out = torch.zeros((n, 8, 256), dtype=torch.int16, device="cuda")
+            try:
+                pid = B.oxy_prefix_create(pool.p)
+                b = B.oxy_prefix_batch_build(pool.p, [(pid, n, n)], 0, pool.stream)
+                B.oxy_stream_append(pool.p, b, 0, dk.data_ptr(), dv.data_ptr(), pool.stream)
+                B.oxy_prefix_attention(pool.p, b, 0, dq.data_ptr(), 4096, out.data_ptr(), 4096, 0, SCALE, pool.stream)
+                check(down(out), None, q, held(k, kv8), held(v, kv8), 0, n, SCALE, "%d tokens" % n)
+                B.oxy_batch_destroy(b)
+            finally:
+                pool.close()
