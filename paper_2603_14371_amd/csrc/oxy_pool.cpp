@@ -1771,6 +1771,12 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
   if (d.tables.size() > table_words_of(p->cfg))
     return fail(OXY_ERR_WORKSPACE, "%s: the block tables list %zu entries > %zu (forked prefixes list shared blocks once each)",
                 who, d.tables.size(), table_words_of(p->cfg));
+  for (size_t w = 0; w < d.work.size() && kind == BATCH_PREFIX; w += oxy::kPrefillWords) {
+    int32_t* r = &d.work[w];
+    const int32_t first = r[oxy::F_BEGIN] / kPage, last = (r[oxy::F_LEN] - 1) / kPage;
+    for (int32_t i = 0; i < oxy::kPrefillPages; ++i)
+      r[oxy::F_PAGES + i] = d.tables[r[oxy::F_SRC] + std::min(first + i, last)];
+  }
   oxy_batch* b = new oxy_batch();
   b->pool = p;
   b->kind = kind;
@@ -1999,6 +2005,8 @@ int32_t oxy_prompt_attention(oxy_pool* p, const oxy_batch* b, const void* q, siz
   if (bad_rows(q, q_stride, oxy::kHeads, b->n_tokens) || bad_rows(out, out_stride, oxy::kHeads, b->n_tokens) ||
       bad_rows(k, k_stride, 1, b->n_tokens) || bad_rows(v, v_stride, 1, b->n_tokens))
     return fail(OXY_ERR_INVALID_ARG, "prompt_attention: rows must be 16-byte aligned, strides at least a token's rows");
+  if (b->n_tokens > 1 && (k_stride >= (size_t)1 << 31 || v_stride >= (size_t)1 << 31))
+    return fail(OXY_ERR_INVALID_ARG, "prompt_attention: k_stride or v_stride of 2 GiB or more");
   oxy::PrefillArgs a = prefill_args(p, b, q, q_stride, out, out_stride, lse, scale);
   a.k = (const char*)k;
   a.v = (const char*)v;

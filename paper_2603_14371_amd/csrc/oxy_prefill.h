@@ -8,7 +8,7 @@
 namespace oxy {
 
 // A record of the work list: query tokens of one item that lie side by side, and the keys [begin, end) of that item.
-constexpr int kPrefillWords = 16;
+constexpr int kPrefillWords = 32;   // a line of 128 bytes
 enum { F_TOK0 = 0,     // first query token: row of q, out and lse
        F_N_TOK,        // query tokens
        F_POS,          // position of the first one in its item
@@ -17,8 +17,12 @@ enum { F_TOK0 = 0,     // first query token: row of q, out and lse
        F_SRC,          // paged: first word of the item's block table; a prompt: row of its first token
        F_PART,         // split result of the first query token, -1: the record writes the output
        F_N_PARTS,      // split results of a token: those of token t begin F_N_PARTS * t behind F_PART
-       F_LEN };        // tokens of the item
+       F_LEN,          // tokens of the item
+       F_PAGES = 16 }; // paged: block ids of the first kPrefillPages pages, the item's last one repeated
+constexpr int kPrefillPages = 16;
 constexpr int kPrefillTokens = 16;   // query tokens of a record, at most
+// Launches of at most this many records have a workgroup a CU.
+constexpr int kPrefillCus = 256;
 // Words of the merge list for each token that has split results: the token, its first one, how many.
 constexpr int kMergeWords = 3;
 

@@ -31,79 +31,94 @@ enum PrefillSource { SRC_PAGES, SRC_PAGES8, SRC_ROWS };
 constexpr int kStep = 32;                       // keys of a tile: two pages
 constexpr int kTileBytes = 2 * kPageBytes;      // of K, or of V
 
-struct __align__(16) PrefillLds {
-  char k[2][kTileBytes];      // in the order of the cache's pages, see oxy.h
-  char v[2][kTileBytes];
-  float vs[2][kStep];         // in 8 bits: what the tile's values are to be multiplied by
-  uint32_t odd[kDim];         // keys of the tile whose value is not finite in a dim
+// In 8 bits: codes and exponents as they lie in the pages, a part for each wavefront, which widens what it requested.
+template <bool kDeep>
+struct RawTiles {
+  static constexpr int kTiles = kDeep ? 4 : 1;
+  char codes[kTiles][4][4096];      // [wavefront]: two pieces of 1 KiB of a K page, two of a V page
+  char exps[kTiles][4][256];        // exponents of a page, then nothing
+};
+struct NoTiles {};
+// kDeep: what is in flight.  One workgroup a CU requests three tiles ahead; of two, each requests one.
+template <int kSrc, bool kDeep>
+struct PrefillLds {
+  static constexpr int kTiles = kSrc == SRC_PAGES8 ? (kDeep ? 2 : 1) : kDeep ? 4 : 2;
+  char k[kTiles][kTileBytes], v[kTiles][kTileBytes];
+  float vs[kTiles][kStep];    // in 8 bits: scales of the values
+  uint32_t odd[kDim];         // keys of a tile whose value is not finite in a dim
+  uint32_t found[4];          // [wavefront]: whether it found one
+  std::conditional_t<kSrc == SRC_PAGES8, RawTiles<kDeep>, NoTiles> raw;
+  uint32_t spare[4][64];      // [wavefront]: what a request in the place of a tile's goes to
 };
 
-typedef const __attribute__((address_space(1))) void* GlobalPtr;
-typedef __attribute__((address_space(3))) void* LdsPtr;
+// `size` bytes a lane from base + offset, base the same for the wavefront, to LDS, lane after lane.  A buffer operation, which
+// counts among vector memory operations only: behind one with a full address the compiler waits for all reads of LDS at once.
+template <int kSize>
+__device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, const uint32_t offset, void* to) {
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+  const auto lds = (__attribute__((address_space(3))) void*)to;
+  if constexpr (kSize == 16)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 16, offset, 0, 0, 0);
+  else
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 4, offset, 0, 0, 0);
+}
+// Waits until at most n of a wavefront's vector memory operations are left.
+//
+// The compiler waits by itself, for everything, in front of a read of LDS that may be of what is being requested.  It compares a
+// read with the kernel's first request only, so that one goes to a place that nothing reads (`spare`), and the reads' indices
+// are such that their ranges are seen.
+template <int n>
+__device__ __forceinline__ void wait_vector() {
+  static_assert(n >= 1 && n < 64, "");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+}
+// What a workgroup wrote to LDS before is seen behind it; requests stay in flight (a fence of the workgroup's scope would wait
+// for those too).
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // LDS operations only
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
 
-// What a thread holds of a tile between its loads and its stores to LDS.
-template <int kSrc>
-struct Staged {};
-template <>
-struct Staged<SRC_PAGES8> {
-  u32x4 k[2], v[2];
-  uint32_t ks[2], vs;
-};
-template <>
-struct Staged<SRC_ROWS> {
-  u32x2 v[8];
-};
+// Rows in LDS as they lie in memory, 512 bytes each, their 16-byte chunks changing places so that the lanes that are served
+// together find theirs in different banks: eight keys of one chunk (K), four keys of two chunks (V, read transposed).
+__device__ __forceinline__ int k_row_swap(const int key) { return key & 7; }
+__device__ __forceinline__ int v_row_swap(const int key) { return (key & 1) * 4 + (key >> 1 & 1); }
 
-// Tile of keys key0 .. key0 + 31 on its way to LDS buffer b: requested here.
-template <int kSrc>
-__device__ __forceinline__ void request_tile(const PrefillArgs& a, PrefillLds& lds, Staged<kSrc>& st, const int b, const int key0,
-                                             const int src, const int len) {
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int last_page = (len - 1) >> 4, page0 = key0 >> 4;
+// A wavefront's part of a tile on its way to LDS, eight operations (five in 8 bits).  blk: the wavefront's page, of rows:
+// nothing.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.
+template <int kSrc, class Lds>
+__device__ __forceinline__ void request_tile(const char* base, const void* second, const size_t k_stride, const size_t v_stride,
+                                             Lds& lds, const int b, const int key0, const int blk, const int src,
+                                             const int len, const int wave, const int lane) {
+  const int pg = wave >> 1, side = wave & 1;
   if constexpr (kSrc == SRC_PAGES) {
-    // wavefronts 0 and 1 bring the first page, 2 and 3 the second one, half of K and half of V each
-    const int pg = wave >> 1, part = (wave & 1) * (kPageBytes / 2);
-    const int blk = ((DescPtr)a.tables)[src + min(page0 + pg, last_page)];
-    const char* from = a.layer_base + (size_t)blk * kBlockBytes + part + lane * 16;
+    const char* from = base + (size_t)blk * kBlockBytes;
+    const int part = side * (kPageBytes / 2), at = pg * kPageBytes + part;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(from + i * 1024), (LdsPtr)(lds.k[b] + pg * kPageBytes + part + i * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(from + kPageBytes + i * 1024),
-                                       (LdsPtr)(lds.v[b] + pg * kPageBytes + part + i * 1024), 16, 0, 0);
-    }
+    for (int i = 0; i < 4; ++i) to_lds<16>(from, kBlockBytes, part + i * 1024 + lane * 16, lds.k[b] + at + i * 1024);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to_lds<16>(from, kBlockBytes, kPageBytes + part + i * 1024 + lane * 16, lds.v[b] + at + i * 1024);
   } else if constexpr (kSrc == SRC_PAGES8) {
-    const int pg = wave >> 1;
-    const int blk = ((DescPtr)a.tables)[src + min(page0 + pg, last_page)];
-    const char* from = a.layer_base + (size_t)blk * kBlockBytes8;
-    const uint8_t* sc = a.scales + (size_t)blk * kScaleBytes8;
-    const int u = t & 127;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      st.k[i] = *(const u32x4*)(from + (u + 128 * i) * 16);
-      st.ks[i] = sc[k8_scale_offset(u & 15)];
-    }
-    // chunks (w, gp, n) and (w, gp + 2, n)
-    const int n = u & 15, gp = (u >> 4) & 1, w = u >> 5;
-    st.v[0] = *(const u32x4*)(from + kPageBytes8 + v8_chunk_offset(w, gp, n));
-    st.v[1] = *(const u32x4*)(from + kPageBytes8 + v8_chunk_offset(w, gp + 2, n));
-    // stale exponents behind the item's end may be infinite: 0 instead
-    st.vs = key0 + pg * 16 + (u & 15) < len ? sc[v8_scale_offset(u & 15)] : 0;
+    // K chunks of all keys and half of the dims; V chunks of all keys of half of the dims
+    const char* from = base + (size_t)blk * kBlockBytes8;
+    char* to = lds.raw.codes[b][wave];
+    to_lds<16>(from, kBlockBytes8, side * 1024 + lane * 16, to);
+    to_lds<16>(from, kBlockBytes8, side * 1024 + 2048 + lane * 16, to + 1024);
+    to_lds<16>(from, kBlockBytes8, kPageBytes8 + side * 2048 + lane * 16, to + 2048);
+    to_lds<16>(from, kBlockBytes8, kPageBytes8 + side * 2048 + 1024 + lane * 16, to + 3072);
+    to_lds<4>((const char*)second + (size_t)blk * kScaleBytes8, kScaleBytes8, lane * 4, lds.raw.exps[b][wave]);   // 8 lanes, then 0
   } else {
-    // K: a lane's 16 bytes are one chunk of the page order
-    const int pg = wave >> 1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int chunk = (wave & 1) * 256 + i * 64 + lane;
-      const int k8 = chunk & 7, g = (chunk >> 3) & 3, hf = (chunk >> 5) & 1, j = chunk >> 6;
-      const int key = min(key0 + pg * 16 + hf * 8 + k8, len - 1);
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(a.k + (size_t)(src + key) * a.k_stride + (4 * j + g) * 16),
-                                       (LdsPtr)(lds.k[b] + pg * kPageBytes + ((wave & 1) * 256 + i * 64) * 16), 16, 0, 0);
-    }
-    const int u = t & 127, n = u & 15, gp = (u >> 4) & 1, w = u >> 5;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int key = min(key0 + pg * 16 + 4 * gp + (e & 3) + 8 * (e >> 2), len - 1);
-      st.v[e] = *(const u32x2*)(a.v + (size_t)(src + key) * a.v_stride + (64 * w + 4 * n) * 2);
+    for (int i = 0; i < 8; ++i) {   // two rows at a time
+      const int two = 8 * wave + 2 * (i & 3), key = two + (lane >> 5), c = lane & 31;
+      const int first = min(key0 + two, len - 1);
+      const size_t stride = i < 4 ? k_stride : v_stride;
+      const uint32_t next = first < len - 1 ? (uint32_t)stride : 0;   // the last one again
+      const char* from = (i < 4 ? base : (const char*)second) + (size_t)(src + first) * stride;
+      to_lds<16>(from, next + kDim * 2, (lane >> 5) * next + (c ^ (i < 4 ? k_row_swap(key) : v_row_swap(key))) * 16,
+                 (i < 4 ? lds.k[b] : lds.v[b]) + two * 512);
     }
   }
 }
@@ -113,96 +128,245 @@ __device__ __forceinline__ u32x2 widen4(const uint32_t codes, const float scale)
   return (u32x2){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))};
 }
-
-// What arrived in registers goes to LDS.
-template <int kSrc>
-__device__ __forceinline__ void store_tile(PrefillLds& lds, const Staged<kSrc>& st, const int b) {
-  const int t = threadIdx.x, u = t & 127, pg = t >> 7;
-  char* kp = lds.k[b] + pg * kPageBytes;
-  char* vp = lds.v[b] + pg * kPageBytes;
-  const int n = u & 15, gp = (u >> 4) & 1, w = u >> 5;
-  if constexpr (kSrc == SRC_PAGES8) {
+// A wavefront's part of a tile in 8 bits, from codes to the page order of bf16.  Keys with their scale; the scales of the
+// values go into the probabilities (see the kernel), since four keys share a word.  left: keys of the item from the tile's first on.
+template <class Lds>
+__device__ __forceinline__ void widen_tile(Lds& lds, const int r, const int b, const int left, const int wave,
+                                           const int lane) {
+  const int pg = wave >> 1, side = wave & 1;
+  const char* from = lds.raw.codes[r][wave] + lane * 16;
+  char* const kp = lds.k[b] + pg * kPageBytes;
+  char* const vp = lds.v[b] + pg * kPageBytes;
+  const int key = lane & 15;
+  const float s = scale_of((uint8_t)lds.raw.exps[r][wave][k8_scale_offset(key)]);
+  // stale exponents behind the item's end may be infinite: 0 instead
+  const float vs = 16 * pg + key < left ? scale_of((uint8_t)lds.raw.exps[r][wave][v8_scale_offset(key)]) : 0.f;
+  const int n = lane & 15, gp = (lane >> 4) & 1, w = lane >> 5;
+  const char* v_from = lds.raw.codes[r][wave] + 2048 + w * 1024 + (gp * 16 + n) * 16;
+  // all reads before the first write: behind a write the compiler waits for what is on its way to LDS before it reads
+  const u32x4 keys[2] = {*(const u32x4*)from, *(const u32x4*)(from + 1024)};
+  const u32x4 lo = *(const u32x4*)v_from, hi = *(const u32x4*)(v_from + 512);   // keys 4gp.. and 8 + 4gp..
+  if (side == 0 && lane < 16) lds.vs[b][16 * pg + lane] = vs;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int chunk = u + 128 * i, key = chunk & 15, ch = 2 * (chunk >> 4);   // 8 dims each: ch and ch + 1
-      const float s = scale_of(st.ks[i]);
-      const u32x2 x0 = widen4(st.k[i][0], s), x1 = widen4(st.k[i][1], s), x2 = widen4(st.k[i][2], s), x3 = widen4(st.k[i][3], s);
-      *(u32x4*)(kp + k_chunk_offset(ch >> 2, key >> 3, ch & 3, key & 7)) = (u32x4){x0[0], x0[1], x1[0], x1[1]};
-      *(u32x4*)(kp + k_chunk_offset((ch + 1) >> 2, key >> 3, (ch + 1) & 3, key & 7)) = (u32x4){x2[0], x2[1], x3[0], x3[1]};
-    }
+  for (int i = 0; i < 2; ++i) {
+    const u32x4 x = keys[i];
+    const int ch = 2 * (4 * side + (lane >> 4) + 8 * i);   // eight dims each: ch and ch + 1
+    const u32x2 x0 = widen4(x[0], s), x1 = widen4(x[1], s), x2 = widen4(x[2], s), x3 = widen4(x[3], s);
+    *(u32x4*)(kp + k_chunk_offset(ch >> 2, key >> 3, ch & 3, key & 7)) = (u32x4){x0[0], x0[1], x1[0], x1[1]};
+    *(u32x4*)(kp + k_chunk_offset((ch + 1) >> 2, key >> 3, (ch + 1) & 3, key & 7)) = (u32x4){x2[0], x2[1], x3[0], x3[1]};
+  }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const u32x2 x = widen4(st.v[0][c], 1.f), y = widen4(st.v[1][c], 1.f);
-      *(u32x4*)(vp + v_chunk_offset(w, c, gp, n)) = (u32x4){x[0], x[1], y[0], y[1]};
-    }
-    if (u < 16) lds.vs[b][pg * 16 + u] = scale_of(st.vs);
-  } else if constexpr (kSrc == SRC_ROWS) {
-    // eight keys of four dims -> four chunks of a dim's eight keys
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t pick = c & 1 ? 0x07060302u : 0x05040100u;
-      u32x4 x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(st.v[2 * i + 1][c >> 1], st.v[2 * i][c >> 1], pick);
-      *(u32x4*)(vp + v_chunk_offset(w, c, gp, n)) = x;
-    }
+  for (int c = 0; c < 4; ++c) {
+    const u32x2 x = widen4(lo[c], 1.f), y = widen4(hi[c], 1.f);
+    *(u32x4*)(vp + v_chunk_offset(2 * side + w, c, gp, n)) = (u32x4){x[0], x[1], y[0], y[1]};
   }
 }
 
 // A value that a row does not see, or that nothing was written to, must not reach it, and 0 times what is not finite is NaN.
-// In tiles that some row sees a part of, such values are therefore taken as 0 and remembered by dim and key: thread t looks
-// after dim t.
-__device__ __forceinline__ bool set_odd_aside(PrefillLds& lds, const int b) {
-  const int t = threadIdx.x;
+// In tiles that some row sees a part of, such values are therefore looked for, which costs a barrier.
+__device__ __forceinline__ bool odd_pair(const uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+template <class Lds>
+__device__ __forceinline__ bool has_odd(Lds& lds, const int b, const int wave) {
+  const int t = threadIdx.x & 255;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32x4 x = *(const u32x4*)(lds.v[b] + (i * 256 + t) * 16);
+    odd = odd || odd_pair(x[0]) || odd_pair(x[1]) || odd_pair(x[2]) || odd_pair(x[3]);
+  }
+  const bool mine = __ballot(odd) != 0;
+  if ((t & 63) == 0) lds.found[wave] = mine;
+  lds_barrier();
+  const u32x4 all = *(const u32x4*)lds.found;
+  return (all[0] | all[1] | all[2] | all[3]) != 0;
+}
+// Such values are taken as 0 and remembered by dim and key: thread t looks after dim t.
+template <int kSrc, class Lds>
+__device__ __forceinline__ void set_odd_aside(Lds& lds, const int b) {
+  const int t = threadIdx.x & 255;
   uint32_t odd = 0;
-#pragma unroll
-  for (int pg = 0; pg < 2; ++pg)
-#pragma unroll
-    for (int gp = 0; gp < 2; ++gp) {
-      u32x4* chunk = (u32x4*)(lds.v[b] + pg * kPageBytes + v_chunk_of_dim(t, gp));
-      u32x4 x = *chunk;
-      uint32_t bits = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t one = e & 1 ? 0x7f800000u : 0x7f80u;
-        if ((x[e >> 1] & one) == one) {
-          bits |= 1u << (16 * pg + 4 * gp + (e & 3) + 8 * (e >> 2));
-          x[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
-        }
-      }
-      if (bits) *chunk = x;
-      odd |= bits;
-    }
+#pragma unroll 1
+  for (int key = 0; key < kStep; ++key) {
+    char* at = lds.v[b];
+    if (kSrc == SRC_ROWS)
+      at += key * 512 + ((t >> 3) ^ v_row_swap(key)) * 16 + (t & 7) * 2;
+    else
+      at += (key >> 4) * kPageBytes + v_chunk_of_dim(t, (key >> 2) & 1) + v_slot_of_key(key & 15) * 2;
+    uint16_t* const x = (uint16_t*)at;
+    if ((*x & 0x7f80u) == 0x7f80u) *x = 0, odd |= 1u << key;
+  }
   lds.odd[t] = odd;
-  return __syncthreads_or(odd != 0);
+  lds_barrier();
 }
 
+// Four keys of one dim from rows of LDS: within 16 lanes, lane 4a + b names four dims of key a, and lane i receives dim i of
+// the sixteen, keys 0 to 3.
+__device__ __forceinline__ u32x2 read_turned(const char* at) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+}
+// The dim, but for 16h, that register r of product j holds: lane half h has 16 dims in a row, of pages in the order of their
+// chunks.
 template <int kSrc>
-__global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
-  __shared__ PrefillLds lds;
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+constexpr int dim_of(const int j, const int r) {
+  return kSrc == SRC_ROWS ? 32 * j + r : 64 * (j >> 1) + 32 * ((r >> 2) & 1) + 4 * (r & 3) + 2 * (j & 1) + (r >> 3);
+}
+// Register of dim d + 16h, d in [32x, 32x + 16).
+template <int kSrc>
+__device__ __forceinline__ float of_dim(const f32x16 (&o)[8], const int d) {
+  if constexpr (kSrc == SRC_ROWS) return o[d >> 5][d & 15];
+  return o[2 * (d >> 6) + ((d >> 1) & 1)][8 * (d & 1) + 4 * ((d >> 5) & 1) + ((d >> 2) & 3)];
+}
+
+// Sixteen products whose operands come from LDS: those of the first kAhead are read at once, then each product is followed by
+// the read of the one kAhead on.  The order is kept from the compiler, which reads one or two ahead.
+template <int kAhead, class Read, class Multiply>
+__device__ __forceinline__ void products(const Read& read, const Multiply& multiply) {
+  constexpr int kAluPasses = 0x6;
+  u32x4 x[kAhead];
+  static_for<kAhead>([&](auto j) { x[j.value] = read(j); });
+  __builtin_amdgcn_sched_barrier(kAluPasses);
+  static_for<16>([&](auto j) {
+    multiply(j, x[j.value % kAhead]);
+    if constexpr (j.value + kAhead < 16) x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
+    __builtin_amdgcn_sched_barrier(kAluPasses);
+  });
+}
+
+// A wavefront's rows leave through LDS (8 KiB of its own), as whole lines, half of the dims at a time: outputs, `scale` times
+// the sums, in bf16; or split results, see store_part, whose exponents go to exps.  to: the first of its four tokens, of which
+// `left` are there.
+template <int kSrc, bool kDirect>
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[8], const float scale, uint32_t& exps, char* lds, char* to,
+                                           const size_t token_stride, const int left, const int lane) {
   const int n = lane & 31, h = lane >> 5;
-  const DescPtr rec = (DescPtr)a.work + (size_t)blockIdx.x * kPrefillWords;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+#pragma unroll
+    for (int w = 2 * half; w < 2 * half + 2; ++w) {
+      float up = scale;
+      if constexpr (!kDirect) {
+        float amax = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) amax = fmaxf(fmaxf(amax, fabsf(o[2 * w][r])), fabsf(o[2 * w + 1][r]));
+        amax = pair_max(amax);
+        const int eb = max(24, min(253, (int)(__float_as_uint(amax) >> 23)));
+        up = __uint_as_float((uint32_t)(127 + 14 + 126 - eb) << 23) + (amax - amax);
+        exps |= (uint32_t)((eb - 126) & 0xff) << (8 * w);
+      }
+#pragma unroll
+      for (int d = 64 * w; d < 64 * w + 64; d += 32)
+#pragma unroll
+        for (int e0 = 0; e0 < 16; e0 += 8) {
+          u32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x0 = of_dim<kSrc>(o, d + e0 + 2 * e) * up, x1 = of_dim<kSrc>(o, d + e0 + 2 * e + 1) * up;
+            x[e] = kDirect ? pack_bf16(x0, x1) : pack_f16(x0, x1);
+          }
+          const int chunk = (d & 127) / 8 + e0 / 8 + 2 * h;
+          *(u32x4*)(lds + n * 256 + (chunk ^ (n & 7)) * 16) = x;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = 4 * i + (lane >> 4), chunk = (lane & 15) ^ (row & 7);
+      const u32x4 x = *(const u32x4*)(lds + row * 256 + (lane & 15) * 16);
+      if ((i >> 1) < left) *(u32x4*)(to + (i >> 1) * token_stride + (row & 7) * (kDim * 2) + 256 * half + chunk * 16) = x;
+    }
+  }
+}
+
+// What a workgroup needs behind its first loads.
+struct PrefillLate {
+  void* out;
+  float* lse;
+  size_t out_stride;
+  const int32_t* tables;
+  uint16_t* part_acc;
+  float* part_ml;
+  float scale;
+};
+
+template <int kSrc, bool kDeep>
+__global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32_t* work, const char* q_rows, const size_t q_stride,
+                                                                     const char* base, const void* second, const size_t k_stride,
+                                                                     const size_t v_stride, const PrefillLate a) {
+  constexpr bool kRaw = kSrc == SRC_PAGES8;
+  __shared__ __align__(16) PrefillLds<kSrc, kDeep> lds;
+  constexpr int kBuffers = kRaw ? RawTiles<kDeep>::kTiles : PrefillLds<kSrc, kDeep>::kTiles;   // that requests go to
+  constexpr int kAhead = kRaw && !kDeep ? 1 : kBuffers - 1;                                  // tiles requested ahead
+  constexpr int kOps = kRaw ? 5 : 8;                                                         // of a tile
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6) & 3;
+  const int n = lane & 31, h = lane >> 5;
+  const DescPtr rec = (DescPtr)work + (size_t)blockIdx.x * kPrefillWords;
   const int tok0 = rec[F_TOK0], n_tok = rec[F_N_TOK], pos = rec[F_POS], full = rec[F_FULL];
   const int kv_begin = rec[F_BEGIN], kv_end = rec[F_END], src = rec[F_SRC], part = rec[F_PART], n_parts = rec[F_N_PARTS],
             len = rec[F_LEN];
+  const int n_tiles = (kv_end - kv_begin + kStep - 1) / kStep;
 
-  Staged<kSrc> st;
-  request_tile<kSrc>(a, lds, st, 0, kv_begin, src, len);
+  // the wavefront's page of a tile
+  auto page_of = [&](const int tile) {
+    if constexpr (kSrc == SRC_ROWS) return 0;
+    const int at = 2 * tile + (wave >> 1), page = min((kv_begin >> 4) + at, (len - 1) >> 4);
+    return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[src + page];
+  };
+  auto request = [&](const int tile, const int blk) {
+    int at = lane;
+    asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
+    request_tile<kSrc>(base, second, k_stride, v_stride, lds, tile % kBuffers, kv_begin + tile * kStep, blk, src, len, wave,
+                       at & 63);
+  };
+
+  // a request that is there to be waited behind
+  auto request_spare = [&]() {
+    to_lds<4>(work + (size_t)blockIdx.x * kPrefillWords, kPrefillWords * 4, lane * 4, lds.spare[wave]);
+  };
+  request_spare();   // the first of all, see wait_vector
+  request(0, page_of(0));
+
+  // The wavefront's 32 query rows, four tokens' eight heads, come through LDS, as whole lines: a row a lane, as the products
+  // take them, would be 64 pieces of 16 bytes each in a line of its own.  Into buffers that the first tile does not go to.
+  u32x4 q[16];
+  {
+    constexpr int kPasses = kDeep ? 1 : 2, kRows = 32 / kPasses;
+    char* const at = kDeep ? (wave < 2 ? lds.k[lds.kTiles - 2 + (wave & 1)] : lds.v[lds.kTiles - 2 + (wave & 1)])
+                           : (wave < 2 ? lds.k[lds.kTiles - 1] : lds.v[lds.kTiles - 1]) + (wave & 1) * 8192;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+#pragma unroll
+      for (int i = 0; i < kRows / 2; ++i) {
+        const int two = pass * kRows + 2 * i, row = two + (lane >> 5);
+        const char* from = q_rows + (size_t)(tok0 + min(4 * wave + (two >> 3), n_tok - 1)) * q_stride;
+        to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, at + i * 1024);
+      }
+      if (kAhead > 1 && n_tiles > 1) {
+        request(1, page_of(1));
+        wait_vector<kOps>();
+      } else {
+        request_spare();
+        wait_vector<1>();
+      }
+      if (kPasses == 1 || (n >> 4) == pass) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          q[j] = *(const u32x4*)(at + (n & (kRows - 1)) * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+      }
+    }
+  }
+  if constexpr (kRaw) lds_barrier();   // the first tile is widened into where rows were
+  int next_page = page_of(kAhead > 1 ? 2 : 1);
 
   // this lane's row
   const int mine = 4 * wave + (n >> 3), tok = min(mine, n_tok - 1);
-  const bool live = mine < n_tok;
   const int sees = min(len, max(pos + tok + 1, full));   // keys below
-  u32x4 q[16];
-  const char* q_row = (const char*)a.q + (size_t)(tok0 + tok) * a.q_stride + (n & 7) * (kDim * 2) + 16 * h;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-  for (int s = 0; s < 16; ++s) q[s] = *(const u32x4*)(q_row + 32 * s) ^ (u32x4){flip, flip, flip, flip};
+  for (int s = 0; s < 16; ++s) q[s] ^= (u32x4){flip, flip, flip, flip};
   float sl2 = fabsf(a.scale * 1.4426950408889634f);
   if (sl2 == 0.f) sl2 = 0x1p-120f;
 
-  // keys that all rows of the workgroup see; that all rows of the wavefront see: those of its first token; the last key that any sees: of its last one
+  // keys that all rows of the workgroup see; that all rows of the wavefront see; the last key that any of them sees
   const int first_tok = min(4 * wave, n_tok - 1), last_tok = min(4 * wave + 3, n_tok - 1);
   const int tile_sees = min(len, max(pos + 1, full));
   const int all_see = min(len, max(pos + first_tok + 1, full));
@@ -211,18 +375,51 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
   f32x16 o[8] = {};
   float m = -__builtin_inff(), l = 0.f;
 
-  store_tile<kSrc>(lds, st, 0);
-  __syncthreads();
-  int b = 0;
-  for (int key0 = kv_begin; key0 < kv_end; key0 += kStep, b ^= 1) {
-    const bool more = key0 + kStep < kv_end;
-    if (more) request_tile<kSrc>(a, lds, st, b ^ 1, key0 + kStep, src, len);
-    const bool odd = key0 + kStep > tile_sees && set_odd_aside(lds, b);
+  for (int i = 0; i < n_tiles; ++i) {
+    const int key0 = kv_begin + i * kStep;
+    // Tile i has arrived: behind it there are at most the requests of the tiles after it, and in their place, or behind
+    // them, a spare one.  The first one lies in front of the queries.
+    if (kAhead > 1 && i > 0 && i + kAhead <= n_tiles)
+      wait_vector<kOps * (kAhead > 1 ? kAhead - 1 : 1)>();
+    else if (i > 0)
+      wait_vector<1>();
+    int b = i % kBuffers;
+    if constexpr (kRaw) {
+      b = i % lds.kTiles;
+      int at = lane, from = i % kBuffers;
+      asm volatile("" : "+v"(at));
+      widen_tile(lds, from, b, len - key0, wave, at & 63);
+    }
+    lds_barrier();
+    // nobody reads the buffers any more that the next requests go to
+    auto request_next = [&](const int tile) {
+      if (tile < n_tiles) {
+        request(tile, next_page);
+        next_page = page_of(tile + 1);
+      }
+      if (kAhead == 1 || tile >= n_tiles) request_spare();
+    };
+    if (kAhead > 1 && i == 0) request_next(2);   // queries were there
+    request_next(i + kAhead);
+    const bool odd = key0 + kStep > tile_sees && has_odd(lds, b, wave);
+    if (odd) set_odd_aside<kSrc>(lds, b);
     if (key0 < any_sees) {
-      f32x16 s = {};
-      const char* kb = lds.k[b] + (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s = mfma32(*(const u32x4*)(kb + (i >> 1) * 1024 + (i & 1) * 256), q[i], s);
+      // with one wavefront a SIMD two sums in turns: a product that adds to the last one's result waits for it
+      constexpr int kSums = kDeep ? 2 : 1;
+      f32x16 sums[kSums] = {};
+      constexpr int kReads = kDeep ? 8 : kSrc == SRC_PAGES ? 5 : 4;
+      const char* kb = lds.k[b] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
+      products<kReads>(
+          [&](auto at) {
+            constexpr int j = at.value;
+            if constexpr (kSrc == SRC_ROWS)
+              return *(const u32x4*)(kb + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+            else
+              return *(const u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 256);
+          },
+          [&](auto at, const u32x4 k) { sums[at.value % kSums] = mfma32(k, q[at.value], sums[at.value % kSums]); });
+      f32x16 s = sums[0];
+      if constexpr (kSums == 2) s += sums[kSums - 1];
       const bool masked = key0 + kStep > all_see;
       if (masked) {
 #pragma unroll
@@ -241,105 +438,69 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
         m = next;
         l *= alpha;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] *= alpha;
+        for (int j = 0; j < 8; ++j) o[j] *= alpha;
       }
       const float ref = m == -__builtin_inff() ? 0.f : m;
       u32x4 p[2];
-      float vs[16];
-      if constexpr (kSrc == SRC_PAGES8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 x = *(const f32x4*)&lds.vs[b][8 * i + 4 * h];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
-        }
-      }
+      const char* vs_at = (char*)lds.vs[b] + 16 * h;
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         float x = fast_exp2(__builtin_fmaf(s[r], sl2, -ref)), y = fast_exp2(__builtin_fmaf(s[r + 1], sl2, -ref));
         l += x + y;
-        if constexpr (kSrc == SRC_PAGES8) x *= vs[r], y *= vs[r + 1];
+        if constexpr (kRaw) {
+          const f32x2 vs = *(const f32x2*)(vs_at + 4 * (8 * (r >> 2) + (r & 3)));
+          x *= vs[0], y *= vs[1];
+        }
         p[r >> 3][(r >> 1) & 3] = pack_bf16(x, y);
       }
-      const char* vb = lds.v[b] + h * 256 + (n >> 4) * 512 + (n & 15) * 16;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg)
-          o[i] = mfma32(*(const u32x4*)(vb + pg * kPageBytes + i * 1024), p[pg], o[i]);
+      // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
+      const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
+      const char* vb = lds.v[b] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
+      products<kReads>(
+          [&](auto at) {
+            constexpr int pg = at.value >> 3, j = at.value & 7;
+            if constexpr (kSrc == SRC_ROWS) {
+              const char* from = vb + pg * 8192 + (j >> 1) * 128 + ((4 * (j & 1) + c) ^ v_row_swap(key)) * 16;
+              const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
+              return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+            } else {
+              return *(const u32x4*)(vb + pg * kPageBytes + j * 1024);
+            }
+          },
+          [&](auto at, const u32x4 v) { o[at.value & 7] = mfma32(v, p[at.value >> 3], o[at.value & 7]); });
       if (odd) {
-        const uint32_t* odd_at = lds.odd + 16 * h;
+        auto odd_at = (const __attribute__((address_space(3))) uint32_t*)(lds.odd + 16 * h);
         asm volatile("" : "+v"(odd_at));   // addressed here, and not by registers kept through the loop
         const uint32_t mask = sees - key0 >= kStep ? ~0u : (1u << max(sees - key0, 0)) - 1u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int j = 0; j < 8; ++j) {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int d = 64 * (i >> 1) + 32 * ((r >> 2) & 1) + 4 * (r & 3) + 2 * (i & 1) + (r >> 3);
-            if (odd_at[d] & mask) o[i][r] = __builtin_nanf("");
-          }
+          for (int r = 0; r < 16; ++r)
+            if (odd_at[dim_of<kSrc>(j, r)] & mask) o[j][r] = __builtin_nanf("");
         }
       }
     }
-    if (more) store_tile<kSrc>(lds, st, b ^ 1);
-    __syncthreads();
+    if constexpr (kRaw && !kDeep) lds_barrier();   // one buffer: the next tile is widened into it
   }
 
   l = pair_sum(l);
+  lds_barrier();
   if (part < 0) {
-    const float inv = 1.f / l;
-    char* out = (char*)a.out + (size_t)(tok0 + tok) * a.out_stride + (n & 7) * (kDim * 2) + 32 * h;
-    if (live) {
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          u32x4 x[2];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 4 * half + i;
-            x[i >> 1][2 * (i & 1)] = pack_bf16(o[2 * w][r] * inv, o[2 * w][8 + r] * inv);
-            x[i >> 1][2 * (i & 1) + 1] = pack_bf16(o[2 * w + 1][r] * inv, o[2 * w + 1][8 + r] * inv);
-          }
-          *(u32x4*)(out + 128 * w + 64 * half) = x[0];
-          *(u32x4*)(out + 128 * w + 64 * half + 16) = x[1];
-        }
-      if (a.lse && h == 0)
-        a.lse[(size_t)(tok0 + tok) * kHeads + (n & 7)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    }
-    return;
-  }
-  const size_t row = ((size_t)part + (size_t)tok * n_parts) * kHeads + (n & 7);
-  char* acc = (char*)(a.part_acc + row * kDim) + 32 * h;
-  uint32_t exps = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    float amax = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) amax = fmaxf(amax, fmaxf(fabsf(o[2 * w][r]), fabsf(o[2 * w + 1][r])));
-    amax = pair_max(amax);
-    const int eb = max(24, min(253, (int)(__float_as_uint(amax) >> 23)));   // as in store_part
-    const float up = __uint_as_float((uint32_t)(127 + 14 + 126 - eb) << 23) + (amax - amax);
-    exps |= (uint32_t)((eb - 126) & 0xff) << (8 * w);
-    if (live) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        u32x4 x[2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * half + i;
-          x[i >> 1][2 * (i & 1)] = pack_f16(o[2 * w][r] * up, o[2 * w][8 + r] * up);
-          x[i >> 1][2 * (i & 1) + 1] = pack_f16(o[2 * w + 1][r] * up, o[2 * w + 1][8 + r] * up);
-        }
-        *(u32x4*)(acc + 128 * w + 64 * half) = x[0];
-        *(u32x4*)(acc + 128 * w + 64 * half + 16) = x[1];
-      }
-    }
-  }
-  if (live && h == 0) {
+    uint32_t exps;
+    store_rows<kSrc, true>(o, 1.f / l, exps, (char*)&lds + wave * 8192, (char*)a.out + (size_t)(tok0 + 4 * wave) * a.out_stride,
+                           a.out_stride, n_tok - 4 * wave, lane);
+    if (a.lse && mine < n_tok && h == 0)
+      a.lse[(size_t)(tok0 + mine) * kHeads + (n & 7)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  } else {
+    const size_t part0 = (size_t)part + (size_t)(4 * wave) * n_parts;
+    uint32_t exps = 0;
+    store_rows<kSrc, false>(o, 0.f, exps, (char*)&lds + wave * 8192, (char*)a.part_acc + part0 * (kHeads * kDim * 2),
+                            (size_t)n_parts * (kHeads * kDim * 2), n_tok - 4 * wave, lane);
     if (l != l && m == -__builtin_inff()) m = 0.f;   // NaN throughout is not a row without keys
-    *(f32x4*)(a.part_ml + row * 4) = (f32x4){m, l, __uint_as_float(exps), 0.f};
+    if (mine < n_tok && h == 0)
+      *(f32x4*)(a.part_ml + ((part0 + (size_t)(n >> 3) * n_parts) * kHeads + (n & 7)) * 4) =
+          (f32x4){m, l, __uint_as_float(exps), 0.f};
   }
 }
 
@@ -353,14 +514,28 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(const PrefillArgs a)
   merge_any(m, (size_t)base, np, 0, h, threadIdx.x & 63);
 }
 
+namespace {
+template <int kSrc>
+void launch_source(const PrefillArgs& a, const char* base, const void* second, hipStream_t s) {
+  const PrefillLate late = {a.out, a.lse, a.out_stride, a.tables, a.part_acc, a.part_ml, a.scale};
+  const auto launch = [&](auto kernel) {
+    kernel<<<a.n_work, 256, 0, s>>>(a.work, (const char*)a.q, a.q_stride, base, second, a.k_stride, a.v_stride, late);
+  };
+  if (a.n_work <= kPrefillCus)
+    launch(prefill_kernel<kSrc, true>);
+  else
+    launch(prefill_kernel<kSrc, false>);
+}
+}  // namespace
+
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s) {
   if (a.n_work <= 0) return hipSuccess;
   if (!a.layer_base)
-    prefill_kernel<SRC_ROWS><<<a.n_work, 256, 0, s>>>(a);
+    launch_source<SRC_ROWS>(a, a.k, a.v, s);
   else if (a.scales)
-    prefill_kernel<SRC_PAGES8><<<a.n_work, 256, 0, s>>>(a);
+    launch_source<SRC_PAGES8>(a, a.layer_base, a.scales, s);
   else
-    prefill_kernel<SRC_PAGES><<<a.n_work, 256, 0, s>>>(a);
+    launch_source<SRC_PAGES>(a, a.layer_base, nullptr, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_merge <= 0) return e;
   prefill_merge_kernel<<<2 * a.n_merge, 256, 0, s>>>(a);

@@ -197,6 +197,18 @@ int main() {
       CHECK(oxy_prompt_attention(p, b, rows, 5120, rows, 512, rows, 640, rows, 4096, nullptr, 1.f, nullptr) == OXY_OK);
       CHECK(g_launches == (total > 0));
       if (total) check_work(items, n_part);
+      for (size_t bad : {(size_t)504, (size_t)520, (size_t)1 << 31})
+        for (int which = 0; which < 2 && total > 1; ++which)
+          CHECK(oxy_prompt_attention(p, b, rows, 4096, rows, which ? 512 : bad, rows, which ? bad : 512, rows, 4096, nullptr, 1.f,
+                                     nullptr) == OXY_ERR_INVALID_ARG);
+      for (size_t bad : {(size_t)4080, (size_t)4100})
+        for (int which = 0; which < 2 && total > 1; ++which)
+          CHECK(oxy_prompt_attention(p, b, rows, which ? 4096 : bad, rows, 512, rows, 512, rows, which ? bad : 4096, nullptr, 1.f,
+                                     nullptr) == OXY_ERR_INVALID_ARG);
+      if (total)
+        CHECK(oxy_prompt_attention(p, b, rows + 8, 4096, rows, 512, rows, 512, rows, 4096, nullptr, 1.f, nullptr) == OXY_ERR_INVALID_ARG &&
+              oxy_prompt_attention(p, b, nullptr, 4096, rows, 512, rows, 512, rows, 4096, nullptr, 1.f, nullptr) == OXY_ERR_INVALID_ARG &&
+              oxy_prompt_attention(p, b, rows, 4096, rows, 512, nullptr, 512, rows, 4096, nullptr, 1.f, nullptr) == OXY_ERR_INVALID_ARG);
       CHECK(oxy_stream_append(p, b, 0, rows, rows, nullptr) == OXY_ERR_INVALID_ARG);
       CHECK(oxy_batch_slots(b, slots.data(), 1 << 30) == OXY_ERR_INVALID_ARG);
       CHECK(oxy_prefix_attention(p, b, 0, rows, 4096, rows, 4096, nullptr, 1.f, nullptr) == OXY_ERR_INVALID_ARG);
