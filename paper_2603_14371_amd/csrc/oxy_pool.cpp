@@ -194,10 +194,14 @@ size_t desc_words_of(const oxy_pool_config& c) {
          3 * (size_t)c.max_q_tokens /* part_off, n_parts, fresh runs */;
 }
 
+// Split results that a batch has room for: a prefill needs up to kPrefillTokens for each workgroup that the GPU holds at a
+// time, whatever max_partials is.
+size_t partials_of(const oxy_pool_config& c) { return std::max(c.max_partials, oxy::kPrefillPartials); }
+
 void layout_of(const oxy_pool_config& c, size_t* acc_off, size_t* ml_off, size_t* total) {
   size_t desc = align_up(desc_words_of(c) * 4, 256);
-  size_t acc = align_up((size_t)c.max_partials * oxy::kHeads * oxy::kDim * sizeof(uint16_t), 256);
-  size_t ml = align_up((size_t)c.max_partials * oxy::kHeads * 4 * sizeof(float), 256);
+  size_t acc = align_up(partials_of(c) * oxy::kHeads * oxy::kDim * sizeof(uint16_t), 256);
+  size_t ml = align_up(partials_of(c) * oxy::kHeads * 4 * sizeof(float), 256);
   *acc_off = desc;
   *ml_off = desc + acc;
   *total = desc + acc + ml;
@@ -1709,7 +1713,7 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
       records += t.parts;
       if (t.parts > 1) partials += (int64_t)t.parts * t.n, split = true;
     }
-    if (!split || (records <= c.max_work_items && partials <= c.max_partials)) break;
+    if (!split || (records <= c.max_work_items && partials <= (int64_t)partials_of(c))) break;
   }
   struct Order {
     int32_t steps, tile, part;
@@ -1765,9 +1769,8 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
     if (!p->slots[i].in_use) slot = i;
   if (slot < 0) return fail(OXY_ERR_BUSY, "%s: %d batches alive (max_live_batches)", who, p->live_batches);
   const int64_t n_work = (int64_t)d.work.size() / oxy::kPrefillWords;
-  if (n_work > p->cfg.max_work_items || d.n_partials > p->cfg.max_partials)
-    return fail(OXY_ERR_WORKSPACE, "%s: %lld work items (max_work_items %d), %lld split results (max_partials %d)", who,
-                (long long)n_work, p->cfg.max_work_items, (long long)d.n_partials, p->cfg.max_partials);
+  if (n_work > p->cfg.max_work_items)
+    return fail(OXY_ERR_WORKSPACE, "%s: %lld work items > max_work_items %d", who, (long long)n_work, p->cfg.max_work_items);
   if (d.tables.size() > table_words_of(p->cfg))
     return fail(OXY_ERR_WORKSPACE, "%s: the block tables list %zu entries > %zu (forked prefixes list shared blocks once each)",
                 who, d.tables.size(), table_words_of(p->cfg));

@@ -31,23 +31,22 @@ enum PrefillSource { SRC_PAGES, SRC_PAGES8, SRC_ROWS };
 constexpr int kStep = 32;                       // keys of a tile: two pages
 constexpr int kTileBytes = 2 * kPageBytes;      // of K, or of V
 
-// In 8 bits: codes and exponents as they lie in the pages, a part for each wavefront, which widens what it requested.
-template <bool kDeep>
-struct RawTiles {
-  static constexpr int kTiles = kDeep ? 4 : 1;
-  char codes[kTiles][4][4096];      // [wavefront]: two pieces of 1 KiB of a K page, two of a V page
-  char exps[kTiles][4][256];        // exponents of a page, then nothing
-};
-struct NoTiles {};
-// kDeep: what is in flight.  One workgroup a CU requests three tiles ahead; of two, each requests one.
-template <int kSrc, bool kDeep>
+// Tiles in use and on their way, in rings.  kPipe: one workgroup a CU, see prefill_pipe_kernel; else two.
+template <int kSrc, bool kPipe>
 struct PrefillLds {
-  static constexpr int kTiles = kSrc == SRC_PAGES8 ? (kDeep ? 2 : 1) : kDeep ? 4 : 2;
-  char k[kTiles][kTileBytes], v[kTiles][kTileBytes];
-  float vs[kTiles][kStep];    // in 8 bits: scales of the values
+  static constexpr bool kIs8 = kSrc == SRC_PAGES8;
+  static constexpr int kKeys = kPipe ? (kIs8 ? 2 : 4) : (kIs8 ? 1 : 2), kValues = kPipe ? 4 : kKeys, kRaw = kPipe ? 3 : 1;
+  char k[kKeys][kTileBytes], v[kValues][kTileBytes];
+  float vs[kValues][kStep];   // in 8 bits: scales of the values
   uint32_t odd[kDim];         // keys of a tile whose value is not finite in a dim
   uint32_t found[4];          // [wavefront]: whether it found one
-  std::conditional_t<kSrc == SRC_PAGES8, RawTiles<kDeep>, NoTiles> raw;
+  // In 8 bits: codes and exponents as they lie in the pages, a part for each wavefront, which widens what it requested.
+  struct Raw {
+    char codes[kRaw][4][4096];   // [wavefront]: two pieces of 1 KiB of a K page, two of a V page
+    char exps[kRaw][4][256];     // exponents of a page, then nothing
+  };
+  struct NoRaw {};
+  std::conditional_t<kIs8, Raw, NoRaw> raw;
   uint32_t spare[4][64];      // [wavefront]: what a request in the place of a tile's goes to
 };
 
@@ -69,7 +68,7 @@ __device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, c
 // are such that their ranges are seen.
 template <int n>
 __device__ __forceinline__ void wait_vector() {
-  static_assert(n >= 1 && n < 64, "");
+  static_assert(n >= 0 && n < 64, "");
   __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
 }
 // What a workgroup wrote to LDS before is seen behind it; requests stay in flight (a fence of the workgroup's scope would wait
@@ -86,40 +85,37 @@ __device__ __forceinline__ void lds_barrier() {
 __device__ __forceinline__ int k_row_swap(const int key) { return key & 7; }
 __device__ __forceinline__ int v_row_swap(const int key) { return (key & 1) * 4 + (key >> 1 & 1); }
 
-// A wavefront's part of a tile on its way to LDS, eight operations (five in 8 bits).  blk: the wavefront's page, of rows:
-// nothing.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.
-template <int kSrc, class Lds>
-__device__ __forceinline__ void request_tile(const char* base, const void* second, const size_t k_stride, const size_t v_stride,
-                                             Lds& lds, const int b, const int key0, const int blk, const int src,
-                                             const int len, const int wave, const int lane) {
+// Operation i of the four (in 8 bits five) that bring a wavefront's part of a tile's keys (kWhat 0; in 8 bits keys and values) or
+// values (1) to LDS.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.  blk: the wavefront's page, of rows:
+// nothing.  there: whether there is such a tile; else the buffer is of no bytes.
+template <int kSrc>
+constexpr int kPartOps = kSrc == SRC_PAGES8 ? 5 : 4;
+template <int kSrc, int kWhat, class Lds>
+__device__ __forceinline__ void request_part(const char* base, const void* second, const size_t k_stride, const size_t v_stride,
+                                             Lds& lds, const int i, const int tile, const bool there, const int key0,
+                                             const int blk, const int src, const int len, const int wave, const int lane) {
   const int pg = wave >> 1, side = wave & 1;
   if constexpr (kSrc == SRC_PAGES) {
-    const char* from = base + (size_t)blk * kBlockBytes;
-    const int part = side * (kPageBytes / 2), at = pg * kPageBytes + part;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to_lds<16>(from, kBlockBytes, part + i * 1024 + lane * 16, lds.k[b] + at + i * 1024);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to_lds<16>(from, kBlockBytes, kPageBytes + part + i * 1024 + lane * 16, lds.v[b] + at + i * 1024);
+    char* to = (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + pg * kPageBytes + side * (kPageBytes / 2);
+    to_lds<16>(base + (size_t)blk * kBlockBytes + kWhat * kPageBytes, there ? kPageBytes : 0,
+               side * (kPageBytes / 2) + i * 1024 + lane * 16, to + i * 1024);
   } else if constexpr (kSrc == SRC_PAGES8) {
-    // K chunks of all keys and half of the dims; V chunks of all keys of half of the dims
-    const char* from = base + (size_t)blk * kBlockBytes8;
-    char* to = lds.raw.codes[b][wave];
-    to_lds<16>(from, kBlockBytes8, side * 1024 + lane * 16, to);
-    to_lds<16>(from, kBlockBytes8, side * 1024 + 2048 + lane * 16, to + 1024);
-    to_lds<16>(from, kBlockBytes8, kPageBytes8 + side * 2048 + lane * 16, to + 2048);
-    to_lds<16>(from, kBlockBytes8, kPageBytes8 + side * 2048 + 1024 + lane * 16, to + 3072);
-    to_lds<4>((const char*)second + (size_t)blk * kScaleBytes8, kScaleBytes8, lane * 4, lds.raw.exps[b][wave]);   // 8 lanes, then 0
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {   // two rows at a time
-      const int two = 8 * wave + 2 * (i & 3), key = two + (lane >> 5), c = lane & 31;
-      const int first = min(key0 + two, len - 1);
-      const size_t stride = i < 4 ? k_stride : v_stride;
-      const uint32_t next = first < len - 1 ? (uint32_t)stride : 0;   // the last one again
-      const char* from = (i < 4 ? base : (const char*)second) + (size_t)(src + first) * stride;
-      to_lds<16>(from, next + kDim * 2, (lane >> 5) * next + (c ^ (i < 4 ? k_row_swap(key) : v_row_swap(key))) * 16,
-                 (i < 4 ? lds.k[b] : lds.v[b]) + two * 512);
-    }
+    if (i < 4)   // two K chunks of all keys and half of the dims; two V chunks of all keys of half of the dims
+      to_lds<16>(base + (size_t)blk * kBlockBytes8, there ? kBlockBytes8 : 0,
+                 (i < 2 ? side * 1024 + i * 2048 : kPageBytes8 + side * 2048 + (i - 2) * 1024) + lane * 16,
+                 lds.raw.codes[tile % Lds::kRaw][wave] + i * 1024);
+    else   // 8 lanes, then 0
+      to_lds<4>((const char*)second + (size_t)blk * kScaleBytes8, there ? kScaleBytes8 : 0, lane * 4,
+                lds.raw.exps[tile % Lds::kRaw][wave]);
+  } else {   // two rows
+    const size_t stride = kWhat ? v_stride : k_stride;
+    const int two = 8 * wave + 2 * i, key = two + (lane >> 5);
+    const int first = min(key0 + two, len - 1);
+    const uint32_t next = first < len - 1 ? (uint32_t)stride : 0;   // the last one again
+    const char* from = (kWhat ? (const char*)second : base) + (size_t)(src + first) * stride;
+    to_lds<16>(from, there ? next + kDim * 2 : 0,
+               (lane >> 5) * next + ((lane & 31) ^ (kWhat ? v_row_swap(key) : k_row_swap(key))) * 16,
+               (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + two * 512);
   }
 }
 
@@ -128,53 +124,54 @@ __device__ __forceinline__ u32x2 widen4(const uint32_t codes, const float scale)
   return (u32x2){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))};
 }
-// A wavefront's part of a tile in 8 bits, from codes to the page order of bf16.  Keys with their scale; the scales of the
-// values go into the probabilities (see the kernel), since four keys share a word.  left: keys of the item from the tile's first on.
-template <class Lds>
-__device__ __forceinline__ void widen_tile(Lds& lds, const int r, const int b, const int left, const int wave,
-                                           const int lane) {
-  const int pg = wave >> 1, side = wave & 1;
-  const char* from = lds.raw.codes[r][wave] + lane * 16;
-  char* const kp = lds.k[b] + pg * kPageBytes;
-  char* const vp = lds.v[b] + pg * kPageBytes;
-  const int key = lane & 15;
-  const float s = scale_of((uint8_t)lds.raw.exps[r][wave][k8_scale_offset(key)]);
-  // stale exponents behind the item's end may be infinite: 0 instead
-  const float vs = 16 * pg + key < left ? scale_of((uint8_t)lds.raw.exps[r][wave][v8_scale_offset(key)]) : 0.f;
-  const int n = lane & 15, gp = (lane >> 4) & 1, w = lane >> 5;
-  const char* v_from = lds.raw.codes[r][wave] + 2048 + w * 1024 + (gp * 16 + n) * 16;
-  // all reads before the first write: behind a write the compiler waits for what is on its way to LDS before it reads
-  const u32x4 keys[2] = {*(const u32x4*)from, *(const u32x4*)(from + 1024)};
-  const u32x4 lo = *(const u32x4*)v_from, hi = *(const u32x4*)(v_from + 512);   // keys 4gp.. and 8 + 4gp..
-  if (side == 0 && lane < 16) lds.vs[b][16 * pg + lane] = vs;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const u32x4 x = keys[i];
-    const int ch = 2 * (4 * side + (lane >> 4) + 8 * i);   // eight dims each: ch and ch + 1
-    const u32x2 x0 = widen4(x[0], s), x1 = widen4(x[1], s), x2 = widen4(x[2], s), x3 = widen4(x[3], s);
-    *(u32x4*)(kp + k_chunk_offset(ch >> 2, key >> 3, ch & 3, key & 7)) = (u32x4){x0[0], x0[1], x1[0], x1[1]};
-    *(u32x4*)(kp + k_chunk_offset((ch + 1) >> 2, key >> 3, (ch + 1) & 3, key & 7)) = (u32x4){x2[0], x2[1], x3[0], x3[1]};
+// A wavefront's part of a tile in 8 bits, from codes to the page order of bf16, in nine pieces.  Keys with their scale; the scales
+// of the values go into the probabilities (see the kernels), since four keys share a word.
+struct Widen {
+  u32x4 x[4];
+  float scale;
+  // left: keys of the item from the tile's first on
+  template <int i, class Lds>
+  __device__ __forceinline__ void piece(Lds& lds, const int tile, const int left, const int wave, const int lane) {
+    const int r = tile % Lds::kRaw, pg = wave >> 1, side = wave & 1;
+    const int n = lane & 15, gp = (lane >> 4) & 1, w = lane >> 5;
+    if constexpr (i == 0) {   // all reads before the first write: behind a write the compiler waits for all requests
+      const char* from = lds.raw.codes[r][wave] + lane * 16;
+      const char* v_from = lds.raw.codes[r][wave] + 2048 + w * 1024 + (gp * 16 + n) * 16;
+      scale = scale_of((uint8_t)lds.raw.exps[r][wave][k8_scale_offset(n)]);
+      // stale exponents behind the item's end may be infinite: 0 instead
+      const float vs = 16 * pg + n < left ? scale_of((uint8_t)lds.raw.exps[r][wave][v8_scale_offset(n)]) : 0.f;
+      x[0] = *(const u32x4*)from, x[1] = *(const u32x4*)(from + 1024);
+      x[2] = *(const u32x4*)v_from, x[3] = *(const u32x4*)(v_from + 512);   // keys 4gp.. and 8 + 4gp..
+      if (side == 0 && lane < 16) lds.vs[tile % Lds::kValues][16 * pg + lane] = vs;
+    } else if constexpr (i < 5) {
+      constexpr int half = (i - 1) >> 1, c = (i - 1) & 1;
+      char* const kp = lds.k[tile % Lds::kKeys] + pg * kPageBytes;
+      const int ch = 2 * (4 * side + (lane >> 4) + 8 * half) + c;   // eight dims
+      const u32x2 a = widen4(x[half][2 * c], scale), b = widen4(x[half][2 * c + 1], scale);
+      *(u32x4*)(kp + k_chunk_offset(ch >> 2, n >> 3, ch & 3, n & 7)) = (u32x4){a[0], a[1], b[0], b[1]};
+    } else {
+      char* const vp = lds.v[tile % Lds::kValues] + pg * kPageBytes;
+      const u32x2 a = widen4(x[2][i - 5], 1.f), b = widen4(x[3][i - 5], 1.f);
+      *(u32x4*)(vp + v_chunk_offset(2 * side + w, i - 5, gp, n)) = (u32x4){a[0], a[1], b[0], b[1]};
+    }
   }
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const u32x2 x = widen4(lo[c], 1.f), y = widen4(hi[c], 1.f);
-    *(u32x4*)(vp + v_chunk_offset(2 * side + w, c, gp, n)) = (u32x4){x[0], x[1], y[0], y[1]};
-  }
-}
+};
 
 // A value that a row does not see, or that nothing was written to, must not reach it, and 0 times what is not finite is NaN.
 // In tiles that some row sees a part of, such values are therefore looked for, which costs a barrier.
-__device__ __forceinline__ bool odd_pair(const uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t odd_pair(const uint32_t x) {
+  return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
+}
 template <class Lds>
 __device__ __forceinline__ bool has_odd(Lds& lds, const int b, const int wave) {
   const int t = threadIdx.x & 255;
-  bool odd = false;
+  uint32_t odd = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const u32x4 x = *(const u32x4*)(lds.v[b] + (i * 256 + t) * 16);
-    odd = odd || odd_pair(x[0]) || odd_pair(x[1]) || odd_pair(x[2]) || odd_pair(x[3]);
+    odd |= odd_pair(x[0]) | odd_pair(x[1]) | odd_pair(x[2]) | odd_pair(x[3]);
   }
-  const bool mine = __ballot(odd) != 0;
+  const bool mine = __ballot(odd != 0) != 0;
   if ((t & 63) == 0) lds.found[wave] = mine;
   lds_barrier();
   const u32x4 all = *(const u32x4*)lds.found;
@@ -230,6 +227,19 @@ __device__ __forceinline__ void products(const Read& read, const Multiply& multi
     multiply(j, x[j.value % kAhead]);
     if constexpr (j.value + kAhead < 16) x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
     __builtin_amdgcn_sched_barrier(kAluPasses);
+  });
+}
+// The same with other work in the time that a product takes: between(j) behind product j.
+template <int kAhead, class Read, class Multiply, class Between>
+__device__ __forceinline__ void products_with(const Read& read, const Multiply& multiply, const Between& between) {
+  u32x4 x[kAhead];
+  static_for<kAhead>([&](auto j) { x[j.value] = read(j); });
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<16>([&](auto j) {
+    multiply(j, x[j.value % kAhead]);
+    if constexpr (j.value + kAhead < 16) x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
+    between(j);
+    __builtin_amdgcn_sched_barrier(0);
   });
 }
 
@@ -288,15 +298,13 @@ struct PrefillLate {
   float scale;
 };
 
-template <int kSrc, bool kDeep>
-__global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32_t* work, const char* q_rows, const size_t q_stride,
-                                                                     const char* base, const void* second, const size_t k_stride,
-                                                                     const size_t v_stride, const PrefillLate a) {
+template <int kSrc>
+__global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, const char* q_rows, const size_t q_stride,
+                                                         const char* base, const void* second, const size_t k_stride,
+                                                         const size_t v_stride, const PrefillLate a) {
   constexpr bool kRaw = kSrc == SRC_PAGES8;
-  __shared__ __align__(16) PrefillLds<kSrc, kDeep> lds;
-  constexpr int kBuffers = kRaw ? RawTiles<kDeep>::kTiles : PrefillLds<kSrc, kDeep>::kTiles;   // that requests go to
-  constexpr int kAhead = kRaw && !kDeep ? 1 : kBuffers - 1;                                  // tiles requested ahead
-  constexpr int kOps = kRaw ? 5 : 8;                                                         // of a tile
+  using Lds = PrefillLds<kSrc, false>;
+  __shared__ __align__(16) Lds lds;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6) & 3;
   const int n = lane & 31, h = lane >> 5;
   const DescPtr rec = (DescPtr)work + (size_t)blockIdx.x * kPrefillWords;
@@ -314,8 +322,16 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
   auto request = [&](const int tile, const int blk) {
     int at = lane;
     asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
-    request_tile<kSrc>(base, second, k_stride, v_stride, lds, tile % kBuffers, kv_begin + tile * kStep, blk, src, len, wave,
-                       at & 63);
+    at &= 63;
+    const int key0 = kv_begin + tile * kStep;
+#pragma unroll
+    for (int i = 0; i < kPartOps<kSrc>; ++i)
+      request_part<kSrc, 0>(base, second, k_stride, v_stride, lds, i, tile, true, key0, blk, src, len, wave, at);
+    if constexpr (!kRaw) {
+#pragma unroll
+      for (int i = 0; i < kPartOps<kSrc>; ++i)
+        request_part<kSrc, 1>(base, second, k_stride, v_stride, lds, i, tile, true, key0, blk, src, len, wave, at);
+    }
   };
 
   // a request that is there to be waited behind
@@ -326,36 +342,29 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
   request(0, page_of(0));
 
   // The wavefront's 32 query rows, four tokens' eight heads, come through LDS, as whole lines: a row a lane, as the products
-  // take them, would be 64 pieces of 16 bytes each in a line of its own.  Into buffers that the first tile does not go to.
+  // take them, would be 64 pieces of 16 bytes each in a line of its own.  Half at a time, into buffers that the first tile does
+  // not go to.
   u32x4 q[16];
-  {
-    constexpr int kPasses = kDeep ? 1 : 2, kRows = 32 / kPasses;
-    char* const at = kDeep ? (wave < 2 ? lds.k[lds.kTiles - 2 + (wave & 1)] : lds.v[lds.kTiles - 2 + (wave & 1)])
-                           : (wave < 2 ? lds.k[lds.kTiles - 1] : lds.v[lds.kTiles - 1]) + (wave & 1) * 8192;
+  char* const q_at = (wave < 2 ? lds.k[Lds::kKeys - 1] : lds.v[Lds::kValues - 1]) + (wave & 1) * 8192;
 #pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
+  for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int i = 0; i < kRows / 2; ++i) {
-        const int two = pass * kRows + 2 * i, row = two + (lane >> 5);
-        const char* from = q_rows + (size_t)(tok0 + min(4 * wave + (two >> 3), n_tok - 1)) * q_stride;
-        to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, at + i * 1024);
-      }
-      if (kAhead > 1 && n_tiles > 1) {
-        request(1, page_of(1));
-        wait_vector<kOps>();
-      } else {
-        request_spare();
-        wait_vector<1>();
-      }
-      if (kPasses == 1 || (n >> 4) == pass) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          q[j] = *(const u32x4*)(at + (n & (kRows - 1)) * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int two = half * 16 + 2 * i, row = two + (lane >> 5);
+      const char* from = q_rows + (size_t)(tok0 + min(4 * wave + (two >> 3), n_tok - 1)) * q_stride;
+      to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, q_at + i * 1024);
     }
+    request_spare();
+    wait_vector<1>();
+    if ((n >> 4) == half) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        q[j] = *(const u32x4*)(q_at + (n & 15) * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // read, before the other half comes there
   }
   if constexpr (kRaw) lds_barrier();   // the first tile is widened into where rows were
-  int next_page = page_of(kAhead > 1 ? 2 : 1);
+  int next_page = page_of(1);
 
   // this lane's row
   const int mine = 4 * wave + (n >> 3), tok = min(mine, n_tok - 1);
@@ -377,38 +386,29 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
 
   for (int i = 0; i < n_tiles; ++i) {
     const int key0 = kv_begin + i * kStep;
-    // Tile i has arrived: behind it there are at most the requests of the tiles after it, and in their place, or behind
-    // them, a spare one.  The first one lies in front of the queries.
-    if (kAhead > 1 && i > 0 && i + kAhead <= n_tiles)
-      wait_vector<kOps * (kAhead > 1 ? kAhead - 1 : 1)>();
-    else if (i > 0)
-      wait_vector<1>();
-    int b = i % kBuffers;
+    // Tile i has arrived: behind it there is a spare request.  The first one lies in front of the queries.
+    if (i > 0) wait_vector<1>();
     if constexpr (kRaw) {
-      b = i % lds.kTiles;
-      int at = lane, from = i % kBuffers;
+      int at = lane;
       asm volatile("" : "+v"(at));
-      widen_tile(lds, from, b, len - key0, wave, at & 63);
+      at &= 63;
+      Widen widen;
+      static_for<9>([&](auto j) { widen.template piece<j.value>(lds, i, len - key0, wave, at); });
     }
     lds_barrier();
     // nobody reads the buffers any more that the next requests go to
-    auto request_next = [&](const int tile) {
-      if (tile < n_tiles) {
-        request(tile, next_page);
-        next_page = page_of(tile + 1);
-      }
-      if (kAhead == 1 || tile >= n_tiles) request_spare();
-    };
-    if (kAhead > 1 && i == 0) request_next(2);   // queries were there
-    request_next(i + kAhead);
-    const bool odd = key0 + kStep > tile_sees && has_odd(lds, b, wave);
-    if (odd) set_odd_aside<kSrc>(lds, b);
+    if (i + 1 < n_tiles) {
+      request(i + 1, next_page);
+      next_page = page_of(i + 2);
+    }
+    request_spare();
+    const int bk = i % Lds::kKeys, bv = i % Lds::kValues;
+    const bool odd = key0 + kStep > tile_sees && has_odd(lds, bv, wave);
+    if (odd) set_odd_aside<kSrc>(lds, bv);
     if (key0 < any_sees) {
-      // with one wavefront a SIMD two sums in turns: a product that adds to the last one's result waits for it
-      constexpr int kSums = kDeep ? 2 : 1;
-      f32x16 sums[kSums] = {};
-      constexpr int kReads = kDeep ? 8 : kSrc == SRC_PAGES ? 5 : 4;
-      const char* kb = lds.k[b] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
+      f32x16 s = {};
+      constexpr int kReads = kSrc == SRC_PAGES ? 5 : 4;
+      const char* kb = lds.k[bk] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int j = at.value;
@@ -417,9 +417,7 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
             else
               return *(const u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 256);
           },
-          [&](auto at, const u32x4 k) { sums[at.value % kSums] = mfma32(k, q[at.value], sums[at.value % kSums]); });
-      f32x16 s = sums[0];
-      if constexpr (kSums == 2) s += sums[kSums - 1];
+          [&](auto at, const u32x4 k) { s = mfma32(k, q[at.value], s); });
       const bool masked = key0 + kStep > all_see;
       if (masked) {
 #pragma unroll
@@ -442,7 +440,7 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
       }
       const float ref = m == -__builtin_inff() ? 0.f : m;
       u32x4 p[2];
-      const char* vs_at = (char*)lds.vs[b] + 16 * h;
+      const char* vs_at = (char*)lds.vs[bv] + 16 * h;
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         float x = fast_exp2(__builtin_fmaf(s[r], sl2, -ref)), y = fast_exp2(__builtin_fmaf(s[r + 1], sl2, -ref));
@@ -455,7 +453,7 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
       }
       // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
       const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
-      const char* vb = lds.v[b] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
+      const char* vb = lds.v[bv] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int pg = at.value >> 3, j = at.value & 7;
@@ -476,13 +474,290 @@ __global__ __launch_bounds__(256, kDeep ? 1 : 2) void prefill_kernel(const int32
         for (int j = 0; j < 8; ++j) {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (odd_at[dim_of<kSrc>(j, r)] & mask) o[j][r] = __builtin_nanf("");
+          for (int r = 0; r < 16; ++r) {
+            float x = odd_at[dim_of<kSrc>(j, r)] & mask ? __builtin_nanf("") : o[j][r];
+            asm volatile("" : "+v"(x));   // chosen here, and not where this path meets the other one
+            o[j][r] = x;
+          }
         }
       }
     }
-    if constexpr (kRaw && !kDeep) lds_barrier();   // one buffer: the next tile is widened into it
+    if constexpr (kRaw) lds_barrier();   // one buffer: the next tile is widened into it
   }
+
+  l = pair_sum(l);
+  lds_barrier();
+  if (part < 0) {
+    uint32_t exps;
+    store_rows<kSrc, true>(o, 1.f / l, exps, (char*)&lds + wave * 8192, (char*)a.out + (size_t)(tok0 + 4 * wave) * a.out_stride,
+                           a.out_stride, n_tok - 4 * wave, lane);
+    if (a.lse && mine < n_tok && h == 0)
+      a.lse[(size_t)(tok0 + mine) * kHeads + (n & 7)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  } else {
+    const size_t part0 = (size_t)part + (size_t)(4 * wave) * n_parts;
+    uint32_t exps = 0;
+    store_rows<kSrc, false>(o, 0.f, exps, (char*)&lds + wave * 8192, (char*)a.part_acc + part0 * (kHeads * kDim * 2),
+                            (size_t)n_parts * (kHeads * kDim * 2), n_tok - 4 * wave, lane);
+    if (l != l && m == -__builtin_inff()) m = 0.f;   // NaN throughout is not a row without keys
+    if (mine < n_tok && h == 0)
+      *(f32x4*)(a.part_ml + ((part0 + (size_t)(n >> 3) * n_parts) * kHeads + (n & 7)) * 4) =
+          (f32x4){m, l, __uint_as_float(exps), 0.f};
+  }
+}
+
+// One workgroup a CU, one wavefront a SIMD: what a wavefront computes by its vector instructions it does while its matrix
+// products run.  Around tile i: the products of tile i - 1's values, and meanwhile the maxima of tile i's logits; then the
+// products of tile i + 1's keys, and meanwhile the exponentials of tile i.
+template <int kSrc>
+__global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* work, const char* q_rows, const size_t q_stride,
+                                                              const char* base, const void* second, const size_t k_stride,
+                                                              const size_t v_stride, const PrefillLate a) {
+  constexpr bool kRaw = kSrc == SRC_PAGES8;
+  using Lds = PrefillLds<kSrc, true>;
+  __shared__ __align__(16) Lds lds;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6) & 3;
+  const int n = lane & 31, h = lane >> 5;
+  const DescPtr rec = (DescPtr)work + (size_t)blockIdx.x * kPrefillWords;
+  const int tok0 = rec[F_TOK0], n_tok = rec[F_N_TOK], pos = rec[F_POS], full = rec[F_FULL];
+  const int kv_begin = rec[F_BEGIN], kv_end = rec[F_END], src = rec[F_SRC], part = rec[F_PART], n_parts = rec[F_N_PARTS],
+            len = rec[F_LEN];
+  const int n_tiles = (kv_end - kv_begin + kStep - 1) / kStep;
+
+  // the wavefront's page of a tile
+  auto page_of = [&](const int tile) {
+    if constexpr (kSrc == SRC_ROWS) return 0;
+    const int at = 2 * tile + (wave >> 1), page = min((kv_begin >> 4) + at, (len - 1) >> 4);
+    return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[src + page];
+  };
+  // Tiles behind the last one are requested too, as buffers of no bytes: every step has as many operations as every other.
+  auto request_one = [&](auto what, const int i, const int tile, const int blk) {
+    int at = lane;
+    asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
+    request_part<kSrc, what.value>(base, second, k_stride, v_stride, lds, i, tile, tile < n_tiles, kv_begin + tile * kStep, blk,
+                                   src, len, wave, at & 63);
+  };
+  auto request = [&](auto what, const int tile, const int blk) {
+    static_for<kPartOps<kSrc>>([&](auto i) { request_one(what, i.value, tile, blk); });
+  };
+  constexpr std::integral_constant<int, 0> kKeys;
+  constexpr std::integral_constant<int, 1> kValues;
+  to_lds<4>(work + (size_t)blockIdx.x * kPrefillWords, kPrefillWords * 4, lane * 4, lds.spare[wave]);   // see wait_vector
+  int page[3];   // of the next tiles whose values are requested
+  page[0] = page_of(0);
+  page[1] = page_of(1);
+  request(kKeys, 0, page[0]);
+
+  // The wavefront's 32 query rows, four tokens' eight heads, come through LDS, as whole lines: a row a lane, as the products
+  // take them, would be 64 pieces of 16 bytes each in a line of its own.
+  u32x4 q[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int row = 2 * i + (lane >> 5);
+    const char* from = q_rows + (size_t)(tok0 + min(4 * wave + (i >> 2), n_tok - 1)) * q_stride;
+    to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, lds.v[wave] + i * 1024);
+  }
+  request(kKeys, 1, page[1]);
+  page[2] = page_of(2);
+  if constexpr (kRaw) {
+    request(kKeys, 2, page[2]);
+    wait_vector<10>();
+  } else {
+    wait_vector<4>();
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j)
+    q[j] = *(const u32x4*)(lds.v[wave] + n * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+  lds_barrier();   // values go to where rows were
+  int next_page = page_of(3);
+  Widen widen;
+  auto widen_piece = [&](const int tile, auto piece) {
+    if constexpr (kRaw) {
+      int at = lane;
+      asm volatile("" : "+v"(at));
+      widen.template piece<piece.value>(lds, tile, len - kv_begin - tile * kStep, wave, at & 63);
+    }
+  };
+  auto widen_all = [&](const int tile) { static_for<9>([&](auto i) { widen_piece(tile, i); }); };
+  if constexpr (kRaw) {
+    widen_all(0);
+    request(kKeys, 3, next_page);
+    next_page = page_of(4);
+    wait_vector<10>();
+    widen_all(1);
+    request(kKeys, 4, next_page);
+    next_page = page_of(5);
+    lds_barrier();
+  } else {
+    request(kKeys, 2, page[2]);
+    request(kValues, 0, page[0]);
+    request(kKeys, 3, next_page);
+    request(kValues, 1, page[1]);
+    page[0] = page[2];
+    page[1] = next_page;
+    next_page = page_of(4);
+  }
+
+  // this lane's row
+  const int mine = 4 * wave + (n >> 3), tok = min(mine, n_tok - 1);
+  const int sees = min(len, max(pos + tok + 1, full));   // keys below
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+  for (int s = 0; s < 16; ++s) q[s] ^= (u32x4){flip, flip, flip, flip};
+  float sl2 = fabsf(a.scale * 1.4426950408889634f);
+  if (sl2 == 0.f) sl2 = 0x1p-120f;
+
+  // keys that all rows of the workgroup see; that all rows of the wavefront see
+  const int tile_sees = min(len, max(pos + 1, full));
+  const int all_see = min(len, max(pos + min(4 * wave, n_tok - 1) + 1, full));
+
+  f32x16 o[8] = {}, s = {};
+  float m = -__builtin_inff(), l = 0.f;
+  u32x4 p[2] = {};
+
+  constexpr int kReads = 4;
+  auto read_key = [&](const char* kb, auto at) {
+    constexpr int j = at.value;
+    if constexpr (kSrc == SRC_ROWS)
+      return *(const u32x4*)(kb + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+    else
+      return *(const u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 256);
+  };
+  auto keys_at = [&](const int tile) {
+    return lds.k[tile % Lds::kKeys] +
+           (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
+  };
+  // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
+  const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
+  // products of a tile's values, and between them what there is to do
+  auto add_values = [&](const int tile, const auto& between) {
+    const char* vb = lds.v[tile % Lds::kValues] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
+    products_with<kReads>(
+        [&](auto at) {
+          constexpr int pg = at.value >> 3, j = at.value & 7;
+          if constexpr (kSrc == SRC_ROWS) {
+            const char* from = vb + pg * 8192 + (j >> 1) * 128 + ((4 * (j & 1) + c) ^ v_row_swap(key)) * 16;
+            const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
+            return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+          } else {
+            return *(const u32x4*)(vb + pg * kPageBytes + j * 1024);
+          }
+        },
+        [&](auto at, const u32x4 v) { o[at.value & 7] = mfma32(v, p[at.value >> 3], o[at.value & 7]); }, between);
+  };
+  auto mark_odd = [&](const int tile) {
+    const int key0 = kv_begin + tile * kStep;
+    auto odd_at = (const __attribute__((address_space(3))) uint32_t*)(lds.odd + 16 * h);
+    asm volatile("" : "+v"(odd_at));   // addressed here, and not by registers kept through the loop
+    const uint32_t mask = sees - key0 >= kStep ? ~0u : (1u << max(sees - key0, 0)) - 1u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = odd_at[dim_of<kSrc>(j, r)] & mask ? __builtin_nanf("") : o[j][r];
+        asm volatile("" : "+v"(x));   // chosen here, and not where this path meets the other one
+        o[j][r] = x;
+      }
+    }
+  };
+  // by all wavefronts
+  auto odd_of_tile = [&](const int tile) {
+    if (kv_begin + (tile + 1) * kStep <= tile_sees) return false;
+    const bool odd = has_odd(lds, tile % Lds::kValues, wave);
+    if (odd) set_odd_aside<kSrc>(lds, tile % Lds::kValues);
+    return odd;
+  };
+
+  // products of a tile's keys, also of one that is not there, and between them what there is to do
+  auto logits = [&](const int tile, const auto& between) {
+    f32x16 sum = {};
+    const char* kb = keys_at(tile);
+    products_with<kReads>([&](auto at) { return read_key(kb, at); },
+                          [&](auto at, const u32x4 k) { sum = mfma32(k, q[at.value], sum); }, between);
+    s = sum;
+  };
+  // What was requested three steps ago (in 8 bits: what the last one requested three steps ago) has arrived, and nobody reads any
+  // more what the step before last read.
+  auto step = [&](const int i) {
+    wait_vector<kRaw ? 10 : 16>();
+    lds_barrier();
+    if constexpr (!kRaw) {
+      request(kKeys, i + 4, next_page);
+      request(kValues, i + 2, page[0]);
+      page[0] = page[1];
+      page[1] = next_page;
+      next_page = page_of(i + 5);
+    }
+  };
+  auto mask = [&](const int i) {
+    const int key0 = kv_begin + i * kStep;
+    if (key0 + kStep > all_see) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = key0 + 8 * (r >> 2) + 4 * h + (r & 3) < sees ? s[r] : -__builtin_inff();
+    }
+  };
+  float top;
+  auto raise = [&](auto at) {
+    if constexpr (at.value & 1) top = fmaxf(fmaxf(top, s[at.value - 1]), s[at.value]);
+  };
+  // the exponentials of tile i, and the logits of the next one; in 8 bits, where tile i + 2 has been widened, the request of the
+  // one that takes its place
+  auto weigh_and_go_on = [&](const int i) {
+    const float ref = m == -__builtin_inff() ? 0.f : m;
+    const char* vs_at = (char*)lds.vs[i % Lds::kValues] + 16 * h;
+    const f32x16 now = s;
+    float x[16];
+    logits(i + 1, [&](auto at) {
+      constexpr int j = at.value;
+      x[j] = fast_exp2(__builtin_fmaf(now[j], sl2, -ref));
+      if constexpr (j & 1) {
+        float x0 = x[j - 1], x1 = x[j];
+        l += x0 + x1;
+        if constexpr (kRaw) {
+          const f32x2 vs = *(const f32x2*)(vs_at + 4 * (8 * (j >> 2) + (j & 2)));
+          x0 *= vs[0], x1 *= vs[1];
+        }
+        p[j >> 3][(j >> 1) & 3] = pack_bf16(x0, x1);
+      }
+      if constexpr (kRaw && j % 3 == 1) request_one(kKeys, j / 3, i + 5, next_page);
+    });
+    if constexpr (kRaw) next_page = page_of(i + 6);
+  };
+
+  logits(0, [](auto) {});
+  step(0);
+  widen_all(2);
+  mask(0);
+  top = -__builtin_inff();
+  static_for<16>(raise);
+  m = pair_max(top) * sl2;
+  weigh_and_go_on(0);
+  for (int i = 1; i < n_tiles; ++i) {
+    step(i);
+    const bool odd = odd_of_tile(i - 1);
+    mask(i);
+    top = -__builtin_inff();
+    add_values(i - 1, [&](auto j) {
+      raise(j);
+      if constexpr (j.value == 0 || (j.value >= 4 && j.value < 12)) widen_piece(i + 2, std::integral_constant<int, j.value == 0 ? 0 : j.value - 3>());
+    });
+    if (odd) mark_odd(i - 1);
+    top = pair_max(top) * sl2;
+    if (__ballot(top > m + kGrow)) {
+      const float next = top > m + kGrow ? top : m;   // a row's reference does not go by other rows
+      const float alpha = next == m ? 1.f : fast_exp2(m - next);
+      m = next;
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] *= alpha;
+    }
+    weigh_and_go_on(i);
+  }
+  wait_vector<0>();   // the last tile's values, and requests of no bytes, which write zeros
+  lds_barrier();
+  const bool odd = odd_of_tile(n_tiles - 1);
+  add_values(n_tiles - 1, [](auto) {});
+  if (odd) mark_odd(n_tiles - 1);
 
   l = pair_sum(l);
   lds_barrier();
@@ -522,9 +797,9 @@ void launch_source(const PrefillArgs& a, const char* base, const void* second, h
     kernel<<<a.n_work, 256, 0, s>>>(a.work, (const char*)a.q, a.q_stride, base, second, a.k_stride, a.v_stride, late);
   };
   if (a.n_work <= kPrefillCus)
-    launch(prefill_kernel<kSrc, true>);
+    launch(prefill_pipe_kernel<kSrc>);
   else
-    launch(prefill_kernel<kSrc, false>);
+    launch(prefill_kernel<kSrc>);
 }
 }  // namespace
 

@@ -155,7 +155,7 @@ int main() {
       CHECK(oxy_prefix_batch_build(p, ask.data(), (int)ask.size(), 0, nullptr, &b) == OXY_OK);
       int32_t n_tok, n_work, n_part;
       CHECK(oxy_batch_info(b, nullptr, &n_tok, &n_work, &n_part) == OXY_OK);
-      CHECK(n_part <= (c.max_partials ? c.max_partials : 32 * c.max_q_tokens));
+      CHECK(n_part <= std::max(kPrefillPartials, c.max_partials ? c.max_partials : 32 * c.max_q_tokens));
       std::vector<int64_t> slots(n_tok);
       CHECK(oxy_batch_slots(b, slots.data(), n_tok) == OXY_OK);
       size_t at = 0;
