@@ -133,7 +133,7 @@ struct oxy_batch {
   int32_t n_fresh = 0;    // blocks of items whose own-phase tiles read k_new / v_new (folded append)
   int32_t off_fresh = 0;
   int32_t max_parts = 0;  // most split results of a token
-  int32_t n_long = 0;     // in 8 bits: tokens of more than kLongParts
+  int32_t n_long = 0;     // in 8 bits: tokens of more than kLongParts; of a prefill: of more than kMergeLong
   int32_t off_long = 0;
   int32_t n_merge = 0;    // of a prefill: tokens with split results
   int32_t off_merges = 0;
@@ -1683,12 +1683,22 @@ struct PrefillItem {
   int32_t src;   // F_SRC of its records
 };
 
-// Work list of a prefill: records in `work`, tokens with split results in `merges`; returns how many split results there are.
+// Work list of a prefill: records in `work`, tokens with split results in `merges`, the n_long with most of them first; returns
+// how many split results there are.
 //
-// A record is up to 16 query tokens of an item and a part of the keys that they see.  kSlots workgroups are resident, two on each of 256 CUs.
+// A record is up to 16 query tokens of an item and a part of the keys that they see, in steps of 32.  A split costs a write and a
+// read of the split results, an idle CU the same time to all.  256 records have a CU each, 512 half of one (us a layer, launches
+// included, by records):
+//   one prefix of 288, 1 new token       5 records 13.0   9 10.0   14 9.3   27 9.2
+//   two prompts of 410                 104 30.5   156 26.6   208 24.6   364 24.1
+//   4 prefixes, 256 new of 960          64 33.6   192 24.2   256 24.8   320 26.4   448 27.9
+//   2048 new of a prefix              176 71.2   240 51.7   320 40.0   476 39.2
+//   1024 new of 69760                 256 618   384 603   512 526   577 685   768 613
+// So a record has at least two steps; work of up to 8 steps a CU goes to at most 256 records, more of it to 512, and one record
+// above that would be a second round.
 int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
-                     std::vector<int32_t>* merges) {
-  constexpr int32_t kSlots = 512, kStepKeys = 32, kLeastSteps = 4;
+                     std::vector<int32_t>* merges, int32_t* n_long) {
+  constexpr int32_t kStepKeys = 32, kLeastSteps = 2, kFewSteps = 8;
   struct Tile {
     const PrefillItem* it;
     int32_t first, n, keys, parts;   // tokens of the item, keys that the last of them sees
@@ -1702,19 +1712,30 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
       tiles.push_back({&it, t, n, keys, 1});
       steps += (keys + kStepKeys - 1) / kStepKeys;
     }
-  int64_t partials = 0;
-  for (int64_t most = std::max<int64_t>(kLeastSteps, (steps + kSlots - 1) / kSlots);; most *= 2) {
-    int64_t records = 0;
-    bool split = false;
-    partials = 0;
+  int64_t records = 0, partials = 0;
+  const auto split = [&](const int64_t most) {   // parts of at most this many steps
+    records = partials = 0;
     for (Tile& t : tiles) {
-      const int32_t n = (t.keys + kStepKeys - 1) / kStepKeys;
-      t.parts = (int32_t)((n + most - 1) / most);
+      t.parts = (int32_t)(((t.keys + kStepKeys - 1) / kStepKeys + most - 1) / most);
       records += t.parts;
-      if (t.parts > 1) partials += (int64_t)t.parts * t.n, split = true;
+      if (t.parts > 1) partials += (int64_t)t.parts * t.n;
     }
-    if (!split || (records <= c.max_work_items && partials <= (int64_t)partials_of(c))) break;
-  }
+  };
+  const int64_t n_tiles = (int64_t)tiles.size();
+  const int64_t slots = steps <= kFewSteps * oxy::kPrefillCus ? oxy::kPrefillCus : 2 * oxy::kPrefillCus;
+  // The fewest steps with at most `slots` records, which (steps / most + tiles) bounds; with more tiles than that, parts of a
+  // slot's share of the steps.
+  int64_t most = std::max<int64_t>(kLeastSteps, (steps + slots - 1) / slots);
+  if (n_tiles < slots)
+    for (int64_t high = std::max(most, (steps + slots - n_tiles - 1) / (slots - n_tiles)); most < high;) {
+      const int64_t mid = (most + high) / 2;
+      split(mid);
+      if (records <= slots)
+        high = mid;
+      else
+        most = mid + 1;
+    }
+  for (split(most); partials > 0 && (records > c.max_work_items || partials > (int64_t)partials_of(c)); split(most)) most *= 2;
   struct Order {
     int32_t steps, tile, part;
   };
@@ -1726,16 +1747,19 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
   std::stable_sort(order.begin(), order.end(), [](const Order& x, const Order& y) { return x.steps > y.steps; });
   std::vector<int32_t> part0(tiles.size(), -1);
   int32_t next = 0;
-  for (size_t i = 0; i < tiles.size(); ++i) {
-    const Tile& t = tiles[i];
-    if (t.parts == 1) continue;
-    part0[i] = next;
-    for (int32_t k = 0; k < t.n; ++k) {
-      const int32_t m[oxy::kMergeWords] = {t.it->tok0 + t.first + k, next, t.parts};
-      merges->insert(merges->end(), m, m + oxy::kMergeWords);
-      next += t.parts;
+  *n_long = 0;
+  for (const bool many : {true, false})
+    for (size_t i = 0; i < tiles.size(); ++i) {
+      const Tile& t = tiles[i];
+      if (t.parts == 1 || (t.parts > oxy::kMergeLong) != many) continue;
+      part0[i] = next;
+      for (int32_t k = 0; k < t.n; ++k) {
+        const int32_t m[oxy::kMergeWords] = {t.it->tok0 + t.first + k, next, t.parts};
+        merges->insert(merges->end(), m, m + oxy::kMergeWords);
+        next += t.parts;
+      }
+      if (many) *n_long += t.n;
     }
-  }
   for (const Order& o : order) {
     const Tile& t = tiles[o.tile];
     const int64_t n = (t.keys + kStepKeys - 1) / kStepKeys;
@@ -1761,6 +1785,7 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
 struct PrefillDesc {
   std::vector<int32_t> work, slots, merges, tables;
   int64_t n_partials = 0;
+  int32_t n_long = 0;
 };
 int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_items, int32_t n_tokens, PrefillDesc& d,
                       void* hip_stream, const char* who, oxy_batch** out) {
@@ -1790,6 +1815,7 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
   b->n_work = b->n_launch = (int32_t)n_work;
   b->n_partials = (int32_t)d.n_partials;
   b->n_merge = (int32_t)(d.merges.size() / oxy::kMergeWords);
+  b->n_long = d.n_long;
   b->off_slots = (int32_t)d.work.size();
   b->off_merges = b->off_slots + (int32_t)d.slots.size();
   b->off_tables = b->off_merges + (int32_t)d.merges.size();
@@ -1870,7 +1896,7 @@ int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_i
     tok0 += pl.n_new;
     words += blocks_for(len);
   }
-  if (!append_only) d.n_partials = plan_prefill(c, work, &d.work, &d.merges);
+  if (!append_only) d.n_partials = plan_prefill(c, work, &d.work, &d.merges, &d.n_long);
   d.slots.reserve(n_tokens);
   // blocks are taken in item order; what fails from here on gives them back in reverse order of their pops
   size_t done = 0;
@@ -1924,7 +1950,7 @@ int32_t prompt_batch_impl(oxy_pool* p, const oxy_prompt* prompts, int32_t n_prom
     work.push_back({at, 0, it.n_tokens, std::min(it.n_full, it.n_tokens), it.n_tokens, at});
     n_tokens += it.n_tokens;
   }
-  d.n_partials = plan_prefill(p->cfg, work, &d.work, &d.merges);
+  d.n_partials = plan_prefill(p->cfg, work, &d.work, &d.merges, &d.n_long);
   return prefill_batch(p, BATCH_PROMPT, 0, n_prompts, (int32_t)n_tokens, d, hip_stream, "prompt_batch_build", out);
 }
 
@@ -1945,6 +1971,7 @@ oxy::PrefillArgs prefill_args(const oxy_pool* p, const oxy_batch* b, const void*
   a.part_ml = (float*)(ds.d_base + p->ml_offset);
   a.n_work = b->n_launch;
   a.n_merge = b->n_merge;
+  a.n_long = b->n_long;
   a.scale = scale;
   return a;
 }

@@ -27,6 +27,8 @@ constexpr int32_t kPrefillPartials = 512 * kPrefillTokens;
 constexpr int kPrefillCus = 256;
 // Words of the merge list for each token that has split results: the token, its first one, how many.
 constexpr int kMergeWords = 3;
+// Tokens with more split results than this are first in the merge list, and a workgroup joins those of one head.
+constexpr int kMergeLong = 16;
 
 struct PrefillArgs {
   const void* q;             // token t, head h at q + t * q_stride + h * 512
@@ -42,7 +44,7 @@ struct PrefillArgs {
   size_t k_stride, v_stride;
   uint16_t* part_acc;        // as in AttnArgs
   float* part_ml;
-  int32_t n_work, n_merge;
+  int32_t n_work, n_merge, n_long;   // n_long: tokens with more than kMergeLong split results
   float scale;
 };
 OXY_WEAK hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s);

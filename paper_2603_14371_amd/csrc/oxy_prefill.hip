@@ -11,6 +11,8 @@
 
 namespace oxy {
 
+constexpr int kMergeWaves = kHeads;   // of a workgroup
+
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
@@ -779,14 +781,75 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   }
 }
 
-// A wavefront per token and head, four heads a workgroup.
-__global__ __launch_bounds__(256) void prefill_merge_kernel(const PrefillArgs a) {
-  const DescPtr rec = (DescPtr)a.merges + (size_t)(blockIdx.x >> 1) * kMergeWords;
+// Joins split results by their (m, l), see merge_head.  A wavefront per token and head, or, where a token has more than sixteen of
+// them, a workgroup: a wavefront's sixteen at a time would be a round trip each.
+__device__ __forceinline__ void merge_long(const MergeArgs& a, const size_t base, const int np, const int h, const int wave,
+                                           const int lane) {
+  __shared__ __align__(16) f32x4 sums[kMergeWaves][64];
+  __shared__ float ml_of[kMergeWaves][2];
+  const int i = lane & 15, q = lane >> 4;
+  const char* ml = (const char*)(a.part_ml + (base * kHeads + h) * 4);
+  const char* acc = (const char*)(a.part_acc + (base * kHeads + h) * kDim);
+  constexpr uint32_t kMlStride = kHeads * 4 * sizeof(float), kAccStride = kHeads * kDim * sizeof(uint16_t);
+  const int end = np * (wave + 1) / kMergeWaves;
+  float big = -__builtin_inff(), total = 0.f;
+  f32x4 o = {};
+  for (int p0 = np * wave / kMergeWaves; p0 < end; p0 += 16) {
+    const f32x4 w = *(const f32x4*)(ml + (uint32_t)min(p0 + i, end - 1) * kMlStride);
+    u32x2 x[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      x[u] = __builtin_nontemporal_load((const u32x2*)(acc + (size_t)min(p0 + u, end - 1) * kAccStride + (uint32_t)lane * 8u));
+    const float next = fmaxf(big, lanes16_max(w[0]));
+    const float alpha = big == next ? 1.f : fast_exp2(big - next);
+    big = next;
+    const bool live = p0 + i < end && w[0] != -__builtin_inff();
+    const float wgt = live ? fast_exp2(w[0] - big) : 0.f;
+    total = total * alpha + lanes16_sum(wgt * (live ? w[1] : 0.f));
+    o *= alpha;
+    const int ex = (int32_t)(__float_as_uint(w[2]) << (24 - 8 * q)) >> 24;   // signed byte q
+    const float ws = __builtin_amdgcn_ldexpf(wgt, ex - 14);
+    static_for<16>([&](auto u) {
+      const float wu = __uint_as_float(
+          __builtin_amdgcn_update_dpp(0, __float_as_uint(ws), kRowBcast0 + u.value, 0xf, 0xf, false));
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float lo, hi;
+        unpack_f16(x[u.value][k], lo, hi);
+        o[2 * k] = __builtin_fmaf(wu, lo, o[2 * k]);
+        o[2 * k + 1] = __builtin_fmaf(wu, hi, o[2 * k + 1]);
+      }
+    });
+  }
+  sums[wave][lane] = o;
+  if (lane == 0) ml_of[wave][0] = big, ml_of[wave][1] = total;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < kMergeWaves; ++w) big = fmaxf(big, ml_of[w][0]);
+  total = 0.f;
+  o = (f32x4){};
+#pragma unroll
+  for (int w = 0; w < kMergeWaves; ++w) {
+    const float m = ml_of[w][0], wgt = m == -__builtin_inff() ? 0.f : fast_exp2(m - big);
+    total = __builtin_fmaf(wgt, ml_of[w][1], total);
+    o += wgt * sums[w][lane];
+  }
+  const float inv = 1.f / total;
+  *(u32x2*)((uint16_t*)a.out + h * kDim + 4 * lane) = (u32x2){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+  if (a.lse && lane == 0) a.lse[h] = (big + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+}
+__global__ __launch_bounds__(64 * kMergeWaves) void prefill_merge_kernel(const PrefillArgs a) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x;
+  const bool wide = b < kHeads * a.n_long;
+  const DescPtr rec = (DescPtr)a.merges + (size_t)(wide ? b / kHeads : b - (kHeads - 1) * a.n_long) * kMergeWords;
   const int tok = rec[0], base = rec[1], np = rec[2];
-  const int h = 4 * (blockIdx.x & 1) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const MergeArgs m = {a.part_acc, a.part_ml, (char*)a.out + (size_t)tok * a.out_stride,
                        a.lse ? a.lse + (size_t)tok * kHeads : nullptr, nullptr, nullptr};
-  merge_any(m, (size_t)base, np, 0, h, threadIdx.x & 63);
+  if (wide)
+    merge_long(m, (size_t)base, np, b % kHeads, wave, lane);
+  else
+    merge_any(m, (size_t)base, np, 0, wave, lane);
 }
 
 namespace {
@@ -813,7 +876,7 @@ hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s) {
     launch_source<SRC_PAGES>(a, a.layer_base, nullptr, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_merge <= 0) return e;
-  prefill_merge_kernel<<<2 * a.n_merge, 256, 0, s>>>(a);
+  prefill_merge_kernel<<<a.n_merge + (kHeads - 1) * a.n_long, 64 * kMergeWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 
