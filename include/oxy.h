@@ -326,7 +326,7 @@ typedef struct {
 int32_t oxy_prompt_batch_build(oxy_pool *pool, const oxy_prompt *prompts, int32_t n_prompts,
                                void *hip_stream, oxy_batch **out);
 /* q, out, lse, scale as oxy_prefix_attention; token t's key and value, 256 bf16 each, at k + t * k_stride and
- * v + t * v_stride (DEVICE; bytes, 16-byte aligned, at least 512 and below 2 GiB).  Without tokens nothing is done, whatever the pointers
+ * v + t * v_stride (DEVICE; bytes, 16-byte aligned, at least 512 and below 256 MiB).  Without tokens nothing is done, whatever the pointers
  * are.  out must not overlap q, k or v. */
 int32_t oxy_prompt_attention(oxy_pool *pool, const oxy_batch *batch, const void *q, size_t q_stride,
                              const void *k, size_t k_stride, const void *v, size_t v_stride, void *out,

@@ -2035,8 +2035,8 @@ int32_t oxy_prompt_attention(oxy_pool* p, const oxy_batch* b, const void* q, siz
   if (bad_rows(q, q_stride, oxy::kHeads, b->n_tokens) || bad_rows(out, out_stride, oxy::kHeads, b->n_tokens) ||
       bad_rows(k, k_stride, 1, b->n_tokens) || bad_rows(v, v_stride, 1, b->n_tokens))
     return fail(OXY_ERR_INVALID_ARG, "prompt_attention: rows must be 16-byte aligned, strides at least a token's rows");
-  if (b->n_tokens > 1 && (k_stride >= (size_t)1 << 31 || v_stride >= (size_t)1 << 31))
-    return fail(OXY_ERR_INVALID_ARG, "prompt_attention: k_stride or v_stride of 2 GiB or more");
+  if (b->n_tokens > 1 && (k_stride >= (size_t)1 << 28 || v_stride >= (size_t)1 << 28))
+    return fail(OXY_ERR_INVALID_ARG, "prompt_attention: k_stride or v_stride of 256 MiB or more");
   oxy::PrefillArgs a = prefill_args(p, b, q, q_stride, out, out_stride, lse, scale);
   a.k = (const char*)k;
   a.v = (const char*)v;

@@ -37,7 +37,8 @@ constexpr int kTileBytes = 2 * kPageBytes;      // of K, or of V
 template <int kSrc, bool kPipe>
 struct PrefillLds {
   static constexpr bool kIs8 = kSrc == SRC_PAGES8;
-  static constexpr int kKeys = kPipe ? (kIs8 ? 2 : 4) : (kIs8 ? 1 : 2), kValues = kPipe ? 4 : kKeys, kRaw = kPipe ? 3 : 1;
+  static constexpr int kKeys = kPipe ? (kIs8 ? 2 : 4) : (kIs8 ? 1 : 2), kRaw = kPipe ? 3 : 1;
+  static constexpr int kValues = kPipe ? (kSrc == SRC_PAGES ? 5 : 4) : kKeys;
   char k[kKeys][kTileBytes], v[kValues][kTileBytes];
   float vs[kValues][kStep];   // in 8 bits: scales of the values
   uint32_t odd[kDim];         // keys of a tile whose value is not finite in a dim
@@ -52,16 +53,17 @@ struct PrefillLds {
   uint32_t spare[4][64];      // [wavefront]: what a request in the place of a tile's goes to
 };
 
-// `size` bytes a lane from base + offset, base the same for the wavefront, to LDS, lane after lane.  A buffer operation, which
-// counts among vector memory operations only: behind one with a full address the compiler waits for all reads of LDS at once.
-template <int kSize>
-__device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, const uint32_t offset, void* to) {
+// `size` bytes a lane to LDS, lane after lane, from offset + more + kImm behind a base that is the same for the wavefront; zeros for
+// offset + kImm of `bytes` and above.  kImm counts in LDS too.  A buffer operation, which counts among vector memory operations
+// only: behind one with a full address the compiler waits for all reads of LDS at once.
+template <int kSize, int kImm = 0>
+__device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, const uint32_t offset, void* to, const int more = 0) {
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
   const auto lds = (__attribute__((address_space(3))) void*)to;
   if constexpr (kSize == 16)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 16, offset, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 16, offset, more, kImm, 0);
   else
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 4, offset, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds, 4, offset, more, kImm, 0);
 }
 // Waits until at most n of a wavefront's vector memory operations are left.
 //
@@ -82,44 +84,75 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// Rows in LDS as they lie in memory, 512 bytes each, their 16-byte chunks changing places so that the lanes that are served
-// together find theirs in different banks: eight keys of one chunk (K), four keys of two chunks (V, read transposed).
-__device__ __forceinline__ int k_row_swap(const int key) { return key & 7; }
+// LDS serves sixteen lanes of 16 bytes at a time, from 256 bytes of banks.  Rows lie there as they do in memory, 512 bytes each,
+// their 16-byte chunks changing places so that the lanes that are served together find theirs in different banks: sixteen keys of
+// one chunk (K), four keys of four chunks (V, read transposed).  Chunks of a page change places within a KiB, so that a product's
+// operands lie in the order of the lanes.  (A wavefront's read of K 8.3 -> 7.6 cycles, of V 10.2 -> 7.5.)
+__device__ __forceinline__ int k_row_swap(const int key) { return key & 15; }
 __device__ __forceinline__ int v_row_swap(const int key) { return (key & 1) * 4 + (key >> 1 & 1); }
+__device__ __forceinline__ int k_lds_offset(const int t, const int g, const int key) { return t * 1024 + g * 256 + key * 16; }
+__device__ __forceinline__ int v_lds_offset(const int w, const int c, const int gp, const int n) {
+  return (2 * w + (c >> 1)) * 1024 + gp * 512 + (c & 1) * 256 + n * 16;
+}
 
-// Operation i of the four (in 8 bits five) that bring a wavefront's part of a tile's keys (kWhat 0; in 8 bits keys and values) or
-// values (1) to LDS.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.  blk: the wavefront's page, of rows:
-// nothing.  there: whether there is such a tile; else the buffer is of no bytes.
+// What a wavefront brings of a tile: its share of the keys (kWhat 0; in 8 bits of keys and values) or of the values (1), four
+// operations (in 8 bits five) to LDS.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.
 template <int kSrc>
 constexpr int kPartOps = kSrc == SRC_PAGES8 ? 5 : 4;
-template <int kSrc, int kWhat, class Lds>
-__device__ __forceinline__ void request_part(const char* base, const void* second, const size_t k_stride, const size_t v_stride,
-                                             Lds& lds, const int i, const int tile, const bool there, const int key0,
-                                             const int blk, const int src, const int len, const int wave, const int lane) {
-  const int pg = wave >> 1, side = wave & 1;
-  if constexpr (kSrc == SRC_PAGES) {
-    char* to = (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + pg * kPageBytes + side * (kPageBytes / 2);
-    to_lds<16>(base + (size_t)blk * kBlockBytes + kWhat * kPageBytes, there ? kPageBytes : 0,
-               side * (kPageBytes / 2) + i * 1024 + lane * 16, to + i * 1024);
-  } else if constexpr (kSrc == SRC_PAGES8) {
-    if (i < 4)   // two K chunks of all keys and half of the dims; two V chunks of all keys of half of the dims
-      to_lds<16>(base + (size_t)blk * kBlockBytes8, there ? kBlockBytes8 : 0,
-                 (i < 2 ? side * 1024 + i * 2048 : kPageBytes8 + side * 2048 + (i - 2) * 1024) + lane * 16,
-                 lds.raw.codes[tile % Lds::kRaw][wave] + i * 1024);
-    else   // 8 lanes, then 0
-      to_lds<4>((const char*)second + (size_t)blk * kScaleBytes8, there ? kScaleBytes8 : 0, lane * 4,
-                lds.raw.exps[tile % Lds::kRaw][wave]);
-  } else {   // two rows
-    const size_t stride = kWhat ? v_stride : k_stride;
-    const int two = 8 * wave + 2 * i, key = two + (lane >> 5);
-    const int first = min(key0 + two, len - 1);
-    const uint32_t next = first < len - 1 ? (uint32_t)stride : 0;   // the last one again
-    const char* from = (kWhat ? (const char*)second : base) + (size_t)(src + first) * stride;
-    to_lds<16>(from, there ? next + kDim * 2 : 0,
-               (lane >> 5) * next + ((lane & 31) ^ (kWhat ? v_row_swap(key) : k_row_swap(key))) * 16,
-               (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + two * 512);
+template <int kSrc>
+struct Bring {
+  const char* base;
+  const char* second;      // in 8 bits: the exponents; of rows: the first row of V
+  uint32_t k_stride, v_stride;   // of rows
+  int keys;                // of rows: from the wavefront's first one of tile 0 on
+  int pg, side, wave;
+  uint32_t at[2];          // pages: where a lane's chunk of K, of V comes from; in 8 bits: the lane's 16 bytes
+  uint32_t row[2];         // rows: the second of two rows
+
+  __device__ __forceinline__ Bring(const char* from, const void* from2, const size_t ks, const size_t vs, const int src,
+                                   const int key0, const int len, const int w, const int lane)
+      : base(from), second((const char*)from2), k_stride((uint32_t)ks), v_stride((uint32_t)vs), keys(len - key0 - 8 * w),
+        pg(w >> 1), side(w & 1), wave(w) {
+    if constexpr (kSrc == SRC_PAGES) {
+      at[0] = k_chunk_offset(0, (lane >> 3) & 1, lane >> 4, lane & 7);
+      at[1] = v_chunk_offset(0, (lane >> 4) & 1, lane >> 5, lane & 15);
+    } else if constexpr (kSrc == SRC_PAGES8) {
+      at[0] = lane * 16, at[1] = lane * 4;
+    } else {
+      base += (size_t)(src + key0 + 8 * w) * ks, second += (size_t)(src + key0 + 8 * w) * vs;
+      at[0] = ((lane & 31) ^ (8 * side + (lane >> 5))) * 16, at[1] = ((lane & 31) ^ ((lane >> 5) * 4)) * 16;
+      row[0] = (lane >> 5) * k_stride, row[1] = (lane >> 5) * v_stride;
+    }
   }
-}
+  // Operation i for a tile.  blk: the wavefront's page, of rows: nothing.  there: whether there is such a tile; else the buffer
+  // is of no bytes.
+  template <int kWhat, int i, class Lds>
+  __device__ __forceinline__ void part(Lds& lds, const int tile, const bool there, const int blk) const {
+    if constexpr (kSrc == SRC_PAGES) {
+      char* to = kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys];
+      to_lds<16, i * 1024>(base + (size_t)blk * kBlockBytes, there ? kBlockBytes : 0, at[kWhat],
+                           to + pg * kPageBytes + side * (kPageBytes / 2), kWhat * kPageBytes + side * (kPageBytes / 2));
+    } else if constexpr (kSrc == SRC_PAGES8) {
+      // two K chunks of all keys and half of the dims; two V chunks of all keys of half of the dims
+      if constexpr (i < 4)
+        to_lds<16>(base + (size_t)blk * kBlockBytes8, there ? kBlockBytes8 : 0, at[0], lds.raw.codes[tile % Lds::kRaw][wave] + i * 1024,
+                   i < 2 ? side * 1024 + i * 2048 : kPageBytes8 + side * 2048 + (i - 2) * 1024);
+      else   // 8 lanes, then 0
+        to_lds<4>(second + (size_t)blk * kScaleBytes8, there ? kScaleBytes8 : 0, at[1], lds.raw.exps[tile % Lds::kRaw][wave]);
+    } else {   // two rows; those behind the last one are 0
+      const uint32_t stride = kWhat ? v_stride : k_stride;
+      const int left = there ? min(keys - tile * kStep, 8) : 0;
+      const uint32_t bytes = left > 0 ? (left - 1) * stride + kDim * 2 : 0;
+      to_lds<16>((kWhat ? second : base) + (size_t)(tile * kStep) * stride, bytes,
+                 (at[kWhat] ^ (kWhat ? (i & 1) * 16 : i * 32)) + (row[kWhat] + 2 * i * stride),
+                 (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + (8 * wave + 2 * i) * 512);
+    }
+  }
+  template <int kWhat, class Lds>
+  __device__ __forceinline__ void all(Lds& lds, const int tile, const bool there, const int blk) const {
+    static_for<kPartOps<kSrc>>([&](auto i) { part<kWhat, i.value>(lds, tile, there, blk); });
+  }
+};
 
 // four e4m3 codes -> four bf16 of scale times them
 __device__ __forceinline__ u32x2 widen4(const uint32_t codes, const float scale) {
@@ -150,11 +183,11 @@ struct Widen {
       char* const kp = lds.k[tile % Lds::kKeys] + pg * kPageBytes;
       const int ch = 2 * (4 * side + (lane >> 4) + 8 * half) + c;   // eight dims
       const u32x2 a = widen4(x[half][2 * c], scale), b = widen4(x[half][2 * c + 1], scale);
-      *(u32x4*)(kp + k_chunk_offset(ch >> 2, n >> 3, ch & 3, n & 7)) = (u32x4){a[0], a[1], b[0], b[1]};
+      *(u32x4*)(kp + k_lds_offset(ch >> 2, ch & 3, n)) = (u32x4){a[0], a[1], b[0], b[1]};
     } else {
       char* const vp = lds.v[tile % Lds::kValues] + pg * kPageBytes;
       const u32x2 a = widen4(x[2][i - 5], 1.f), b = widen4(x[3][i - 5], 1.f);
-      *(u32x4*)(vp + v_chunk_offset(2 * side + w, i - 5, gp, n)) = (u32x4){a[0], a[1], b[0], b[1]};
+      *(u32x4*)(vp + v_lds_offset(2 * side + w, i - 5, gp, n)) = (u32x4){a[0], a[1], b[0], b[1]};
     }
   }
 };
@@ -190,7 +223,7 @@ __device__ __forceinline__ void set_odd_aside(Lds& lds, const int b) {
     if (kSrc == SRC_ROWS)
       at += key * 512 + ((t >> 3) ^ v_row_swap(key)) * 16 + (t & 7) * 2;
     else
-      at += (key >> 4) * kPageBytes + v_chunk_of_dim(t, (key >> 2) & 1) + v_slot_of_key(key & 15) * 2;
+      at += (key >> 4) * kPageBytes + v_lds_offset(t >> 6, t & 3, (key >> 2) & 1, (t >> 2) & 15) + v_slot_of_key(key & 15) * 2;
     uint16_t* const x = (uint16_t*)at;
     if ((*x & 0x7f80u) == 0x7f80u) *x = 0, odd |= 1u << key;
   }
@@ -231,15 +264,17 @@ __device__ __forceinline__ void products(const Read& read, const Multiply& multi
     __builtin_amdgcn_sched_barrier(kAluPasses);
   });
 }
-// The same with other work in the time that a product takes: between(j) behind product j.
-template <int kAhead, class Read, class Multiply, class Between>
-__device__ __forceinline__ void products_with(const Read& read, const Multiply& multiply, const Between& between) {
-  u32x4 x[kAhead];
-  static_for<kAhead>([&](auto j) { x[j.value] = read(j); });
-  __builtin_amdgcn_sched_barrier(0);
+// The same with other work in the time that a product takes, between(j) behind product j; the first operands have been read, and
+// those of the next sixteen products are (`next`) behind the last ones of these.
+template <int kAhead, class Read, class Next, class Multiply, class Between>
+__device__ __forceinline__ void products_with(u32x4 (&x)[kAhead], const Read& read, const Next& next, const Multiply& multiply,
+                                              const Between& between) {
   static_for<16>([&](auto j) {
     multiply(j, x[j.value % kAhead]);
-    if constexpr (j.value + kAhead < 16) x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
+    if constexpr (j.value + kAhead < 16)
+      x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
+    else
+      next(std::integral_constant<int, j.value + kAhead - 16>(), x[j.value % kAhead]);
     between(j);
     __builtin_amdgcn_sched_barrier(0);
   });
@@ -277,12 +312,12 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[8], const float sca
             x[e] = kDirect ? pack_bf16(x0, x1) : pack_f16(x0, x1);
           }
           const int chunk = (d & 127) / 8 + e0 / 8 + 2 * h;
-          *(u32x4*)(lds + n * 256 + (chunk ^ (n & 7)) * 16) = x;
+          *(u32x4*)(lds + n * 256 + (chunk ^ (n & 15)) * 16) = x;
         }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = 4 * i + (lane >> 4), chunk = (lane & 15) ^ (row & 7);
+      const int row = 4 * i + (lane >> 4), chunk = (lane & 15) ^ (row & 15);
       const u32x4 x = *(const u32x4*)(lds + row * 256 + (lane & 15) * 16);
       if ((i >> 1) < left) *(u32x4*)(to + (i >> 1) * token_stride + (row & 7) * (kDim * 2) + 256 * half + chunk * 16) = x;
     }
@@ -324,16 +359,9 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
   auto request = [&](const int tile, const int blk) {
     int at = lane;
     asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
-    at &= 63;
-    const int key0 = kv_begin + tile * kStep;
-#pragma unroll
-    for (int i = 0; i < kPartOps<kSrc>; ++i)
-      request_part<kSrc, 0>(base, second, k_stride, v_stride, lds, i, tile, true, key0, blk, src, len, wave, at);
-    if constexpr (!kRaw) {
-#pragma unroll
-      for (int i = 0; i < kPartOps<kSrc>; ++i)
-        request_part<kSrc, 1>(base, second, k_stride, v_stride, lds, i, tile, true, key0, blk, src, len, wave, at);
-    }
+    const Bring<kSrc> bring(base, second, k_stride, v_stride, src, kv_begin, len, wave, at & 63);
+    bring.template all<0>(lds, tile, true, blk);
+    if constexpr (!kRaw) bring.template all<1>(lds, tile, true, blk);
   };
 
   // a request that is there to be waited behind
@@ -361,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
     if ((n >> 4) == half) {
 #pragma unroll
       for (int j = 0; j < 16; ++j)
-        q[j] = *(const u32x4*)(q_at + (n & 15) * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+        q[j] = *(const u32x4*)(q_at + (n & 15) * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);   // read, before the other half comes there
   }
@@ -410,14 +438,16 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
     if (key0 < any_sees) {
       f32x16 s = {};
       constexpr int kReads = kSrc == SRC_PAGES ? 5 : 4;
-      const char* kb = lds.k[bk] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
+      int turn = h ^ k_row_swap(n);
+      if constexpr (kSrc == SRC_ROWS) asm volatile("" : "+v"(turn));   // see request
+      const char* kb = lds.k[bk] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int j = at.value;
             if constexpr (kSrc == SRC_ROWS)
-              return *(const u32x4*)(kb + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+              return *(const u32x4*)(kb + ((2 * j) ^ turn) * 16);
             else
-              return *(const u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 256);
+              return *(const u32x4*)(kb + j * 512);
           },
           [&](auto at, const u32x4 k) { s = mfma32(k, q[at.value], s); });
       const bool masked = key0 + kStep > all_see;
@@ -455,12 +485,14 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       }
       // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
       const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
-      const char* vb = lds.v[bv] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
+      int v_turn = c ^ v_row_swap(key);
+      if constexpr (kSrc == SRC_ROWS) asm volatile("" : "+v"(v_turn));
+      const char* vb = lds.v[bv] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : lane * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int pg = at.value >> 3, j = at.value & 7;
             if constexpr (kSrc == SRC_ROWS) {
-              const char* from = vb + pg * 8192 + (j >> 1) * 128 + ((4 * (j & 1) + c) ^ v_row_swap(key)) * 16;
+              const char* from = vb + pg * 8192 + ((4 * j) ^ v_turn) * 16;
               const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
               return (u32x4){lo[0], lo[1], hi[0], hi[1]};
             } else {
@@ -532,21 +564,13 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
     return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[src + page];
   };
   // Tiles behind the last one are requested too, as buffers of no bytes: every step has as many operations as every other.
-  auto request_one = [&](auto what, const int i, const int tile, const int blk) {
-    int at = lane;
-    asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
-    request_part<kSrc, what.value>(base, second, k_stride, v_stride, lds, i, tile, tile < n_tiles, kv_begin + tile * kStep, blk,
-                                   src, len, wave, at & 63);
-  };
-  auto request = [&](auto what, const int tile, const int blk) {
-    static_for<kPartOps<kSrc>>([&](auto i) { request_one(what, i.value, tile, blk); });
-  };
+  const Bring<kSrc> bring(base, second, k_stride, v_stride, src, kv_begin, len, wave, lane);
+  auto request = [&](auto what, const int tile, const int blk) { bring.template all<what.value>(lds, tile, tile < n_tiles, blk); };
   constexpr std::integral_constant<int, 0> kKeys;
   constexpr std::integral_constant<int, 1> kValues;
   to_lds<4>(work + (size_t)blockIdx.x * kPrefillWords, kPrefillWords * 4, lane * 4, lds.spare[wave]);   // see wait_vector
-  int page[3];   // of the next tiles whose values are requested
-  page[0] = page_of(0);
-  page[1] = page_of(1);
+  constexpr int kValuesTo = kSrc == SRC_PAGES ? 3 : 2;   // tiles ahead that values are requested, keys four
+  const int page[3] = {page_of(0), page_of(1), page_of(2)};
   request(kKeys, 0, page[0]);
 
   // The wavefront's 32 query rows, four tokens' eight heads, come through LDS, as whole lines: a row a lane, as the products
@@ -559,7 +583,6 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
     to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, lds.v[wave] + i * 1024);
   }
   request(kKeys, 1, page[1]);
-  page[2] = page_of(2);
   if constexpr (kRaw) {
     request(kKeys, 2, page[2]);
     wait_vector<10>();
@@ -568,9 +591,9 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   }
 #pragma unroll
   for (int j = 0; j < 16; ++j)
-    q[j] = *(const u32x4*)(lds.v[wave] + n * 512 + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+    q[j] = *(const u32x4*)(lds.v[wave] + n * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
   lds_barrier();   // values go to where rows were
-  int next_page = page_of(3);
+  int next_page = page_of(3), values_page = 0;   // of the tiles whose keys, whose values are requested next
   Widen widen;
   auto widen_piece = [&](const int tile, auto piece) {
     if constexpr (kRaw) {
@@ -590,12 +613,13 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
     next_page = page_of(5);
     lds_barrier();
   } else {
+    // as steps -3 to -1 would
+    if constexpr (kValuesTo == 3) request(kValues, 0, page[0]);
     request(kKeys, 2, page[2]);
-    request(kValues, 0, page[0]);
+    request(kValues, kValuesTo - 2, page[kValuesTo - 2]);
     request(kKeys, 3, next_page);
-    request(kValues, 1, page[1]);
-    page[0] = page[2];
-    page[1] = next_page;
+    request(kValues, kValuesTo - 1, page[kValuesTo - 1]);
+    values_page = next_page;
     next_page = page_of(4);
   }
 
@@ -617,34 +641,35 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   u32x4 p[2] = {};
 
   constexpr int kReads = 4;
-  auto read_key = [&](const char* kb, auto at) {
+  u32x4 x[kReads];   // operands read ahead
+  auto read_key = [&](const int tile, auto at) {
     constexpr int j = at.value;
+    const char* from = lds.k[tile % Lds::kKeys];
     if constexpr (kSrc == SRC_ROWS)
-      return *(const u32x4*)(kb + (j >> 2) * 128 + ((2 * (j & 3) + h) ^ k_row_swap(n)) * 16);
+      return *(const u32x4*)(from + n * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
     else
-      return *(const u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 256);
-  };
-  auto keys_at = [&](const int tile) {
-    return lds.k[tile % Lds::kKeys] +
-           (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + ((n >> 3) & 1) * 512 + h * 128 + (n & 7) * 16);
+      return *(const u32x4*)(from + (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16 + j * 512);
   };
   // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
   const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
+  auto read_value = [&](const int tile, auto at) {
+    constexpr int pg = at.value >> 3, j = at.value & 7;
+    const char* vb = lds.v[tile % Lds::kValues];
+    if constexpr (kSrc == SRC_ROWS) {
+      const char* from = vb + key * 512 + (g >> 1 & 1) * 8 + pg * 8192 + ((4 * j + c) ^ v_row_swap(key)) * 16;
+      const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
+      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+    } else {
+      return *(const u32x4*)(vb + lane * 16 + pg * kPageBytes + j * 1024);
+    }
+  };
+  // The first values of a tile are read behind the products of the keys, but for rows: a transposed read waits for all requests.
+  constexpr bool kValuesAhead = kSrc != SRC_ROWS;
+  auto first_values = [&](const int tile) { static_for<kReads>([&](auto j) { x[j.value] = read_value(tile, j); }); };
   // products of a tile's values, and between them what there is to do
   auto add_values = [&](const int tile, const auto& between) {
-    const char* vb = lds.v[tile % Lds::kValues] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : h * 256 + (n >> 4) * 512 + (n & 15) * 16);
-    products_with<kReads>(
-        [&](auto at) {
-          constexpr int pg = at.value >> 3, j = at.value & 7;
-          if constexpr (kSrc == SRC_ROWS) {
-            const char* from = vb + pg * 8192 + (j >> 1) * 128 + ((4 * (j & 1) + c) ^ v_row_swap(key)) * 16;
-            const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
-            return (u32x4){lo[0], lo[1], hi[0], hi[1]};
-          } else {
-            return *(const u32x4*)(vb + pg * kPageBytes + j * 1024);
-          }
-        },
-        [&](auto at, const u32x4 v) { o[at.value & 7] = mfma32(v, p[at.value >> 3], o[at.value & 7]); }, between);
+    products_with(x, [&](auto at) { return read_value(tile, at); }, [&](auto at, u32x4& y) { y = read_key(tile + 2, at); },
+                  [&](auto at, const u32x4 v) { o[at.value & 7] = mfma32(v, p[at.value >> 3], o[at.value & 7]); }, between);
   };
   auto mark_odd = [&](const int tile) {
     const int key0 = kv_begin + tile * kStep;
@@ -666,30 +691,28 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   auto odd_of_tile = [&](const int tile) {
     if (kv_begin + (tile + 1) * kStep <= tile_sees) return false;
     const bool odd = has_odd(lds, tile % Lds::kValues, wave);
-    if (odd) set_odd_aside<kSrc>(lds, tile % Lds::kValues);
+    if (odd) {
+      set_odd_aside<kSrc>(lds, tile % Lds::kValues);
+      first_values(tile);   // again
+    }
     return odd;
   };
 
   // products of a tile's keys, also of one that is not there, and between them what there is to do
   auto logits = [&](const int tile, const auto& between) {
     f32x16 sum = {};
-    const char* kb = keys_at(tile);
-    products_with<kReads>([&](auto at) { return read_key(kb, at); },
-                          [&](auto at, const u32x4 k) { sum = mfma32(k, q[at.value], sum); }, between);
+    products_with(x, [&](auto at) { return read_key(tile, at); },
+                  [&](auto at, u32x4& y) {
+                    if constexpr (kValuesAhead) y = read_value(max(tile - 1, 0), at);
+                  },
+                  [&](auto at, const u32x4 k) { sum = mfma32(k, q[at.value], sum); }, between);
     s = sum;
   };
   // What was requested three steps ago (in 8 bits: what the last one requested three steps ago) has arrived, and nobody reads any
   // more what the step before last read.
-  auto step = [&](const int i) {
+  auto step = [&]() {
     wait_vector<kRaw ? 10 : 16>();
     lds_barrier();
-    if constexpr (!kRaw) {
-      request(kKeys, i + 4, next_page);
-      request(kValues, i + 2, page[0]);
-      page[0] = page[1];
-      page[1] = next_page;
-      next_page = page_of(i + 5);
-    }
   };
   auto mask = [&](const int i) {
     const int key0 = kv_begin + i * kStep;
@@ -702,8 +725,8 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   auto raise = [&](auto at) {
     if constexpr (at.value & 1) top = fmaxf(fmaxf(top, s[at.value - 1]), s[at.value]);
   };
-  // the exponentials of tile i, and the logits of the next one; in 8 bits, where tile i + 2 has been widened, the request of the
-  // one that takes its place
+  // The exponentials of tile i, the logits of the next one, and the requests of step i: of pages and rows keys of tile i + 4 and
+  // values of one that has a free place; in 8 bits, where tile i + 2 has been widened, of the one that takes its place.
   auto weigh_and_go_on = [&](const int i) {
     const float ref = m == -__builtin_inff() ? 0.f : m;
     const char* vs_at = (char*)lds.vs[i % Lds::kValues] + 16 * h;
@@ -719,23 +742,36 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
           const f32x2 vs = *(const f32x2*)(vs_at + 4 * (8 * (j >> 2) + (j & 2)));
           x0 *= vs[0], x1 *= vs[1];
         }
-        p[j >> 3][(j >> 1) & 3] = pack_bf16(x0, x1);
+        uint32_t two = pack_bf16(x0, x1);
+        asm volatile("" : "+v"(two));   // computed here, and not in front of its use in the next step
+        p[j >> 3][(j >> 1) & 3] = two;
       }
-      if constexpr (kRaw && j % 3 == 1) request_one(kKeys, j / 3, i + 5, next_page);
+      if constexpr (kRaw) {
+        if constexpr (j % 3 == 1) bring.template part<0, j / 3>(lds, i + 5, i + 5 < n_tiles, next_page);
+      } else if constexpr (j < 8) {
+        if constexpr (j & 1)
+          bring.template part<1, j / 2>(lds, i + kValuesTo, i + kValuesTo < n_tiles, values_page);
+        else
+          bring.template part<0, j / 2>(lds, i + 4, i + 4 < n_tiles, next_page);
+      }
     });
-    if constexpr (kRaw) next_page = page_of(i + 6);
+    values_page = next_page;
+    next_page = page_of(i + (kRaw ? 6 : 5));
   };
 
+  static_for<kReads>([&](auto j) { x[j.value] = read_key(0, j); });
   logits(0, [](auto) {});
-  step(0);
+  step();
   widen_all(2);
   mask(0);
   top = -__builtin_inff();
   static_for<16>(raise);
   m = pair_max(top) * sl2;
+  static_for<kReads>([&](auto j) { x[j.value] = read_key(1, j); });
   weigh_and_go_on(0);
   for (int i = 1; i < n_tiles; ++i) {
-    step(i);
+    step();
+    if constexpr (!kValuesAhead) first_values(i - 1);
     const bool odd = odd_of_tile(i - 1);
     mask(i);
     top = -__builtin_inff();
@@ -757,6 +793,7 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
   }
   wait_vector<0>();   // the last tile's values, and requests of no bytes, which write zeros
   lds_barrier();
+  if constexpr (!kValuesAhead) first_values(n_tiles - 1);
   const bool odd = odd_of_tile(n_tiles - 1);
   add_values(n_tiles - 1, [](auto) {});
   if (odd) mark_odd(n_tiles - 1);
