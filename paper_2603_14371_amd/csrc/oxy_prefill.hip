@@ -164,30 +164,36 @@ __device__ __forceinline__ u32x2 widen4(const uint32_t codes, const float scale)
 struct Widen {
   u32x4 x[4];
   float scale;
+  uint32_t v_exp;
+  int wave, key, from[2], to[2];   // key of the tile whose scales the lane reads; offsets in its codes, in the tile: of K, of V
+
+  __device__ __forceinline__ Widen(const int w, const int lane) : wave(w), key(16 * (w >> 1) + (lane & 15)) {
+    const int side = w & 1, n = lane & 15, gp = (lane >> 4) & 1, half = lane >> 5, ch = 2 * (4 * side + (lane >> 4));
+    from[0] = lane * 16, from[1] = 2048 + half * 1024 + (gp * 16 + n) * 16;
+    to[0] = (w >> 1) * kPageBytes + k_lds_offset(ch >> 2, ch & 3, n);   // ch: eight dims
+    to[1] = (w >> 1) * kPageBytes + v_lds_offset(2 * side + half, 0, gp, n);
+  }
   // left: keys of the item from the tile's first on
   template <int i, class Lds>
-  __device__ __forceinline__ void piece(Lds& lds, const int tile, const int left, const int wave, const int lane) {
-    const int r = tile % Lds::kRaw, pg = wave >> 1, side = wave & 1;
-    const int n = lane & 15, gp = (lane >> 4) & 1, w = lane >> 5;
+  __device__ __forceinline__ void piece(Lds& lds, const int tile, const int left) {
+    const int r = tile % Lds::kRaw;
     if constexpr (i == 0) {   // all reads before the first write: behind a write the compiler waits for all requests
-      const char* from = lds.raw.codes[r][wave] + lane * 16;
-      const char* v_from = lds.raw.codes[r][wave] + 2048 + w * 1024 + (gp * 16 + n) * 16;
-      scale = scale_of((uint8_t)lds.raw.exps[r][wave][k8_scale_offset(n)]);
-      // stale exponents behind the item's end may be infinite: 0 instead
-      const float vs = 16 * pg + n < left ? scale_of((uint8_t)lds.raw.exps[r][wave][v8_scale_offset(n)]) : 0.f;
-      x[0] = *(const u32x4*)from, x[1] = *(const u32x4*)(from + 1024);
-      x[2] = *(const u32x4*)v_from, x[3] = *(const u32x4*)(v_from + 512);   // keys 4gp.. and 8 + 4gp..
-      if (side == 0 && lane < 16) lds.vs[tile % Lds::kValues][16 * pg + lane] = vs;
+      const char* codes = lds.raw.codes[r][wave];
+      const char* exps = lds.raw.exps[r][wave];
+      x[0] = *(const u32x4*)(codes + from[0]), x[1] = *(const u32x4*)(codes + from[0] + 1024);
+      x[2] = *(const u32x4*)(codes + from[1]), x[3] = *(const u32x4*)(codes + from[1] + 512);   // keys 4gp.. and 8 + 4gp..
+      scale = scale_of((uint8_t)exps[k8_scale_offset(key & 15)]);
+      v_exp = (uint8_t)exps[v8_scale_offset(key & 15)];
     } else if constexpr (i < 5) {
       constexpr int half = (i - 1) >> 1, c = (i - 1) & 1;
-      char* const kp = lds.k[tile % Lds::kKeys] + pg * kPageBytes;
-      const int ch = 2 * (4 * side + (lane >> 4) + 8 * half) + c;   // eight dims
+      if constexpr (i == 1)   // stale exponents behind the item's end may be infinite: 0 instead; by four lanes each
+        lds.vs[tile % Lds::kValues][key] = key < left ? scale_of(v_exp) : 0.f;
       const u32x2 a = widen4(x[half][2 * c], scale), b = widen4(x[half][2 * c + 1], scale);
-      *(u32x4*)(kp + k_lds_offset(ch >> 2, ch & 3, n)) = (u32x4){a[0], a[1], b[0], b[1]};
+      *(u32x4*)(lds.k[tile % Lds::kKeys] + to[0] + half * 4096 + c * 256) = (u32x4){a[0], a[1], b[0], b[1]};
     } else {
-      char* const vp = lds.v[tile % Lds::kValues] + pg * kPageBytes;
-      const u32x2 a = widen4(x[2][i - 5], 1.f), b = widen4(x[3][i - 5], 1.f);
-      *(u32x4*)(vp + v_lds_offset(2 * side + w, i - 5, gp, n)) = (u32x4){a[0], a[1], b[0], b[1]};
+      constexpr int c = i - 5;
+      const u32x2 a = widen4(x[2][c], 1.f), b = widen4(x[3][c], 1.f);
+      *(u32x4*)(lds.v[tile % Lds::kValues] + to[1] + (c >> 1) * 1024 + (c & 1) * 256) = (u32x4){a[0], a[1], b[0], b[1]};
     }
   }
 };
@@ -422,8 +428,8 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       int at = lane;
       asm volatile("" : "+v"(at));
       at &= 63;
-      Widen widen;
-      static_for<9>([&](auto j) { widen.template piece<j.value>(lds, i, len - key0, wave, at); });
+      Widen widen(wave, at);
+      static_for<9>([&](auto j) { widen.template piece<j.value>(lds, i, len - key0); });
     }
     lds_barrier();
     // nobody reads the buffers any more that the next requests go to
@@ -437,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
     if (odd) set_odd_aside<kSrc>(lds, bv);
     if (key0 < any_sees) {
       f32x16 s = {};
-      constexpr int kReads = kSrc == SRC_PAGES ? 5 : 4;
+      constexpr int kReads = kSrc == SRC_PAGES ? 5 : kSrc == SRC_ROWS ? 4 : 3;   // more would not fit the registers
       int turn = h ^ k_row_swap(n);
       if constexpr (kSrc == SRC_ROWS) asm volatile("" : "+v"(turn));   // see request
       const char* kb = lds.k[bk] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16);
@@ -594,12 +600,10 @@ __global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* wor
     q[j] = *(const u32x4*)(lds.v[wave] + n * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
   lds_barrier();   // values go to where rows were
   int next_page = page_of(3), values_page = 0;   // of the tiles whose keys, whose values are requested next
-  Widen widen;
+  Widen widen(wave, lane);
   auto widen_piece = [&](const int tile, auto piece) {
     if constexpr (kRaw) {
-      int at = lane;
-      asm volatile("" : "+v"(at));
-      widen.template piece<piece.value>(lds, tile, len - kv_begin - tile * kStep, wave, at & 63);
+      widen.template piece<piece.value>(lds, tile, len - kv_begin - tile * kStep);
     }
   };
   auto widen_all = [&](const int tile) { static_for<9>([&](auto i) { widen_piece(tile, i); }); };
