@@ -10,11 +10,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboxy.so")
 SOURCES = ["oxy_kernels.hip", "oxy_kv8.hip", "oxy_rotary.hip", "oxy_prefill.hip", "oxy_pool.cpp", "oxy_sched.cpp"]
 # packed fp32 VALU forms are switched off for device code on purpose; the first eight arguments of a
-# kernel (at most 14 words, none from a struct on) are preloaded into scalar registers; results of matrix instructions lie in
-# vector registers where a kernel may have more than 256 (by itself the compiler takes accumulation registers there, and copies
-# what other instructions read)
+# kernel (at most 14 words, none from a struct on) are preloaded into scalar registers
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-                "-mllvm", "-amdgpu-kernarg-preload-count=8", "-mllvm", "-amdgpu-mfma-vgpr-form"]
+                "-mllvm", "-amdgpu-kernarg-preload-count=8"]
 
 
 PROBE_SRC = os.path.join(HERE, "benchaid", "probe_kernels.hip")

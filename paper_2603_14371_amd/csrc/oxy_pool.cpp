@@ -1689,16 +1689,17 @@ struct PrefillItem {
 // A record is up to 16 query tokens of an item and a part of the keys that they see, in steps of 32.  A split costs a write and a
 // read of the split results, an idle CU the same time to all.  256 records have a CU each, 512 half of one (us a layer, launches
 // included, by records):
-//   one prefix of 288, 1 new token       5 records 13.0   9 10.0   14 9.3   27 9.2
-//   two prompts of 410                 104 30.5   156 26.6   208 24.6   364 24.1
-//   4 prefixes, 256 new of 960          64 33.6   192 24.2   256 24.8   320 26.4   448 27.9
-//   2048 new of a prefix              176 71.2   240 51.7   320 40.0   476 39.2
-//   1024 new of 69760                 256 618   384 603   512 526   577 685   768 613
-// So a record has at least two steps; work of up to 8 steps a CU goes to at most 256 records, more of it to 512, and one record
-// above that would be a second round.
+//   833 keys, 1 new token               5 13.3     9 10.3    14 9.6     27 9.2
+//   896 keys, 64 new tokens            14 18.2    28 13.0    56 12.0   110 14.4
+//   a prompt of 832                   104 26.8   156 23.7   208 23.0   364 24.9
+//   4 prefixes, 256 new behind 576     64 35.6   192 24.8   256 24.8   320 27.2   448 27.7
+//   a causal prompt of 2048           160 65.6   192 50.4   240 44.4   320 42.0   476 40.2
+//   2048 new behind 32781             256 633    384 607    512 542    768 624
+// So work of up to 8 steps a CU goes to at most 256 records, more of it to 512, and one record above that would be a second round.
+// A record has at least two steps, or one where there are few: more split results cost as much as they save.
 int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
                      std::vector<int32_t>* merges, int32_t* n_long) {
-  constexpr int32_t kStepKeys = 32, kLeastSteps = 2, kFewSteps = 8;
+  constexpr int32_t kStepKeys = 32, kFewSteps = 8, kTwoSteps = 32;   // steps a CU; steps from which on a record has two
   struct Tile {
     const PrefillItem* it;
     int32_t first, n, keys, parts;   // tokens of the item, keys that the last of them sees
@@ -1725,7 +1726,7 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
   const int64_t slots = steps <= kFewSteps * oxy::kPrefillCus ? oxy::kPrefillCus : 2 * oxy::kPrefillCus;
   // The fewest steps with at most `slots` records, which (steps / most + tiles) bounds; with more tiles than that, parts of a
   // slot's share of the steps.
-  int64_t most = std::max<int64_t>(kLeastSteps, (steps + slots - 1) / slots);
+  int64_t most = std::max<int64_t>(steps <= kTwoSteps ? 1 : 2, (steps + slots - 1) / slots);
   if (n_tiles < slots)
     for (int64_t high = std::max(most, (steps + slots - n_tiles - 1) / (slots - n_tiles)); most < high;) {
       const int64_t mid = (most + high) / 2;

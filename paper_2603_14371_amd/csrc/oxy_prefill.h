@@ -23,7 +23,6 @@ constexpr int kPrefillPages = 16;
 constexpr int kPrefillTokens = 16;   // query tokens of a record, at most
 // Split results that every workspace has room for: two workgroups on each of 256 CUs (35 MB).
 constexpr int32_t kPrefillPartials = 512 * kPrefillTokens;
-// Launches of at most this many records have a workgroup a CU.
 constexpr int kPrefillCus = 256;
 // Words of the merge list for each token that has split results: the token, its first one, how many.
 constexpr int kMergeWords = 3;

@@ -4,7 +4,18 @@
 //   o = sum_j softmax_j(scale <q, k_j>) v_j   over   j < min(len, max(p + 1, full)),   p the query's position
 //
 // One pass over the keys with the running maximum m and sum l of a row: for a tile of keys S = K q, P = 2^(S - m), l += sum P,
-// O += V P.  All eight heads of a token share a key, so a token is eight rows of one matrix product.
+// O += V P.  All eight heads of a token share a key, so a token is eight rows of one matrix product, and 16 tokens, 128 rows, are a
+// workgroup's: 32 rows a wavefront, queries (64 registers) and sums (128) in registers, tiles of 32 keys through LDS.  The products
+// are taken turned round, keys by rows and dims by rows: a lane then has one row's logits, and with the cache's order of keys
+// its probabilities are the next product's operand as they are.
+//
+// What bounds it: a tile's 32 products take a SIMD 1024 cycles; LDS gives four wavefronts 32 KiB each and takes in 32, at 128
+// bytes a cycle 1280; the rest of a wavefront's instructions overlap with the other workgroup's on the CU.  2048 new tokens behind 32781
+// reach 1100 TFLOP/s and a causal prompt of 16391 tokens 1040, where an 8192^3 product reaches 1247 on this card; small
+// calls are bound by the way to the first tile (position in the work list - page - rows: 4 us) and by the launches.
+//
+// A workgroup that has a CU to itself was also built with tiles requested three and four ahead and a tile's softmax among the products of its
+// neighbours: 64 workgroups 0.94 us a tile instead of 0.97, 256 as here, more of them 1.2 to 1.3 times as slow.
 #include "oxy_merge.h"
 #include "oxy_prefill.h"
 #include "oxy_kv8_device.h"
@@ -33,25 +44,29 @@ enum PrefillSource { SRC_PAGES, SRC_PAGES8, SRC_ROWS };
 constexpr int kStep = 32;                       // keys of a tile: two pages
 constexpr int kTileBytes = 2 * kPageBytes;      // of K, or of V
 
-// Tiles in use and on their way, in rings.  kPipe: one workgroup a CU, see prefill_pipe_kernel; else two.
-template <int kSrc, bool kPipe>
+// Tiles of keys and values: one in use, one on its way.  Two workgroups share a CU.
+template <int kSrc>
 struct PrefillLds {
-  static constexpr bool kIs8 = kSrc == SRC_PAGES8;
-  static constexpr int kKeys = kPipe ? (kIs8 ? 2 : 4) : (kIs8 ? 1 : 2), kRaw = kPipe ? 3 : 1;
-  static constexpr int kValues = kPipe ? (kSrc == SRC_PAGES ? 5 : 4) : kKeys;
-  char k[kKeys][kTileBytes], v[kValues][kTileBytes];
-  float vs[kValues][kStep];   // in 8 bits: scales of the values
-  uint32_t odd[kDim];         // keys of a tile whose value is not finite in a dim
-  uint32_t found[4];          // [wavefront]: whether it found one
-  // In 8 bits: codes and exponents as they lie in the pages, a part for each wavefront, which widens what it requested.
-  struct Raw {
-    char codes[kRaw][4][4096];   // [wavefront]: two pieces of 1 KiB of a K page, two of a V page
-    char exps[kRaw][4][256];     // exponents of a page, then nothing
-  };
-  struct NoRaw {};
-  std::conditional_t<kIs8, Raw, NoRaw> raw;
-  uint32_t spare[4][64];      // [wavefront]: what a request in the place of a tile's goes to
+  static constexpr int kTiles = 2;
+  char k[kTiles][kTileBytes], v[kTiles][kTileBytes];
 };
+// In 8 bits what is on its way are codes and exponents as they lie in the pages, a part for each wavefront, which widens what it
+// requested.
+template <>
+struct PrefillLds<SRC_PAGES8> {
+  static constexpr int kTiles = 1;
+  char k[kTiles][kTileBytes], v[kTiles][kTileBytes];
+  char codes[4][4096];     // [wavefront]: two pieces of 1 KiB of a K page, two of a V page
+  char exps[4][256];       // exponents of a page, then nothing
+  float vs[kStep];         // scales of the values
+};
+struct PrefillSmall {
+  uint32_t odd[kDim];      // keys of a tile whose value is not finite in a dim
+  uint32_t found[4];       // [wavefront]: whether it found one
+  uint32_t spare[4][64];   // [wavefront]: what a request in the place of a tile's goes to
+};
+template <int kSrc>
+struct PrefillShared : PrefillLds<kSrc>, PrefillSmall {};
 
 // `size` bytes a lane to LDS, lane after lane, from offset + more + kImm behind a base that is the same for the wavefront; zeros for
 // offset + kImm of `bytes` and above.  kImm counts in LDS too.  A buffer operation, which counts among vector memory operations
@@ -95,108 +110,79 @@ __device__ __forceinline__ int v_lds_offset(const int w, const int c, const int 
   return (2 * w + (c >> 1)) * 1024 + gp * 512 + (c & 1) * 256 + n * 16;
 }
 
-// What a wavefront brings of a tile: its share of the keys (kWhat 0; in 8 bits of keys and values) or of the values (1), four
-// operations (in 8 bits five) to LDS.  Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.
-template <int kSrc>
-constexpr int kPartOps = kSrc == SRC_PAGES8 ? 5 : 4;
-template <int kSrc>
-struct Bring {
-  const char* base;
-  const char* second;      // in 8 bits: the exponents; of rows: the first row of V
-  uint32_t k_stride, v_stride;   // of rows
-  int keys;                // of rows: from the wavefront's first one of tile 0 on
-  int pg, side, wave;
-  uint32_t at[2];          // pages: where a lane's chunk of K, of V comes from; in 8 bits: the lane's 16 bytes
-  uint32_t row[2];         // rows: the second of two rows
-
-  __device__ __forceinline__ Bring(const char* from, const void* from2, const size_t ks, const size_t vs, const int src,
-                                   const int key0, const int len, const int w, const int lane)
-      : base(from), second((const char*)from2), k_stride((uint32_t)ks), v_stride((uint32_t)vs), keys(len - key0 - 8 * w),
-        pg(w >> 1), side(w & 1), wave(w) {
-    if constexpr (kSrc == SRC_PAGES) {
-      at[0] = k_chunk_offset(0, (lane >> 3) & 1, lane >> 4, lane & 7);
-      at[1] = v_chunk_offset(0, (lane >> 4) & 1, lane >> 5, lane & 15);
-    } else if constexpr (kSrc == SRC_PAGES8) {
-      at[0] = lane * 16, at[1] = lane * 4;
-    } else {
-      base += (size_t)(src + key0 + 8 * w) * ks, second += (size_t)(src + key0 + 8 * w) * vs;
-      at[0] = ((lane & 31) ^ (8 * side + (lane >> 5))) * 16, at[1] = ((lane & 31) ^ ((lane >> 5) * 4)) * 16;
-      row[0] = (lane >> 5) * k_stride, row[1] = (lane >> 5) * v_stride;
+// A wavefront's part of a tile on its way to LDS, eight operations (in 8 bits five).  blk: the wavefront's page, of rows: nothing.
+// Wavefronts 0 and 1 bring the tile's first 16 keys, 2 and 3 the others.
+template <int kSrc, class Lds>
+__device__ __forceinline__ void request_tile(const char* base, const char* second, const size_t k_stride, const size_t v_stride,
+                                             Lds& lds, const int b, const int key0, const int blk, const int src,
+                                             const int len, const int wave, const int lane) {
+  const int pg = wave >> 1, side = wave & 1, part = side * (kPageBytes / 2);
+  if constexpr (kSrc == SRC_PAGES) {
+    const char* from = base + (size_t)blk * kBlockBytes;
+    const uint32_t k_chunk = k_chunk_offset(0, (lane >> 3) & 1, lane >> 4, lane & 7);
+    const uint32_t v_chunk = v_chunk_offset(0, (lane >> 4) & 1, lane >> 5, lane & 15);
+    static_for<4>([&](auto i) { to_lds<16, i.value * 1024>(from, kBlockBytes, k_chunk, lds.k[b] + pg * kPageBytes + part, part); });
+    static_for<4>([&](auto i) {
+      to_lds<16, i.value * 1024>(from, kBlockBytes, v_chunk, lds.v[b] + pg * kPageBytes + part, kPageBytes + part);
+    });
+  } else if constexpr (kSrc == SRC_PAGES8) {
+    // K chunks of all keys and half of the dims; V chunks of all keys of half of the dims
+    const char* from = base + (size_t)blk * kBlockBytes8;
+    char* to = lds.codes[wave];
+    to_lds<16>(from, kBlockBytes8, lane * 16, to, side * 1024);
+    to_lds<16>(from, kBlockBytes8, lane * 16, to + 1024, side * 1024 + 2048);
+    to_lds<16>(from, kBlockBytes8, lane * 16, to + 2048, kPageBytes8 + side * 2048);
+    to_lds<16>(from, kBlockBytes8, lane * 16, to + 3072, kPageBytes8 + side * 2048 + 1024);
+    to_lds<4>(second + (size_t)blk * kScaleBytes8, kScaleBytes8, lane * 4, lds.exps[wave]);   // 8 lanes, then 0
+  } else {
+    // two rows at a time; those behind the last one are 0.  Strides are below 2^28, so eight of them fit 32 bits.
+    const int first = key0 + 8 * wave, left = min(len - first, 8);
+    const uint32_t half = lane >> 5, chunk = lane & 31;
+    const uint32_t k_chunk = (chunk ^ (8 * side + half)) * 16, v_chunk = (chunk ^ (4 * half)) * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int two = 2 * (i & 3);
+      const uint32_t stride = (uint32_t)(i < 4 ? k_stride : v_stride), bytes = left > 0 ? (left - 1) * stride + kDim * 2 : 0;
+      to_lds<16>((i < 4 ? base : second) + (size_t)(src + first) * stride, bytes,
+                 (i < 4 ? k_chunk ^ two * 16 : v_chunk ^ (two & 2) * 8) + (two + half) * stride,
+                 (i < 4 ? lds.k[b] : lds.v[b]) + (8 * wave + two) * 512);
     }
   }
-  // Operation i for a tile.  blk: the wavefront's page, of rows: nothing.  there: whether there is such a tile; else the buffer
-  // is of no bytes.
-  template <int kWhat, int i, class Lds>
-  __device__ __forceinline__ void part(Lds& lds, const int tile, const bool there, const int blk) const {
-    if constexpr (kSrc == SRC_PAGES) {
-      char* to = kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys];
-      to_lds<16, i * 1024>(base + (size_t)blk * kBlockBytes, there ? kBlockBytes : 0, at[kWhat],
-                           to + pg * kPageBytes + side * (kPageBytes / 2), kWhat * kPageBytes + side * (kPageBytes / 2));
-    } else if constexpr (kSrc == SRC_PAGES8) {
-      // two K chunks of all keys and half of the dims; two V chunks of all keys of half of the dims
-      if constexpr (i < 4)
-        to_lds<16>(base + (size_t)blk * kBlockBytes8, there ? kBlockBytes8 : 0, at[0], lds.raw.codes[tile % Lds::kRaw][wave] + i * 1024,
-                   i < 2 ? side * 1024 + i * 2048 : kPageBytes8 + side * 2048 + (i - 2) * 1024);
-      else   // 8 lanes, then 0
-        to_lds<4>(second + (size_t)blk * kScaleBytes8, there ? kScaleBytes8 : 0, at[1], lds.raw.exps[tile % Lds::kRaw][wave]);
-    } else {   // two rows; those behind the last one are 0
-      const uint32_t stride = kWhat ? v_stride : k_stride;
-      const int left = there ? min(keys - tile * kStep, 8) : 0;
-      const uint32_t bytes = left > 0 ? (left - 1) * stride + kDim * 2 : 0;
-      to_lds<16>((kWhat ? second : base) + (size_t)(tile * kStep) * stride, bytes,
-                 (at[kWhat] ^ (kWhat ? (i & 1) * 16 : i * 32)) + (row[kWhat] + 2 * i * stride),
-                 (kWhat ? lds.v[tile % Lds::kValues] : lds.k[tile % Lds::kKeys]) + (8 * wave + 2 * i) * 512);
-    }
-  }
-  template <int kWhat, class Lds>
-  __device__ __forceinline__ void all(Lds& lds, const int tile, const bool there, const int blk) const {
-    static_for<kPartOps<kSrc>>([&](auto i) { part<kWhat, i.value>(lds, tile, there, blk); });
-  }
-};
+}
 
 // four e4m3 codes -> four bf16 of scale times them
 __device__ __forceinline__ u32x2 widen4(const uint32_t codes, const float scale) {
   return (u32x2){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))};
 }
-// A wavefront's part of a tile in 8 bits, from codes to the page order of bf16, in nine pieces.  Keys with their scale; the scales
-// of the values go into the probabilities (see the kernels), since four keys share a word.
-struct Widen {
-  u32x4 x[4];
-  float scale;
-  uint32_t v_exp;
-  int wave, key, from[2], to[2];   // key of the tile whose scales the lane reads; offsets in its codes, in the tile: of K, of V
-
-  __device__ __forceinline__ Widen(const int w, const int lane) : wave(w), key(16 * (w >> 1) + (lane & 15)) {
-    const int side = w & 1, n = lane & 15, gp = (lane >> 4) & 1, half = lane >> 5, ch = 2 * (4 * side + (lane >> 4));
-    from[0] = lane * 16, from[1] = 2048 + half * 1024 + (gp * 16 + n) * 16;
-    to[0] = (w >> 1) * kPageBytes + k_lds_offset(ch >> 2, ch & 3, n);   // ch: eight dims
-    to[1] = (w >> 1) * kPageBytes + v_lds_offset(2 * side + half, 0, gp, n);
+// A wavefront's part of a tile in 8 bits, from codes to bf16.  Keys with their scale; the scales of the values go into the
+// probabilities (see the kernel), since four keys share a word.  left: keys of the item from the tile's first on.
+template <class Lds>
+__device__ __forceinline__ void widen_tile(Lds& lds, const int left, const int wave, const int lane) {
+  const int pg = wave >> 1, side = wave & 1, n = lane & 15, gp = (lane >> 4) & 1, half = lane >> 5;
+  const char* from = lds.codes[wave] + lane * 16;
+  const char* v_from = lds.codes[wave] + 2048 + half * 1024 + (gp * 16 + n) * 16;
+  // all reads before the first write: behind a write the compiler waits for what is on its way to LDS before it reads
+  const u32x4 keys[2] = {*(const u32x4*)from, *(const u32x4*)(from + 1024)};
+  const u32x4 lo = *(const u32x4*)v_from, hi = *(const u32x4*)(v_from + 512);   // keys 4gp.. and 8 + 4gp..
+  const float s = scale_of((uint8_t)lds.exps[wave][k8_scale_offset(n)]);
+  const float vs = scale_of((uint8_t)lds.exps[wave][v8_scale_offset(n)]);
+  // stale exponents behind the item's end may be infinite: 0 instead; by eight lanes each
+  lds.vs[16 * pg + n] = 16 * pg + n < left ? vs : 0.f;
+  const int ch = 2 * (4 * side + (lane >> 4));   // eight dims
+  char* const kp = lds.k[0] + pg * kPageBytes + k_lds_offset(ch >> 2, ch & 3, n);
+  char* const vp = lds.v[0] + pg * kPageBytes + v_lds_offset(2 * side + half, 0, gp, n);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32x2 x = widen4(keys[i >> 1][2 * (i & 1)], s), y = widen4(keys[i >> 1][2 * (i & 1) + 1], s);
+    *(u32x4*)(kp + (i >> 1) * 4096 + (i & 1) * 256) = (u32x4){x[0], x[1], y[0], y[1]};
   }
-  // left: keys of the item from the tile's first on
-  template <int i, class Lds>
-  __device__ __forceinline__ void piece(Lds& lds, const int tile, const int left) {
-    const int r = tile % Lds::kRaw;
-    if constexpr (i == 0) {   // all reads before the first write: behind a write the compiler waits for all requests
-      const char* codes = lds.raw.codes[r][wave];
-      const char* exps = lds.raw.exps[r][wave];
-      x[0] = *(const u32x4*)(codes + from[0]), x[1] = *(const u32x4*)(codes + from[0] + 1024);
-      x[2] = *(const u32x4*)(codes + from[1]), x[3] = *(const u32x4*)(codes + from[1] + 512);   // keys 4gp.. and 8 + 4gp..
-      scale = scale_of((uint8_t)exps[k8_scale_offset(key & 15)]);
-      v_exp = (uint8_t)exps[v8_scale_offset(key & 15)];
-    } else if constexpr (i < 5) {
-      constexpr int half = (i - 1) >> 1, c = (i - 1) & 1;
-      if constexpr (i == 1)   // stale exponents behind the item's end may be infinite: 0 instead; by four lanes each
-        lds.vs[tile % Lds::kValues][key] = key < left ? scale_of(v_exp) : 0.f;
-      const u32x2 a = widen4(x[half][2 * c], scale), b = widen4(x[half][2 * c + 1], scale);
-      *(u32x4*)(lds.k[tile % Lds::kKeys] + to[0] + half * 4096 + c * 256) = (u32x4){a[0], a[1], b[0], b[1]};
-    } else {
-      constexpr int c = i - 5;
-      const u32x2 a = widen4(x[2][c], 1.f), b = widen4(x[3][c], 1.f);
-      *(u32x4*)(lds.v[tile % Lds::kValues] + to[1] + (c >> 1) * 1024 + (c & 1) * 256) = (u32x4){a[0], a[1], b[0], b[1]};
-    }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const u32x2 x = widen4(lo[c], 1.f), y = widen4(hi[c], 1.f);
+    *(u32x4*)(vp + (c >> 1) * 1024 + (c & 1) * 256) = (u32x4){x[0], x[1], y[0], y[1]};
   }
-};
+}
 
 // A value that a row does not see, or that nothing was written to, must not reach it, and 0 times what is not finite is NaN.
 // In tiles that some row sees a part of, such values are therefore looked for, which costs a barrier.
@@ -270,22 +256,6 @@ __device__ __forceinline__ void products(const Read& read, const Multiply& multi
     __builtin_amdgcn_sched_barrier(kAluPasses);
   });
 }
-// The same with other work in the time that a product takes, between(j) behind product j; the first operands have been read, and
-// those of the next sixteen products are (`next`) behind the last ones of these.
-template <int kAhead, class Read, class Next, class Multiply, class Between>
-__device__ __forceinline__ void products_with(u32x4 (&x)[kAhead], const Read& read, const Next& next, const Multiply& multiply,
-                                              const Between& between) {
-  static_for<16>([&](auto j) {
-    multiply(j, x[j.value % kAhead]);
-    if constexpr (j.value + kAhead < 16)
-      x[j.value % kAhead] = read(std::integral_constant<int, j.value + kAhead>());
-    else
-      next(std::integral_constant<int, j.value + kAhead - 16>(), x[j.value % kAhead]);
-    between(j);
-    __builtin_amdgcn_sched_barrier(0);
-  });
-}
-
 // A wavefront's rows leave through LDS (8 KiB of its own), as whole lines, half of the dims at a time: outputs, `scale` times
 // the sums, in bf16; or split results, see store_part, whose exponents go to exps.  to: the first of its four tokens, of which
 // `left` are there.
@@ -346,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
                                                          const char* base, const void* second, const size_t k_stride,
                                                          const size_t v_stride, const PrefillLate a) {
   constexpr bool kRaw = kSrc == SRC_PAGES8;
-  using Lds = PrefillLds<kSrc, false>;
+  using Lds = PrefillShared<kSrc>;
   __shared__ __align__(16) Lds lds;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6) & 3;
   const int n = lane & 31, h = lane >> 5;
@@ -365,9 +335,8 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
   auto request = [&](const int tile, const int blk) {
     int at = lane;
     asm volatile("" : "+v"(at));   // addresses are made here, and not kept in registers through the loop
-    const Bring<kSrc> bring(base, second, k_stride, v_stride, src, kv_begin, len, wave, at & 63);
-    bring.template all<0>(lds, tile, true, blk);
-    if constexpr (!kRaw) bring.template all<1>(lds, tile, true, blk);
+    request_tile<kSrc>(base, (const char*)second, k_stride, v_stride, lds, tile % Lds::kTiles, kv_begin + tile * kStep, blk, src,
+                       len, wave, at & 63);
   };
 
   // a request that is there to be waited behind
@@ -381,7 +350,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
   // take them, would be 64 pieces of 16 bytes each in a line of its own.  Half at a time, into buffers that the first tile does
   // not go to.
   u32x4 q[16];
-  char* const q_at = (wave < 2 ? lds.k[Lds::kKeys - 1] : lds.v[Lds::kValues - 1]) + (wave & 1) * 8192;
+  char* const q_at = (wave < 2 ? lds.k[Lds::kTiles - 1] : lds.v[Lds::kTiles - 1]) + (wave & 1) * 8192;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -427,9 +396,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
     if constexpr (kRaw) {
       int at = lane;
       asm volatile("" : "+v"(at));
-      at &= 63;
-      Widen widen(wave, at);
-      static_for<9>([&](auto j) { widen.template piece<j.value>(lds, i, len - key0); });
+      widen_tile(lds, len - key0, wave, at & 63);
     }
     lds_barrier();
     // nobody reads the buffers any more that the next requests go to
@@ -438,15 +405,15 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       next_page = page_of(i + 2);
     }
     request_spare();
-    const int bk = i % Lds::kKeys, bv = i % Lds::kValues;
-    const bool odd = key0 + kStep > tile_sees && has_odd(lds, bv, wave);
-    if (odd) set_odd_aside<kSrc>(lds, bv);
+    const int b = i % Lds::kTiles;
+    const bool odd = key0 + kStep > tile_sees && has_odd(lds, b, wave);
+    if (odd) set_odd_aside<kSrc>(lds, b);
     if (key0 < any_sees) {
       f32x16 s = {};
       constexpr int kReads = kSrc == SRC_PAGES ? 5 : kSrc == SRC_ROWS ? 4 : 3;   // more would not fit the registers
       int turn = h ^ k_row_swap(n);
       if constexpr (kSrc == SRC_ROWS) asm volatile("" : "+v"(turn));   // see request
-      const char* kb = lds.k[bk] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16);
+      const char* kb = lds.k[b] + (kSrc == SRC_ROWS ? n * 512 : (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int j = at.value;
@@ -478,13 +445,12 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       }
       const float ref = m == -__builtin_inff() ? 0.f : m;
       u32x4 p[2];
-      const char* vs_at = (char*)lds.vs[bv] + 16 * h;
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         float x = fast_exp2(__builtin_fmaf(s[r], sl2, -ref)), y = fast_exp2(__builtin_fmaf(s[r + 1], sl2, -ref));
         l += x + y;
         if constexpr (kRaw) {
-          const f32x2 vs = *(const f32x2*)(vs_at + 4 * (8 * (r >> 2) + (r & 3)));
+          const f32x2 vs = *(const f32x2*)&lds.vs[8 * (r >> 2) + 4 * h + (r & 3)];
           x *= vs[0], y *= vs[1];
         }
         p[r >> 3][(r >> 1) & 3] = pack_bf16(x, y);
@@ -493,7 +459,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
       int v_turn = c ^ v_row_swap(key);
       if constexpr (kSrc == SRC_ROWS) asm volatile("" : "+v"(v_turn));
-      const char* vb = lds.v[bv] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : lane * 16);
+      const char* vb = lds.v[b] + (kSrc == SRC_ROWS ? key * 512 + (g >> 1 & 1) * 8 : lane * 16);
       products<kReads>(
           [&](auto at) {
             constexpr int pg = at.value >> 3, j = at.value & 7;
@@ -524,283 +490,6 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
     }
     if constexpr (kRaw) lds_barrier();   // one buffer: the next tile is widened into it
   }
-
-  l = pair_sum(l);
-  lds_barrier();
-  if (part < 0) {
-    uint32_t exps;
-    store_rows<kSrc, true>(o, 1.f / l, exps, (char*)&lds + wave * 8192, (char*)a.out + (size_t)(tok0 + 4 * wave) * a.out_stride,
-                           a.out_stride, n_tok - 4 * wave, lane);
-    if (a.lse && mine < n_tok && h == 0)
-      a.lse[(size_t)(tok0 + mine) * kHeads + (n & 7)] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  } else {
-    const size_t part0 = (size_t)part + (size_t)(4 * wave) * n_parts;
-    uint32_t exps = 0;
-    store_rows<kSrc, false>(o, 0.f, exps, (char*)&lds + wave * 8192, (char*)a.part_acc + part0 * (kHeads * kDim * 2),
-                            (size_t)n_parts * (kHeads * kDim * 2), n_tok - 4 * wave, lane);
-    if (l != l && m == -__builtin_inff()) m = 0.f;   // NaN throughout is not a row without keys
-    if (mine < n_tok && h == 0)
-      *(f32x4*)(a.part_ml + ((part0 + (size_t)(n >> 3) * n_parts) * kHeads + (n & 7)) * 4) =
-          (f32x4){m, l, __uint_as_float(exps), 0.f};
-  }
-}
-
-// One workgroup a CU, one wavefront a SIMD: what a wavefront computes by its vector instructions it does while its matrix
-// products run.  Around tile i: the products of tile i - 1's values, and meanwhile the maxima of tile i's logits; then the
-// products of tile i + 1's keys, and meanwhile the exponentials of tile i.
-template <int kSrc>
-__global__ __launch_bounds__(256, 1) void prefill_pipe_kernel(const int32_t* work, const char* q_rows, const size_t q_stride,
-                                                              const char* base, const void* second, const size_t k_stride,
-                                                              const size_t v_stride, const PrefillLate a) {
-  constexpr bool kRaw = kSrc == SRC_PAGES8;
-  using Lds = PrefillLds<kSrc, true>;
-  __shared__ __align__(16) Lds lds;
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6) & 3;
-  const int n = lane & 31, h = lane >> 5;
-  const DescPtr rec = (DescPtr)work + (size_t)blockIdx.x * kPrefillWords;
-  const int tok0 = rec[F_TOK0], n_tok = rec[F_N_TOK], pos = rec[F_POS], full = rec[F_FULL];
-  const int kv_begin = rec[F_BEGIN], kv_end = rec[F_END], src = rec[F_SRC], part = rec[F_PART], n_parts = rec[F_N_PARTS],
-            len = rec[F_LEN];
-  const int n_tiles = (kv_end - kv_begin + kStep - 1) / kStep;
-
-  // the wavefront's page of a tile
-  auto page_of = [&](const int tile) {
-    if constexpr (kSrc == SRC_ROWS) return 0;
-    const int at = 2 * tile + (wave >> 1), page = min((kv_begin >> 4) + at, (len - 1) >> 4);
-    return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[src + page];
-  };
-  // Tiles behind the last one are requested too, as buffers of no bytes: every step has as many operations as every other.
-  const Bring<kSrc> bring(base, second, k_stride, v_stride, src, kv_begin, len, wave, lane);
-  auto request = [&](auto what, const int tile, const int blk) { bring.template all<what.value>(lds, tile, tile < n_tiles, blk); };
-  constexpr std::integral_constant<int, 0> kKeys;
-  constexpr std::integral_constant<int, 1> kValues;
-  to_lds<4>(work + (size_t)blockIdx.x * kPrefillWords, kPrefillWords * 4, lane * 4, lds.spare[wave]);   // see wait_vector
-  constexpr int kValuesTo = kSrc == SRC_PAGES ? 3 : 2;   // tiles ahead that values are requested, keys four
-  const int page[3] = {page_of(0), page_of(1), page_of(2)};
-  request(kKeys, 0, page[0]);
-
-  // The wavefront's 32 query rows, four tokens' eight heads, come through LDS, as whole lines: a row a lane, as the products
-  // take them, would be 64 pieces of 16 bytes each in a line of its own.
-  u32x4 q[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int row = 2 * i + (lane >> 5);
-    const char* from = q_rows + (size_t)(tok0 + min(4 * wave + (i >> 2), n_tok - 1)) * q_stride;
-    to_lds<16>(from, kHeads * kDim * 2, (row & 7) * (kDim * 2) + ((lane & 31) ^ k_row_swap(row)) * 16, lds.v[wave] + i * 1024);
-  }
-  request(kKeys, 1, page[1]);
-  if constexpr (kRaw) {
-    request(kKeys, 2, page[2]);
-    wait_vector<10>();
-  } else {
-    wait_vector<4>();
-  }
-#pragma unroll
-  for (int j = 0; j < 16; ++j)
-    q[j] = *(const u32x4*)(lds.v[wave] + n * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
-  lds_barrier();   // values go to where rows were
-  int next_page = page_of(3), values_page = 0;   // of the tiles whose keys, whose values are requested next
-  Widen widen(wave, lane);
-  auto widen_piece = [&](const int tile, auto piece) {
-    if constexpr (kRaw) {
-      widen.template piece<piece.value>(lds, tile, len - kv_begin - tile * kStep);
-    }
-  };
-  auto widen_all = [&](const int tile) { static_for<9>([&](auto i) { widen_piece(tile, i); }); };
-  if constexpr (kRaw) {
-    widen_all(0);
-    request(kKeys, 3, next_page);
-    next_page = page_of(4);
-    wait_vector<10>();
-    widen_all(1);
-    request(kKeys, 4, next_page);
-    next_page = page_of(5);
-    lds_barrier();
-  } else {
-    // as steps -3 to -1 would
-    if constexpr (kValuesTo == 3) request(kValues, 0, page[0]);
-    request(kKeys, 2, page[2]);
-    request(kValues, kValuesTo - 2, page[kValuesTo - 2]);
-    request(kKeys, 3, next_page);
-    request(kValues, kValuesTo - 1, page[kValuesTo - 1]);
-    values_page = next_page;
-    next_page = page_of(4);
-  }
-
-  // this lane's row
-  const int mine = 4 * wave + (n >> 3), tok = min(mine, n_tok - 1);
-  const int sees = min(len, max(pos + tok + 1, full));   // keys below
-  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-  for (int s = 0; s < 16; ++s) q[s] ^= (u32x4){flip, flip, flip, flip};
-  float sl2 = fabsf(a.scale * 1.4426950408889634f);
-  if (sl2 == 0.f) sl2 = 0x1p-120f;
-
-  // keys that all rows of the workgroup see; that all rows of the wavefront see
-  const int tile_sees = min(len, max(pos + 1, full));
-  const int all_see = min(len, max(pos + min(4 * wave, n_tok - 1) + 1, full));
-
-  f32x16 o[8] = {}, s = {};
-  float m = -__builtin_inff(), l = 0.f;
-  u32x4 p[2] = {};
-
-  constexpr int kReads = 4;
-  u32x4 x[kReads];   // operands read ahead
-  auto read_key = [&](const int tile, auto at) {
-    constexpr int j = at.value;
-    const char* from = lds.k[tile % Lds::kKeys];
-    if constexpr (kSrc == SRC_ROWS)
-      return *(const u32x4*)(from + n * 512 + ((2 * j + h) ^ k_row_swap(n)) * 16);
-    else
-      return *(const u32x4*)(from + (n >> 4) * kPageBytes + h * 256 + (n & 15) * 16 + j * 512);
-  };
-  // Rows: lane 16x + i of each half reads keys 4h + i / 4 (and 8 on), group 4x + i % 4 of four dims, see dim_of
-  const int g = ((lane >> 4) & 1) * 4 + (lane & 3), key = 4 * h + ((lane >> 2) & 3), c = 2 * (g & 1) + (g >> 2);
-  auto read_value = [&](const int tile, auto at) {
-    constexpr int pg = at.value >> 3, j = at.value & 7;
-    const char* vb = lds.v[tile % Lds::kValues];
-    if constexpr (kSrc == SRC_ROWS) {
-      const char* from = vb + key * 512 + (g >> 1 & 1) * 8 + pg * 8192 + ((4 * j + c) ^ v_row_swap(key)) * 16;
-      const u32x2 lo = read_turned(from), hi = read_turned(from + 8 * 512);
-      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
-    } else {
-      return *(const u32x4*)(vb + lane * 16 + pg * kPageBytes + j * 1024);
-    }
-  };
-  // The first values of a tile are read behind the products of the keys, but for rows: a transposed read waits for all requests.
-  constexpr bool kValuesAhead = kSrc != SRC_ROWS;
-  auto first_values = [&](const int tile) { static_for<kReads>([&](auto j) { x[j.value] = read_value(tile, j); }); };
-  // products of a tile's values, and between them what there is to do
-  auto add_values = [&](const int tile, const auto& between) {
-    products_with(x, [&](auto at) { return read_value(tile, at); }, [&](auto at, u32x4& y) { y = read_key(tile + 2, at); },
-                  [&](auto at, const u32x4 v) { o[at.value & 7] = mfma32(v, p[at.value >> 3], o[at.value & 7]); }, between);
-  };
-  auto mark_odd = [&](const int tile) {
-    const int key0 = kv_begin + tile * kStep;
-    auto odd_at = (const __attribute__((address_space(3))) uint32_t*)(lds.odd + 16 * h);
-    asm volatile("" : "+v"(odd_at));   // addressed here, and not by registers kept through the loop
-    const uint32_t mask = sees - key0 >= kStep ? ~0u : (1u << max(sees - key0, 0)) - 1u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = odd_at[dim_of<kSrc>(j, r)] & mask ? __builtin_nanf("") : o[j][r];
-        asm volatile("" : "+v"(x));   // chosen here, and not where this path meets the other one
-        o[j][r] = x;
-      }
-    }
-  };
-  // by all wavefronts
-  auto odd_of_tile = [&](const int tile) {
-    if (kv_begin + (tile + 1) * kStep <= tile_sees) return false;
-    const bool odd = has_odd(lds, tile % Lds::kValues, wave);
-    if (odd) {
-      set_odd_aside<kSrc>(lds, tile % Lds::kValues);
-      first_values(tile);   // again
-    }
-    return odd;
-  };
-
-  // products of a tile's keys, also of one that is not there, and between them what there is to do
-  auto logits = [&](const int tile, const auto& between) {
-    f32x16 sum = {};
-    products_with(x, [&](auto at) { return read_key(tile, at); },
-                  [&](auto at, u32x4& y) {
-                    if constexpr (kValuesAhead) y = read_value(max(tile - 1, 0), at);
-                  },
-                  [&](auto at, const u32x4 k) { sum = mfma32(k, q[at.value], sum); }, between);
-    s = sum;
-  };
-  // What was requested three steps ago (in 8 bits: what the last one requested three steps ago) has arrived, and nobody reads any
-  // more what the step before last read.
-  auto step = [&]() {
-    wait_vector<kRaw ? 10 : 16>();
-    lds_barrier();
-  };
-  auto mask = [&](const int i) {
-    const int key0 = kv_begin + i * kStep;
-    if (key0 + kStep > all_see) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = key0 + 8 * (r >> 2) + 4 * h + (r & 3) < sees ? s[r] : -__builtin_inff();
-    }
-  };
-  float top;
-  auto raise = [&](auto at) {
-    if constexpr (at.value & 1) top = fmaxf(fmaxf(top, s[at.value - 1]), s[at.value]);
-  };
-  // The exponentials of tile i, the logits of the next one, and the requests of step i: of pages and rows keys of tile i + 4 and
-  // values of one that has a free place; in 8 bits, where tile i + 2 has been widened, of the one that takes its place.
-  auto weigh_and_go_on = [&](const int i) {
-    const float ref = m == -__builtin_inff() ? 0.f : m;
-    const char* vs_at = (char*)lds.vs[i % Lds::kValues] + 16 * h;
-    const f32x16 now = s;
-    float x[16];
-    logits(i + 1, [&](auto at) {
-      constexpr int j = at.value;
-      x[j] = fast_exp2(__builtin_fmaf(now[j], sl2, -ref));
-      if constexpr (j & 1) {
-        float x0 = x[j - 1], x1 = x[j];
-        l += x0 + x1;
-        if constexpr (kRaw) {
-          const f32x2 vs = *(const f32x2*)(vs_at + 4 * (8 * (j >> 2) + (j & 2)));
-          x0 *= vs[0], x1 *= vs[1];
-        }
-        uint32_t two = pack_bf16(x0, x1);
-        asm volatile("" : "+v"(two));   // computed here, and not in front of its use in the next step
-        p[j >> 3][(j >> 1) & 3] = two;
-      }
-      if constexpr (kRaw) {
-        if constexpr (j % 3 == 1) bring.template part<0, j / 3>(lds, i + 5, i + 5 < n_tiles, next_page);
-      } else if constexpr (j < 8) {
-        if constexpr (j & 1)
-          bring.template part<1, j / 2>(lds, i + kValuesTo, i + kValuesTo < n_tiles, values_page);
-        else
-          bring.template part<0, j / 2>(lds, i + 4, i + 4 < n_tiles, next_page);
-      }
-    });
-    values_page = next_page;
-    next_page = page_of(i + (kRaw ? 6 : 5));
-  };
-
-  static_for<kReads>([&](auto j) { x[j.value] = read_key(0, j); });
-  logits(0, [](auto) {});
-  step();
-  widen_all(2);
-  mask(0);
-  top = -__builtin_inff();
-  static_for<16>(raise);
-  m = pair_max(top) * sl2;
-  static_for<kReads>([&](auto j) { x[j.value] = read_key(1, j); });
-  weigh_and_go_on(0);
-  for (int i = 1; i < n_tiles; ++i) {
-    step();
-    if constexpr (!kValuesAhead) first_values(i - 1);
-    const bool odd = odd_of_tile(i - 1);
-    mask(i);
-    top = -__builtin_inff();
-    add_values(i - 1, [&](auto j) {
-      raise(j);
-      if constexpr (j.value == 0 || (j.value >= 4 && j.value < 12)) widen_piece(i + 2, std::integral_constant<int, j.value == 0 ? 0 : j.value - 3>());
-    });
-    if (odd) mark_odd(i - 1);
-    top = pair_max(top) * sl2;
-    if (__ballot(top > m + kGrow)) {
-      const float next = top > m + kGrow ? top : m;   // a row's reference does not go by other rows
-      const float alpha = next == m ? 1.f : fast_exp2(m - next);
-      m = next;
-      l *= alpha;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] *= alpha;
-    }
-    weigh_and_go_on(i);
-  }
-  wait_vector<0>();   // the last tile's values, and requests of no bytes, which write zeros
-  lds_barrier();
-  if constexpr (!kValuesAhead) first_values(n_tiles - 1);
-  const bool odd = odd_of_tile(n_tiles - 1);
-  add_values(n_tiles - 1, [](auto) {});
-  if (odd) mark_odd(n_tiles - 1);
 
   l = pair_sum(l);
   lds_barrier();
@@ -893,28 +582,18 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prefill_merge_kernel(const P
     merge_any(m, (size_t)base, np, 0, wave, lane);
 }
 
-namespace {
-template <int kSrc>
-void launch_source(const PrefillArgs& a, const char* base, const void* second, hipStream_t s) {
-  const PrefillLate late = {a.out, a.lse, a.out_stride, a.tables, a.part_acc, a.part_ml, a.scale};
-  const auto launch = [&](auto kernel) {
-    kernel<<<a.n_work, 256, 0, s>>>(a.work, (const char*)a.q, a.q_stride, base, second, a.k_stride, a.v_stride, late);
-  };
-  if (a.n_work <= kPrefillCus)
-    launch(prefill_pipe_kernel<kSrc>);
-  else
-    launch(prefill_kernel<kSrc>);
-}
-}  // namespace
-
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s) {
   if (a.n_work <= 0) return hipSuccess;
+  const PrefillLate late = {a.out, a.lse, a.out_stride, a.tables, a.part_acc, a.part_ml, a.scale};
+  const auto launch = [&](auto kernel, const char* base, const void* second) {
+    kernel<<<a.n_work, 256, 0, s>>>(a.work, (const char*)a.q, a.q_stride, base, second, a.k_stride, a.v_stride, late);
+  };
   if (!a.layer_base)
-    launch_source<SRC_ROWS>(a, a.k, a.v, s);
+    launch(prefill_kernel<SRC_ROWS>, a.k, a.v);
   else if (a.scales)
-    launch_source<SRC_PAGES8>(a, a.layer_base, a.scales, s);
+    launch(prefill_kernel<SRC_PAGES8>, a.layer_base, a.scales);
   else
-    launch_source<SRC_PAGES>(a, a.layer_base, nullptr, s);
+    launch(prefill_kernel<SRC_PAGES>, a.layer_base, nullptr);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_merge <= 0) return e;
   prefill_merge_kernel<<<a.n_merge + (kHeads - 1) * a.n_long, 64 * kMergeWaves, 0, s>>>(a);
