@@ -139,7 +139,8 @@ typedef struct {
   int32_t max_q_tokens;     /* query tokens per attended batch (0 -> 1024; at most 2^20)     */
   int32_t max_append_tokens;/* new tokens per batch, append-only ones included (0 -> 16*num_blocks) */
   int32_t max_work_items;   /* attention work items per batch (0 -> 16384)                   */
-  int32_t max_partials;     /* per-token split results per batch (0 -> 32*max_q_tokens)      */
+  int32_t max_partials;     /* per-token split results per batch (0 -> 32*max_q_tokens);
+                             * the workspace has room for 8192 of a prefill in any case     */
   int32_t split_tokens;     /* KV tokens per work item wherever query tokens share KV pages: the
                                prefix phase (single decode items and token pairs, in large
                                launches tiles of 4 or 8 tokens) and the own phase of
@@ -312,7 +313,8 @@ int32_t oxy_prefix_batch_build(oxy_pool *pool, const oxy_prefix_item *items, int
                                int32_t flags, void *hip_stream, oxy_batch **out);
 /* q, out: DEVICE bf16, token t's eight rows of 256 at q + t * q_stride and out + t * out_stride (bytes; 16-byte
  * aligned, at least 4096), tokens in batch order, so a projection's output is taken as it is.  lse: DEVICE float
- * [n][8] or NULL.  Any scale.  Must be enqueued behind what stores the new rows of this layer.  out must not overlap q. */
+ * [n][8] or NULL.  Any scale.  Must be enqueued behind what stores the new rows of this layer.  out must not overlap q.
+ * Split results lie in the batch's workspace slot: calls with one batch must not overlap, calls with two may. */
 int32_t oxy_prefix_attention(oxy_pool *pool, const oxy_batch *batch, int32_t layer, const void *q,
                              size_t q_stride, void *out, size_t out_stride, float *lse, float scale,
                              void *hip_stream);
@@ -326,8 +328,8 @@ typedef struct {
 int32_t oxy_prompt_batch_build(oxy_pool *pool, const oxy_prompt *prompts, int32_t n_prompts,
                                void *hip_stream, oxy_batch **out);
 /* q, out, lse, scale as oxy_prefix_attention; token t's key and value, 256 bf16 each, at k + t * k_stride and
- * v + t * v_stride (DEVICE; bytes, 16-byte aligned, at least 512 and below 256 MiB).  Without tokens nothing is done, whatever the pointers
- * are.  out must not overlap q, k or v. */
+ * v + t * v_stride (DEVICE; bytes, 16-byte aligned, at least 512 and below 256 MiB).  Without tokens nothing is done,
+ * whatever the pointers are.  out must not overlap q, k or v. */
 int32_t oxy_prompt_attention(oxy_pool *pool, const oxy_batch *batch, const void *q, size_t q_stride,
                              const void *k, size_t k_stride, const void *v, size_t v_stride, void *out,
                              size_t out_stride, float *lse, float scale, void *hip_stream);

@@ -84,11 +84,12 @@ static void check_work(const std::vector<Item>& items, int n_partials) {
   for (int m = 0; m < a.n_merge; ++m) {
     const int32_t* r = a.merges + (size_t)m * kMergeWords;
     CHECK(r[0] >= 0 && r[0] < n_tok && !once[r[0]] && r[2] == n_parts[r[0]] && r[2] > 1);
+    CHECK((m < a.n_long) == (r[2] > kMergeLong));
     once[r[0]] = 1;
     for (int k = 0; k < r[2]; ++k) CHECK(parts[r[1] + k] == r[0]);
     merged += r[2];
   }
-  CHECK(merged == n_partials);
+  CHECK(merged == n_partials && a.n_long >= 0 && a.n_long <= a.n_merge);
   for (int p : parts) CHECK(p >= 0);
 }
 

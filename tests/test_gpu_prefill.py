@@ -174,3 +174,76 @@ def test_no_tokens():
             B.oxy_batch_destroy(batch)
     finally:
         pool.close()
+
+
+@FORMS
+def test_few_long_items_among_others(kv8):
+    """Tokens of more and of fewer split results than a wavefront joins at once, in one launch."""
+    chunk([(200, 17, 0), (3000, 3, 0), (0, 1, 0), (330, 20, 400), (2500, 18, 0), (5, 2, 9)], kv8, seed=41)
+
+
+@FORMS
+def test_blocks_behind_four_gibibytes(kv8):
+    """The prefix lies in blocks whose bytes in the layer begin behind 2^32."""
+    import torch
+    size = 8192 if kv8 else 16384
+    blocks = 2 ** 32 // size + 200
+    rng = np.random.default_rng(5)
+    past, n = 700, 20
+    from paper_2603_14371_amd import binding as B
+    order = np.concatenate([np.arange(blocks - 150), blocks - 150 + rng.permutation(150)])
+    at = {}
+    for name in (order, order[::-1]):       # whichever end blocks are taken from
+        cfg = B.make_config(1, blocks, free_order=name, flags=(B.POOL_KV_FP8 if kv8 else 0) | B.POOL_HOST_ONLY)
+        p = B.oxy_pool_create(cfg)
+        pid = B.oxy_prefix_create(p)
+        B.oxy_prefix_append(p, pid, 0, 0, 0, past + n, 0, 0)
+        at[min(B.oxy_prefix_blocks(p, pid))] = name
+        B.oxy_prefix_release(p, pid)
+        B.oxy_pool_destroy(p)
+    assert max(at) * size >= 2 ** 32
+    cfg = B.make_config(1, blocks, free_order=at[max(at)], flags=B.POOL_KV_FP8 if kv8 else 0)
+    kv = torch.empty(B.oxy_kv_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(B.oxy_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    cfg.kv_base, cfg.kv_bytes, cfg.workspace, cfg.workspace_bytes = kv.data_ptr(), kv.numel(), ws.data_ptr(), ws.numel()
+    pool = B.oxy_pool_create(cfg)
+    stream = torch.cuda.current_stream().cuda_stream
+    k, v, q = bits(rng, past + n, 256), bits(rng, past + n, 256), bits(rng, n, 8, 256)
+    dk, dv, dq = up(k), up(v), up(q)
+    pid = B.oxy_prefix_create(pool)
+    B.oxy_prefix_append(pool, pid, 0, dk.data_ptr(), dv.data_ptr(), past, 0, stream)
+    batch = B.oxy_prefix_batch_build(pool, [(pid, n, 0)], 0, stream)
+    assert min(B.oxy_prefix_blocks(pool, pid)) * size >= 2 ** 32
+    B.oxy_stream_append(pool, batch, 0, dk.data_ptr() + past * 512, dv.data_ptr() + past * 512, stream)
+    out, z = torch.zeros((n, 8, 256), dtype=torch.int16, device="cuda"), torch.zeros((n, 8), device="cuda")
+    B.oxy_prefix_attention(pool, batch, 0, dq.data_ptr(), 4096, out.data_ptr(), 4096, z.data_ptr(), SCALE, stream)
+    check(down(out), z.cpu().numpy().astype(np.float64), q, held(k, kv8), held(v, kv8), past, 0, SCALE)
+    B.oxy_batch_destroy(batch)
+    B.oxy_pool_destroy(pool)
+
+
+def test_rows_as_far_apart_as_may_be():
+    """Keys 256 MiB less 16 bytes apart, values a little less; from there on the call is refused."""
+    import torch
+    rng = np.random.default_rng(6)
+    n, far, less = 17, 2 ** 28 - 16, 2 ** 28 - 4096
+    pool = Pool(1, 1, max_q_tokens=32)
+    B = pool.B
+    q, k, v = bits(rng, n, 8, 256), bits(rng, n, 256), bits(rng, n, 256)
+    dq, out = up(q), torch.zeros((n, 8, 256), dtype=torch.int16, device="cuda")
+    big = torch.empty((n * far + 1024) // 2, dtype=torch.int16, device="cuda")
+    for t in range(n):
+        big[t * far // 2:t * far // 2 + 256] = up(k[t])
+        big[t * less // 2 + 512:t * less // 2 + 768] = up(v[t])
+    batch = B.oxy_prompt_batch_build(pool.p, [(n, 0)], pool.stream)
+    a = big.data_ptr()
+    args = lambda ks, vs: (pool.p, batch, dq.data_ptr(), 4096, a, ks, a + 1024, vs, out.data_ptr(), 4096, 0, SCALE,  # noqa: E731
+                           pool.stream)
+    B.oxy_prompt_attention(*args(far, less))
+    check(down(out), None, q, held(k, False), held(v, False), 0, 0, SCALE)
+    for ks, vs in ((far + 16, less), (less, far + 16), (far + 8, less), (496, less), (less, 0)):
+        with pytest.raises(B.OxyError) as e:
+            B.oxy_prompt_attention(*args(ks, vs))
+        assert e.value.code == B.ERR_INVALID_ARG
+    B.oxy_batch_destroy(batch)
+    pool.close()
