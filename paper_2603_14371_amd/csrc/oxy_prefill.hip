@@ -9,10 +9,10 @@
 // are taken turned round, keys by rows and dims by rows: a lane then has one row's logits, and with the cache's order of keys
 // its probabilities are the next product's operand as they are.
 //
-// What bounds it: a tile's 32 products take a SIMD 1024 cycles; LDS gives four wavefronts 32 KiB each and takes in 32, at 128
-// bytes a cycle 1280; the rest of a wavefront's instructions overlap with the other workgroup's on the CU.  2048 new tokens behind 32781
-// reach 1100 TFLOP/s and a causal prompt of 16391 tokens 1040, where an 8192^3 product reaches 1247 on this card; small
-// calls are bound by the way to the first tile (position in the work list - page - rows: 4 us) and by the launches.
+// What bounds it: large calls, the clock under this load (1.6 GHz of 2.4), at which the matrix pipes are busy 60 % of the time; the
+// rest of a wavefront's instructions overlap with the other workgroup's on the CU.  2048 new tokens behind 32781 reach
+// 1120 TFLOP/s and a causal prompt of 16391 tokens 1040, where an 8192^3 product reaches 1247 on this card.  Middle ones,
+// the split results and the way to the first tile (record - page - rows: 4 us); small ones, that and the launches.
 //
 // A workgroup that has a CU to itself was also built with tiles requested three and four ahead and a tile's softmax among the products of its
 // neighbours: 64 workgroups 0.94 us a tile instead of 0.97, 256 as here, more of them 1.2 to 1.3 times as slow.
@@ -102,9 +102,10 @@ __device__ __forceinline__ void lds_barrier() {
 // LDS serves sixteen lanes of 16 bytes at a time, from 256 bytes of banks.  Rows lie there as they do in memory, 512 bytes each,
 // their 16-byte chunks changing places so that the lanes that are served together find theirs in different banks: sixteen keys of
 // one chunk (K), four keys of four chunks (V, read transposed).  Chunks of a page change places within a KiB, so that a product's
-// operands lie in the order of the lanes.  (A wavefront's read of K 8.3 -> 7.6 cycles, of V 10.2 -> 7.5.)
+// operands lie in the order of the lanes.  (Of an LDS read of K 8.3 -> 7.6
+// cycles, of V 10.2 -> 7.5; the counter of conflicts is at zero.)
 __device__ __forceinline__ int k_row_swap(const int key) { return key & 15; }
-__device__ __forceinline__ int v_row_swap(const int key) { return (key & 1) * 4 + (key >> 1 & 1); }
+__device__ __forceinline__ int v_row_swap(const int key) { return (key & 3) * 4; }
 __device__ __forceinline__ int k_lds_offset(const int t, const int g, const int key) { return t * 1024 + g * 256 + key * 16; }
 __device__ __forceinline__ int v_lds_offset(const int w, const int c, const int gp, const int n) {
   return (2 * w + (c >> 1)) * 1024 + gp * 512 + (c & 1) * 256 + n * 16;
@@ -144,7 +145,7 @@ __device__ __forceinline__ void request_tile(const char* base, const char* secon
       const int two = 2 * (i & 3);
       const uint32_t stride = (uint32_t)(i < 4 ? k_stride : v_stride), bytes = left > 0 ? (left - 1) * stride + kDim * 2 : 0;
       to_lds<16>((i < 4 ? base : second) + (size_t)(src + first) * stride, bytes,
-                 (i < 4 ? k_chunk ^ two * 16 : v_chunk ^ (two & 2) * 8) + (two + half) * stride,
+                 (i < 4 ? k_chunk ^ two * 16 : v_chunk ^ (two & 2) * 64) + (two + half) * stride,
                  (i < 4 ? lds.k[b] : lds.v[b]) + (8 * wave + two) * 512);
     }
   }
