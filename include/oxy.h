@@ -140,7 +140,8 @@ typedef struct {
   int32_t max_append_tokens;/* new tokens per batch, append-only ones included (0 -> 16*num_blocks) */
   int32_t max_work_items;   /* attention work items per batch (0 -> 16384)                   */
   int32_t max_partials;     /* per-token split results per batch (0 -> 32*max_q_tokens);
-                             * the workspace has room for 8192 of a prefill in any case     */
+                             * oxy_workspace_bytes() counts 8192 of a prefill in any case;
+                             * a smaller workspace that holds max_partials is taken too      */
   int32_t split_tokens;     /* KV tokens per work item wherever query tokens share KV pages: the
                                prefix phase (single decode items and token pairs, in large
                                launches tiles of 4 or 8 tokens) and the own phase of

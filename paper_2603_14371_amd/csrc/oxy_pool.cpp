@@ -110,6 +110,7 @@ struct oxy_pool {
   size_t desc_words = 0;
   size_t per_batch_bytes = 0;
   size_t acc_offset = 0, ml_offset = 0;
+  int32_t partials = 0;   // split results of a prefill that a batch has room for
   std::vector<DescSlot> slots;
   int32_t live_batches = 0;
   uint64_t build_seq = 0;
@@ -194,17 +195,22 @@ size_t desc_words_of(const oxy_pool_config& c) {
          3 * (size_t)c.max_q_tokens /* part_off, n_parts, fresh runs */;
 }
 
-// Split results that a batch has room for: a prefill needs up to kPrefillTokens for each workgroup that the GPU holds at a
-// time, whatever max_partials is.
-size_t partials_of(const oxy_pool_config& c) { return std::max(c.max_partials, oxy::kPrefillPartials); }
+// Split results that a batch should have room for: a prefill has up to kPrefillTokens for each workgroup that the GPU holds at
+// a time, whatever max_partials is.  A workspace that is too small for them has room for max_partials.
+int32_t wanted_partials(const oxy_pool_config& c) { return std::max(c.max_partials, oxy::kPrefillPartials); }
 
-void layout_of(const oxy_pool_config& c, size_t* acc_off, size_t* ml_off, size_t* total) {
+void layout_of(const oxy_pool_config& c, int32_t partials, size_t* acc_off, size_t* ml_off, size_t* total) {
   size_t desc = align_up(desc_words_of(c) * 4, 256);
-  size_t acc = align_up(partials_of(c) * oxy::kHeads * oxy::kDim * sizeof(uint16_t), 256);
-  size_t ml = align_up(partials_of(c) * oxy::kHeads * 4 * sizeof(float), 256);
+  size_t acc = align_up((size_t)partials * oxy::kHeads * oxy::kDim * sizeof(uint16_t), 256);
+  size_t ml = align_up((size_t)partials * oxy::kHeads * 4 * sizeof(float), 256);
   *acc_off = desc;
   *ml_off = desc + acc;
   *total = desc + acc + ml;
+}
+size_t workspace_of(const oxy_pool_config& c, int32_t partials) {
+  size_t a, m, total;
+  layout_of(c, partials, &a, &m, &total);
+  return total * c.max_live_batches;
 }
 
 void unref_table(oxy_pool* p, const std::vector<int32_t>& table) {
@@ -327,9 +333,7 @@ size_t oxy_kv_bytes(const oxy_pool_config* cfg) {
 size_t oxy_workspace_bytes(const oxy_pool_config* cfg) {
   oxy_pool_config c;
   if (!resolve_config(cfg, &c)) return 0;
-  size_t a, m, total;
-  layout_of(c, &a, &m, &total);
-  return total * c.max_live_batches;
+  return workspace_of(c, wanted_partials(c));
 }
 
 int32_t oxy_pool_create(const oxy_pool_config* cfg, oxy_pool** out) {
@@ -347,11 +351,9 @@ int32_t oxy_pool_create(const oxy_pool_config* cfg, oxy_pool** out) {
     if (!c.kv_base || c.kv_bytes < oxy_kv_bytes(cfg) || ((uintptr_t)c.kv_base & 255))
       return fail(OXY_ERR_INVALID_ARG, "pool_create: kv buffer missing, misaligned or < %zu bytes",
                   oxy_kv_bytes(cfg));
-    if (!c.workspace || c.workspace_bytes < oxy_workspace_bytes(cfg) ||
-        ((uintptr_t)c.workspace & 255))
-      return fail(OXY_ERR_INVALID_ARG,
-                  "pool_create: workspace missing, misaligned or < %zu bytes",
-                  oxy_workspace_bytes(cfg));
+    const size_t least = workspace_of(c, c.max_partials);
+    if (!c.workspace || c.workspace_bytes < least || ((uintptr_t)c.workspace & 255))
+      return fail(OXY_ERR_INVALID_ARG, "pool_create: workspace missing, misaligned or < %zu bytes", least);
   }
   std::vector<int32_t> order(c.num_blocks);
   if (c.free_order) {
@@ -375,7 +377,8 @@ int32_t oxy_pool_create(const oxy_pool_config* cfg, oxy_pool** out) {
   p->free_stack.assign(order.rbegin(), order.rend());  // first element of free_order on top
   p->ref.assign(c.num_blocks, 0);
   p->desc_words = desc_words_of(c);
-  layout_of(c, &p->acc_offset, &p->ml_offset, &p->per_batch_bytes);
+  p->partials = host_only || c.workspace_bytes >= workspace_of(c, wanted_partials(c)) ? wanted_partials(c) : c.max_partials;
+  layout_of(c, p->partials, &p->acc_offset, &p->ml_offset, &p->per_batch_bytes);
   p->slots.resize(c.max_live_batches);
   for (int32_t i = 0; i < c.max_live_batches; ++i) {
     DescSlot& s = p->slots[i];
@@ -1697,7 +1700,7 @@ struct PrefillItem {
 //   2048 new behind 32781             256 633    384 607    512 542    768 624
 // So work of up to 8 steps a CU goes to at most 256 records, more of it to 512, and one record above that would be a second round.
 // A record has at least two steps, or one where there are few: more split results cost as much as they save.
-int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
+int64_t plan_prefill(const oxy_pool* p, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
                      std::vector<int32_t>* merges, int32_t* n_long) {
   constexpr int32_t kStepKeys = 32, kFewSteps = 8, kTwoSteps = 32;   // steps a CU; steps from which on a record has two
   struct Tile {
@@ -1736,7 +1739,7 @@ int64_t plan_prefill(const oxy_pool_config& c, const std::vector<PrefillItem>& i
       else
         most = mid + 1;
     }
-  for (split(most); partials > 0 && (records > c.max_work_items || partials > (int64_t)partials_of(c)); split(most)) most *= 2;
+  for (split(most); partials > 0 && (records > p->cfg.max_work_items || partials > p->partials); split(most)) most *= 2;
   struct Order {
     int32_t steps, tile, part;
   };
@@ -1897,7 +1900,7 @@ int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_i
     tok0 += pl.n_new;
     words += blocks_for(len);
   }
-  if (!append_only) d.n_partials = plan_prefill(c, work, &d.work, &d.merges, &d.n_long);
+  if (!append_only) d.n_partials = plan_prefill(p, work, &d.work, &d.merges, &d.n_long);
   d.slots.reserve(n_tokens);
   // blocks are taken in item order; what fails from here on gives them back in reverse order of their pops
   size_t done = 0;
@@ -1951,7 +1954,7 @@ int32_t prompt_batch_impl(oxy_pool* p, const oxy_prompt* prompts, int32_t n_prom
     work.push_back({at, 0, it.n_tokens, std::min(it.n_full, it.n_tokens), it.n_tokens, at});
     n_tokens += it.n_tokens;
   }
-  d.n_partials = plan_prefill(p->cfg, work, &d.work, &d.merges, &d.n_long);
+  d.n_partials = plan_prefill(p, work, &d.work, &d.merges, &d.n_long);
   return prefill_batch(p, BATCH_PROMPT, 0, n_prompts, (int32_t)n_tokens, d, hip_stream, "prompt_batch_build", out);
 }
 

@@ -9,6 +9,7 @@ namespace oxy {
 
 // A record of the work list: query tokens of one item that lie side by side, and the keys [begin, end) of that item.
 constexpr int kPrefillWords = 32;   // a line of 128 bytes
+static_assert(kPrefillWords <= kWorkWords, "a descriptor has room for kWorkWords a record");
 enum { F_TOK0 = 0,     // first query token: row of q, out and lse
        F_N_TOK,        // query tokens
        F_POS,          // position of the first one in its item
@@ -21,7 +22,7 @@ enum { F_TOK0 = 0,     // first query token: row of q, out and lse
        F_PAGES = 16 }; // paged: block ids of the first kPrefillPages pages, the item's last one repeated
 constexpr int kPrefillPages = 16;
 constexpr int kPrefillTokens = 16;   // query tokens of a record, at most
-// Split results that every workspace has room for: two workgroups on each of 256 CUs (35 MB).
+// Split results that a workspace should have room for: two workgroups on each of 256 CUs (35 MB).
 constexpr int32_t kPrefillPartials = 512 * kPrefillTokens;
 constexpr int kPrefillCus = 256;
 // Words of the merge list for each token that has split results: the token, its first one, how many.

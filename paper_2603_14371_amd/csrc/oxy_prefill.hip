@@ -14,8 +14,9 @@
 // 1120 TFLOP/s and a causal prompt of 16391 tokens 1040, where an 8192^3 product reaches 1247 on this card.  Middle ones,
 // the split results and the way to the first tile (record - page - rows: 4 us); small ones, that and the launches.
 //
-// A workgroup that has a CU to itself was also built with tiles requested three and four ahead and a tile's softmax among the products of its
-// neighbours: 64 workgroups 0.94 us a tile instead of 0.97, 256 as here, more of them 1.2 to 1.3 times as slow.
+// A workgroup that has a CU to itself was also built, with tiles requested three and four ahead and a tile's softmax among the
+// products of its neighbours: 64 records of 30 tiles 32.2 us instead of 35.6, 208 to 256 records of 6 to 10 as here, more of them
+// 1.2 to 1.3 times as slow.
 #include "oxy_merge.h"
 #include "oxy_prefill.h"
 #include "oxy_kv8_device.h"
@@ -68,11 +69,12 @@ struct PrefillSmall {
 template <int kSrc>
 struct PrefillShared : PrefillLds<kSrc>, PrefillSmall {};
 
-// `size` bytes a lane to LDS, lane after lane, from offset + more + kImm behind a base that is the same for the wavefront; zeros for
-// offset + kImm of `bytes` and above.  kImm counts in LDS too.  A buffer operation, which counts among vector memory operations
-// only: behind one with a full address the compiler waits for all reads of LDS at once.
+// kSize bytes a lane to LDS, lane after lane, from offset + more + kImm behind a base that is the same for the wavefront; zeros
+// for offset + kImm of `bytes` and above.  kImm counts in LDS too.  A buffer operation, which counts among vector memory
+// operations only: behind one with a full address the compiler waits for all reads of LDS at once.
 template <int kSize, int kImm = 0>
-__device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, const uint32_t offset, void* to, const int more = 0) {
+__device__ __forceinline__ void to_lds(const void* base, const uint32_t bytes, const uint32_t offset, void* to,
+                                       const int more = 0) {
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
   const auto lds = (__attribute__((address_space(3))) void*)to;
   if constexpr (kSize == 16)

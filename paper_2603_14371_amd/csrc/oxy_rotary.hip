@@ -280,10 +280,10 @@ int form_of(const RotaryArgs& r) {
 template <int kForm, class... Axes>
 void launch_append_form(const RotaryAppendArgs& a, hipStream_t s, const Axes&... axes) {
   const RotaryLate late = {a.rotary.freqs, a.d_slots, a.q_out, a.layer_base, a.scales, a.rotary.amplitude};
+  const uint32_t rot_and_rounds = (uint32_t)a.rotary.rot_dims | (uint32_t)(a.n_tokens >> 7) << 9;
   const auto launch = [&](auto kernel) {
     kernel<<<a.n_tokens, 320, 0, s>>>(a.rotary.positions, (const char*)a.q, (const char*)a.k_new, (const char*)a.v_new,
-                                      a.q_stride, a.k_stride, a.v_stride, (uint32_t)a.rotary.rot_dims | (uint32_t)(a.n_tokens >> 7) << 9, late,
-                                      axes...);
+                                      a.q_stride, a.k_stride, a.v_stride, rot_and_rounds, late, axes...);
   };
   if (a.scales)
     launch(rotary_append_kernel<kForm, true, Axes...>);

@@ -116,6 +116,17 @@ int main() {
     c.max_partials = upto(3) == 0 ? 1 + upto(500) : 0;
     c.max_work_items = upto(4) == 0 ? 2000 : 0;
     c.kv_bytes = oxy_kv_bytes(&c), c.workspace_bytes = oxy_workspace_bytes(&c);
+    const int asked = c.max_partials ? c.max_partials : 32 * c.max_q_tokens;
+    int room = std::max(kPrefillPartials, asked);
+    if (room > asked && round % 2) {   // a workspace of max_partials split results, with or without bytes that are not enough for more
+      const size_t per_batch = (size_t)(room - asked) * 4096 + (room * 128 - (asked * 128 + 255) / 256 * 256);
+      c.workspace_bytes -= 2 * per_batch + 1;
+      c.workspace = rows;
+      oxy_pool* none = nullptr;
+      CHECK(oxy_pool_create(&c, &none) == OXY_ERR_INVALID_ARG && !none);
+      c.workspace_bytes += round % 4 == 1 ? 1 : 2 * per_batch;
+      room = asked;
+    }
     c.kv_base = rows;
     c.workspace = aligned_alloc(256, (c.workspace_bytes + 255) / 256 * 256);
     oxy_pool* p = nullptr;
@@ -156,7 +167,7 @@ int main() {
       CHECK(oxy_prefix_batch_build(p, ask.data(), (int)ask.size(), 0, nullptr, &b) == OXY_OK);
       int32_t n_tok, n_work, n_part;
       CHECK(oxy_batch_info(b, nullptr, &n_tok, &n_work, &n_part) == OXY_OK);
-      CHECK(n_part <= std::max(kPrefillPartials, c.max_partials ? c.max_partials : 32 * c.max_q_tokens));
+      CHECK(n_part <= room);
       std::vector<int64_t> slots(n_tok);
       CHECK(oxy_batch_slots(b, slots.data(), n_tok) == OXY_OK);
       size_t at = 0;
@@ -193,7 +204,7 @@ int main() {
         items.push_back({0, m, prompts.back().n_full, m, {}});
       }
       CHECK(oxy_prompt_batch_build(p, prompts.data(), (int)prompts.size(), nullptr, &b) == OXY_OK);
-      CHECK(oxy_batch_info(b, nullptr, &n_tok, &n_work, &n_part) == OXY_OK && n_tok == total);
+      CHECK(oxy_batch_info(b, nullptr, &n_tok, &n_work, &n_part) == OXY_OK && n_tok == total && n_part <= room);
       g_launches = 0;
       CHECK(oxy_prompt_attention(p, b, rows, 5120, rows, 512, rows, 640, rows, 4096, nullptr, 1.f, nullptr) == OXY_OK);
       CHECK(g_launches == (total > 0));
