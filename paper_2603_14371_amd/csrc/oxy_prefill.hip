@@ -135,7 +135,7 @@ __device__ __forceinline__ void request_tile(const char* base, const char* secon
     to_lds<16>(from, kBlockBytes8, lane * 16, to, side * 1024);
     to_lds<16>(from, kBlockBytes8, lane * 16, to + 1024, side * 1024 + 2048);
     to_lds<16>(from, kBlockBytes8, lane * 16, to + 2048, kPageBytes8 + side * 2048);
-    to_lds<16>(from, kBlockBytes8, lane * 16, to + 3072, kPageBytes8 + side * 2048 + 1024);
+    to_lds<16>(from, kBlockBytes8, lane * 16, to + 3 * 1024, kPageBytes8 + side * 2048 + 1024);
     to_lds<4>(second + (size_t)blk * kScaleBytes8, kScaleBytes8, lane * 4, lds.exps[wave]);   // 8 lanes, then 0
   } else {
     // two rows at a time; those behind the last one are 0.  Strides are below 2^28, so eight of them fit 32 bits.

@@ -27,14 +27,19 @@ def down(t):
 class Pool:
     """A pool on the device."""
 
-    def __init__(self, layers, blocks, kv8=False, seed=None, **kw):
+    def __init__(self, layers, blocks, kv8=False, seed=None, small=False, **kw):
+        """small: a workspace for max_partials split results and no more."""
         import torch
         from paper_2603_14371_amd import binding as B
         order = None if seed is None else np.random.default_rng(seed).permutation(blocks)
         cfg = B.make_config(layers, blocks, free_order=order, flags=B.POOL_KV_FP8 if kv8 else 0, **kw)
         # never-written slots hold NaN
         self.kv = torch.full((B.oxy_kv_bytes(cfg),), 0xff, dtype=torch.uint8, device="cuda")
-        self.ws = torch.full((B.oxy_workspace_bytes(cfg),), 0xff, dtype=torch.uint8, device="cuda")
+        n_ws = B.oxy_workspace_bytes(cfg)
+        if small:
+            few = kw["max_partials"]
+            n_ws -= 2 * ((8192 - few) * 4096 + 8192 * 128 - -(-few * 128 // 256) * 256)
+        self.ws = torch.full((n_ws,), 0xff, dtype=torch.uint8, device="cuda")
         cfg.kv_base, cfg.kv_bytes = self.kv.data_ptr(), self.kv.numel()
         cfg.workspace, cfg.workspace_bytes = self.ws.data_ptr(), self.ws.numel()
         self.B, self.kv8, self.p = B, kv8, B.oxy_pool_create(cfg)

@@ -10,14 +10,14 @@ SCALE = 1.0 / 16
 
 
 def chunk(items, kv8=False, scale=SCALE, fork=False, lse=True, q_pad=0, out_pad=0, seed=0, sigma=1.0, parts=None,
-          change=None):
+          change=None, small=False):
     """items: (past, n_new, n_full).  One batch of them on a pool whose pages lie in random order; every row checked."""
     import torch
     rng = np.random.default_rng(seed)
     n = sum(it[1] for it in items)
     blocks = sum((p + m + 15) // 16 for p, m, _ in items) + 8
     kw = {} if parts is None else {"max_partials": parts}
-    pool = Pool(2, blocks, kv8, seed, max_q_tokens=max(16, n), max_append_tokens=max(16, n), **kw)
+    pool = Pool(2, blocks, kv8, seed, small, max_q_tokens=max(16, n), max_append_tokens=max(16, n), **kw)
     B = pool.B
     try:
         if fork:
@@ -137,6 +137,13 @@ def test_room_for_split_results(kv8):
     items = [(1500, 40, 0), (20, 30, 50)]
     n = [chunk(items, kv8, seed=7, parts=p)[3] for p in (1, 100000)]
     assert 0 < n[0] == n[1] <= 8192
+
+
+@FORMS
+@pytest.mark.parametrize("parts", [1, 7, 200])
+def test_a_workspace_of_few_split_results(parts, kv8):
+    info = chunk([(1500, 40, 0), (20, 30, 50), (900, 3, 0)], kv8, seed=7, parts=parts, small=True)
+    assert info[3] <= parts
 
 
 @pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 33, 64, 65, 130, 300])

@@ -163,6 +163,28 @@ def test_recorded_and_replayed_on_another_stream(kv8):
 
 
 @FORMS
+def test_two_batches_on_two_streams(kv8):
+    """Each batch has split results of its own."""
+    import torch
+    c = Calls(kv8)
+    try:
+        c.run()
+        want = c.taken()
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        a = c.x.data_ptr()
+        for _ in range(4):
+            torch.cuda.synchronize()
+            for _ in range(8):
+                c.B.oxy_prefix_attention(c.pool.p, c.prefix, 0, c.q.data_ptr(), 4096, c.out[0].data_ptr(), 4096,
+                                         c.lse[0].data_ptr(), SCALE, one.cuda_stream)
+                c.B.oxy_prompt_attention(c.pool.p, c.prompt, c.q.data_ptr(), 4096, a, 1024, a + 512, 1024,
+                                         c.out[1].data_ptr(), 4096, c.lse[1].data_ptr(), SCALE, two.cuda_stream)
+            assert all(np.array_equal(x, y) for x, y in zip(want, c.taken()))
+    finally:
+        c.close()
+
+
+@FORMS
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan], ids=str)
 @pytest.mark.parametrize("at", [0, 16, 35, 63, 64, 71])
 def test_values_that_are_not_finite(at, bad, kv8):
