@@ -153,3 +153,42 @@ def test_append(layout, rot, n_axes, kv8):
             t.check(x[:, :8], pos, got[1][0])
     finally:
         pool.close()
+
+
+@pytest.mark.parametrize("kv8", [False, True], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("n_axes", [0, 3])
+@pytest.mark.parametrize("n", [127, 128, 129, 255, 256, 300, 1100])
+def test_append_of_whole_rounds_and_others(n, n_axes, kv8):
+    """Around multiples of 128 tokens, from which on they run in another order; n_axes 0: the call of one axis."""
+    import torch
+    rng = np.random.default_rng(n)
+    t = Turn(256, "halves", _axes(rng, 128, max(n_axes, 1), "turns"), max(n_axes, 1))
+    pool = Pool(1, 160, kv8, seed=2, max_q_tokens=1200, max_append_tokens=1200)
+    B = pool.B
+    try:
+        x = bits(rng, n, 10, 256)
+        pos = rng.integers(0, 5000, (max(n_axes, 1), n))
+        d, dpos = up(x), torch.from_numpy(pos.astype(np.int32)).cuda()
+        turned = t.rotate(d, pos, 9, x_stride=5120)
+        got = []
+        for fused in (False, True):
+            pid = pool.prefix(bits(np.random.default_rng(1), 5, 256), bits(np.random.default_rng(2), 5, 256))
+            batch = B.oxy_prefix_batch_build(pool.p, [(pid, n, 0)], B.BATCH_APPEND_ONLY, pool.stream)
+            q_out = torch.zeros((n + 1, 8, 256), dtype=torch.int16, device="cuda")
+            rows = (d.data_ptr(), 5120, q_out.data_ptr(), d.data_ptr() + 4096, 5120, d.data_ptr() + 4608, 5120, pool.stream)
+            if fused and n_axes:
+                B.oxy_rotary_axes_append(pool.p, batch, 0, t.cfg, t.map, dpos.data_ptr(), *rows)
+            elif fused:
+                B.oxy_rotary_append(pool.p, batch, 0, t.cfg, dpos.data_ptr(), *rows)
+            else:
+                k, v = turned[:, 8].contiguous(), d[:, 9].contiguous()
+                q_out[:n].copy_(turned[:, :8])
+                B.oxy_stream_append(pool.p, batch, 0, k.data_ptr(), v.data_ptr(), pool.stream)
+            back = torch.zeros((2, n, 256), dtype=torch.int16, device="cuda")
+            B.oxy_gather_kv(pool.p, 0, B.oxy_batch_slots(batch), back[0].data_ptr(), back[1].data_ptr(), pool.stream)
+            got.append((down(q_out), down(back)))
+            B.oxy_batch_destroy(batch)
+            B.oxy_prefix_release(pool.p, pid)
+        assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    finally:
+        pool.close()
