@@ -1683,7 +1683,7 @@ namespace {
 // New tokens of a prefix, or a whole prompt, in a prefill's batch.
 struct PrefillItem {
   int32_t tok0, past, n_new, full, len;
-  int32_t src;   // F_SRC of its records
+  int32_t src, head, own;   // F_SRC, F_HEAD and F_OWN of its records
 };
 
 // Work list of a prefill: records in `work`, tokens with split results in `merges`, the n_long with most of them first; returns
@@ -1780,6 +1780,8 @@ int64_t plan_prefill(const oxy_pool* p, const std::vector<PrefillItem>& items, s
     w[oxy::F_PART] = t.parts > 1 ? part0[o.tile] + o.part : -1;
     w[oxy::F_N_PARTS] = t.parts;
     w[oxy::F_LEN] = t.it->len;
+    w[oxy::F_HEAD] = t.it->head;
+    w[oxy::F_OWN] = t.it->own;
     work->insert(work->end(), w, w + oxy::kPrefillWords);
   }
   return partials;
@@ -1800,14 +1802,17 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
   const int64_t n_work = (int64_t)d.work.size() / oxy::kPrefillWords;
   if (n_work > p->cfg.max_work_items)
     return fail(OXY_ERR_WORKSPACE, "%s: %lld work items > max_work_items %d", who, (long long)n_work, p->cfg.max_work_items);
-  if (d.tables.size() > table_words_of(p->cfg))
-    return fail(OXY_ERR_WORKSPACE, "%s: the block tables list %zu entries > %zu (forked prefixes list shared blocks once each)",
-                who, d.tables.size(), table_words_of(p->cfg));
+  const size_t words = d.work.size() + d.slots.size() + d.merges.size() + d.tables.size();
+  if (words > p->desc_words)
+    return fail(OXY_ERR_WORKSPACE, "%s: work list and block tables of %zu words > %zu (forks of forks list blocks again)",
+                who, words, p->desc_words);
   for (size_t w = 0; w < d.work.size() && kind == BATCH_PREFIX; w += oxy::kPrefillWords) {
     int32_t* r = &d.work[w];
     const int32_t first = r[oxy::F_BEGIN] / kPage, last = (r[oxy::F_LEN] - 1) / kPage;
-    for (int32_t i = 0; i < oxy::kPrefillPages; ++i)
-      r[oxy::F_PAGES + i] = d.tables[r[oxy::F_SRC] + std::min(first + i, last)];
+    for (int32_t i = 0; i < oxy::kPrefillPages; ++i) {
+      const int32_t page = std::min(first + i, last);
+      r[oxy::F_PAGES + i] = d.tables[page + (page < r[oxy::F_HEAD] ? r[oxy::F_SRC] : r[oxy::F_OWN])];
+    }
   }
   oxy_batch* b = new oxy_batch();
   b->pool = p;
@@ -1830,10 +1835,6 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
     delete b;
     throw;
   }
-  if (b->host.size() > p->desc_words) {   // cannot happen: every section was bounded above
-    delete b;
-    return fail(OXY_ERR_WORKSPACE, "%s: descriptor overflow (internal)", who);
-  }
   DescSlot& ds = p->slots[slot];
   if (!p->host_only && !b->host.empty()) {
     if (ds.event_pending) {
@@ -1853,6 +1854,51 @@ int32_t prefill_batch(oxy_pool* p, BatchKind kind, int32_t flags, int32_t n_item
   p->live_batches++;
   *out = b;
   return OXY_OK;
+}
+
+// Places of the items' block tables, side by side in the items' order, where forks do not list again what they share: an item
+// whose pages are half another one's or more, and that one has a table of its own, has only the others.  A longer item is
+// asked first whether it has one, so of a chain of forks all but the last go by that one.  Returns how many words they are.
+int64_t share_tables(const std::vector<const std::vector<int32_t>*>& blocks, std::vector<PrefillItem>* items) {
+  const auto common = [](const std::vector<int32_t>& x, const std::vector<int32_t>& y) {
+    // what two prefixes share is how they begin
+    int32_t low = 0, high = (int32_t)std::min(x.size(), y.size());
+    while (low < high) {
+      const int32_t mid = (low + high + 1) / 2;
+      if (x[mid - 1] == y[mid - 1])
+        low = mid;
+      else
+        high = mid - 1;
+    }
+    return low;
+  };
+  std::vector<int32_t> order(items->size()), base(items->size(), -1);
+  for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return blocks[x]->size() > blocks[y]->size(); });
+  std::unordered_map<int32_t, std::vector<int32_t>> whole;   // items with a table of their own by their first block
+  for (const int32_t i : order) {
+    PrefillItem& it = (*items)[i];
+    it.head = 0;
+    if (blocks[i]->empty()) continue;
+    std::vector<int32_t>& among = whole[blocks[i]->front()];
+    for (const int32_t j : among) {
+      const int32_t n = common(*blocks[i], *blocks[j]);
+      if (n > it.head) it.head = n, base[i] = j;
+    }
+    if (2 * it.head >= blocks_for(it.len)) continue;
+    it.head = 0;
+    base[i] = -1;
+    among.push_back(i);
+  }
+  int64_t at = 0;
+  for (PrefillItem& it : *items) {
+    it.src = (int32_t)at;
+    it.own = (int32_t)at - it.head;
+    at += blocks_for(it.len) - it.head;
+  }
+  for (size_t i = 0; i < items->size(); ++i)
+    if (base[i] >= 0) (*items)[i].src = (*items)[base[i]].src;
+  return at;
 }
 
 int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_items, int32_t flags, void* hip_stream,
@@ -1893,12 +1939,21 @@ int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_i
                 (long long)n_tokens, c.max_append_tokens, c.max_q_tokens);
   PrefillDesc d;
   std::vector<PrefillItem> work;
-  int32_t tok0 = 0, words = 0;
+  int32_t tok0 = 0;
+  int64_t words = 0;
   for (const Plan& pl : plan) {
     const int32_t len = pl.old_len + pl.n_new;
-    work.push_back({tok0, pl.old_len, pl.n_new, std::min(pl.full, len), len, words});
+    work.push_back({tok0, pl.old_len, pl.n_new, std::min(pl.full, len), len, (int32_t)words, 0, (int32_t)words});
     tok0 += pl.n_new;
     words += blocks_for(len);
+  }
+  if (!append_only && words > (int64_t)table_words_of(c)) {
+    std::vector<const std::vector<int32_t>*> blocks;
+    for (const Plan& pl : plan) blocks.push_back(&pl.px->blocks);
+    words = share_tables(blocks, &work);
+    if (words > (int64_t)p->desc_words)
+      return fail(OXY_ERR_WORKSPACE, "prefix_batch_build: block tables of %lld words > %zu (forks of forks list blocks again)",
+                  (long long)words, p->desc_words);
   }
   if (!append_only) d.n_partials = plan_prefill(p, work, &d.work, &d.merges, &d.n_long);
   d.slots.reserve(n_tokens);
@@ -1929,7 +1984,8 @@ int32_t prefix_batch_impl(oxy_pool* p, const oxy_prefix_item* items, int32_t n_i
       ++done;
       for (int32_t t = pl.old_len; t < pl.px->len; ++t) d.slots.push_back(pl.px->blocks[t / kPage] * kPage + t % kPage);
       if (!append_only)
-        d.tables.insert(d.tables.end(), pl.px->blocks.begin(), pl.px->blocks.begin() + blocks_for(pl.px->len));
+        d.tables.insert(d.tables.end(), pl.px->blocks.begin() + work[done - 1].head,
+                        pl.px->blocks.begin() + blocks_for(pl.px->len));
     }
     status = prefill_batch(p, BATCH_PREFIX, flags, n_items, (int32_t)n_tokens, d, hip_stream, "prefix_batch_build", out);
   } catch (...) {
@@ -1951,7 +2007,7 @@ int32_t prompt_batch_impl(oxy_pool* p, const oxy_prompt* prompts, int32_t n_prom
     if (n_tokens + it.n_tokens > p->cfg.max_q_tokens)
       return fail(OXY_ERR_WORKSPACE, "prompt_batch_build: more than max_q_tokens %d tokens", p->cfg.max_q_tokens);
     const int32_t at = (int32_t)n_tokens;
-    work.push_back({at, 0, it.n_tokens, std::min(it.n_full, it.n_tokens), it.n_tokens, at});
+    work.push_back({at, 0, it.n_tokens, std::min(it.n_full, it.n_tokens), it.n_tokens, at, 0, at});
     n_tokens += it.n_tokens;
   }
   d.n_partials = plan_prefill(p, work, &d.work, &d.merges, &d.n_long);

@@ -15,10 +15,12 @@ enum { F_TOK0 = 0,     // first query token: row of q, out and lse
        F_POS,          // position of the first one in its item
        F_FULL,         // a query at position p sees keys below max(p + 1, this)
        F_BEGIN, F_END, // keys of this record; F_BEGIN is a multiple of the page size
-       F_SRC,          // paged: first word of the item's block table; a prompt: row of its first token
+       F_SRC,          // paged: where page 0 stands in the block tables; a prompt: row of its first token
        F_PART,         // split result of the first query token, -1: the record writes the output
        F_N_PARTS,      // split results of a token: those of token t begin F_N_PARTS * t behind F_PART
        F_LEN,          // tokens of the item
+       F_HEAD,         // paged: pages from here on do not stand behind F_SRC, where another item's table is, but
+       F_OWN,          // page p at F_OWN + p (0 and F_SRC: a table of the item's own)
        F_PAGES = 16 }; // paged: block ids of the first kPrefillPages pages, the item's last one repeated
 constexpr int kPrefillPages = 16;
 constexpr int kPrefillTokens = 16;   // query tokens of a record, at most

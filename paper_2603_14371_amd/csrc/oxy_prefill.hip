@@ -326,14 +326,14 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
   const DescPtr rec = (DescPtr)work + (size_t)blockIdx.x * kPrefillWords;
   const int tok0 = rec[F_TOK0], n_tok = rec[F_N_TOK], pos = rec[F_POS], full = rec[F_FULL];
   const int kv_begin = rec[F_BEGIN], kv_end = rec[F_END], src = rec[F_SRC], part = rec[F_PART], n_parts = rec[F_N_PARTS],
-            len = rec[F_LEN];
+            len = rec[F_LEN], head = rec[F_HEAD], own = rec[F_OWN];
   const int n_tiles = (kv_end - kv_begin + kStep - 1) / kStep;
 
   // the wavefront's page of a tile
   auto page_of = [&](const int tile) {
     if constexpr (kSrc == SRC_ROWS) return 0;
     const int at = 2 * tile + (wave >> 1), page = min((kv_begin >> 4) + at, (len - 1) >> 4);
-    return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[src + page];
+    return at < kPrefillPages ? rec[F_PAGES + at] : ((DescPtr)a.tables)[page + (page < head ? src : own)];
   };
   auto request = [&](const int tile, const int blk) {
     int at = lane;
