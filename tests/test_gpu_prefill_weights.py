@@ -55,6 +55,7 @@ def both(way, q, k, v, past=0, full=0, scale=SCALE, whole=False):
     tol = HALF16 * np.abs(o) + 1.01 * each * spread + 1e-37
     err = np.abs(widen_bf16(got) - o)
     assert np.all(err <= tol), "%s: worst %.3f of what the roundings allow" % (way, np.max(err / tol))
+    return split
 
 
 @WAYS
