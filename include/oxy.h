@@ -295,9 +295,11 @@ int32_t oxy_batch_destroy(oxy_batch *batch);
  * j < min(len, max(p + 1, n_full)).  n_full = 0: causal; len or more: every token sees every token; between:
  * what the item begins with (an observation's images and instruction, Eq. 1) sees itself whole, what follows
  * is causal.  A row of outputs depends on its queries and on the tokens that it sees, up to rounding: how keys are cut
- * into parts goes by all items of the batch.  Values that a query does not see do not reach it, whatever they are; a key
- * that is not finite makes the outputs of the queries that see it NaN, a value that is not finite its dim, or the 64 dims
- * that it is among, of theirs NaN or infinite. */
+ * into parts goes by all items of the batch.  Values that a query does not see do not reach it, whatever they are; a value
+ * that is not finite makes its dim, or the 64 dims that it is among, of the outputs of the queries that see it NaN or
+ * infinite.  A logit of NaN or +infinity makes a head's outputs NaN; one of -infinity (of a key with an infinite dim) is a
+ * weight of 0, and a head that sees no other key has outputs of NaN and a log-sum-exp of -infinity.  A pool in 8 bits holds
+ * what is not finite as NaN. */
 typedef struct {
   int32_t prefix_id;
   int32_t n_new;  /* >= 1 tokens appended behind the prefix's length AND queried */
