@@ -311,7 +311,8 @@ typedef struct {
  * its creator's reference.  The rows are stored, layer by layer, by oxy_stream_append, oxy_rotary_append or
  * oxy_rotary_axes_append with this batch, then attended over by oxy_prefix_attention; oxy_batch_slots and
  * oxy_batch_info serve it too, the calls of a step of streams do not (OXY_ERR_INVALID_ARG).  At most max_q_tokens
- * (with OXY_BATCH_APPEND_ONLY max_append_tokens) new tokens.  Forks of one history list its blocks once.  Forks of forks may
+ * (with OXY_BATCH_APPEND_ONLY max_append_tokens) new tokens.  Made for many new tokens: a token or two at a time take less
+ * as a step of streams on the prefix.  Forks of one history list its blocks once.  Forks of forks may
  * list some again, and are refused (OXY_ERR_WORKSPACE) if a descriptor (32 * max_work_items words, 2 * num_blocks and
  * more) has no room for that. */
 int32_t oxy_prefix_batch_build(oxy_pool *pool, const oxy_prefix_item *items, int32_t n_items,

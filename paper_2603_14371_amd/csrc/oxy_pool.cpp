@@ -1691,15 +1691,19 @@ struct PrefillItem {
 //
 // A record is up to 16 query tokens of an item and a part of the keys that they see, in steps of 32.  A split costs a write and a
 // read of the split results, an idle CU the same time to all.  256 records have a CU each, 512 half of one (us a layer, launches
-// included, by records):
-//   833 keys, 1 new token               5 13.3     9 10.3    14 9.6     27 9.2
-//   896 keys, 64 new tokens            14 18.2    28 13.0    56 12.0   110 14.4
-//   a prompt of 832                   104 26.8   156 23.7   208 23.0   364 24.9
-//   4 prefixes, 256 new behind 576     64 35.6   192 24.8   256 24.8   320 27.2   448 27.7
-//   a causal prompt of 2048           160 65.6   192 50.4   240 44.4   320 42.0   476 40.2
-//   2048 new behind 32781             256 633    384 607    512 542    768 624
-// So work of up to 8 steps a CU goes to at most 256 records, more of it to 512, and one record above that would be a second round.
-// A record has at least two steps, or one where there are few: more split results cost as much as they save.
+// included, by records; in brackets steps for each of 256 CUs):
+//   833 keys, 1 new token (0.1)             5 14.5     9 10.7    14 10.0    27 9.3
+//   896 keys, 64 new tokens (0.4)          16 17.5    28 13.7    56 12.3   110 14.4
+//   a prompt of 832 (5.3)                 104 30.6   156 26.4   208 24.5   260 27.5   364 26.1   468 25.2
+//   a causal prompt of 1152 (5.2)         222 26.7   252 25.5   296 28.3   360 27.5   468 27.4
+//   4 prefixes, 256 new behind 576 (6.5)  128 30.4   192 26.9   256 26.4   320 29.7   448 29.5
+//   a causal prompt of 1408 (7.7)         208 32.2   240 32.2   260 30.8   288 33.6   322 32.4   432 31.8   528 36.6
+//   a causal prompt of 1664 (11)          168 48.6   224 39.8   260 36.4   324 39.0   392 37.7   504 36.3   594 41.1
+//   a causal prompt of 2048 (16)          160 81.1   192 60.4   240 51.8   320 48.6   408 46.7   476 44.8   576 50.8
+//   2048 new behind 32781 (530)           185 1405   313 845    437 734    512 680-743   513 867   785 795
+// So work of up to 8 steps a CU goes to at most 256 records (around there it makes little difference), more of it to 512, and one
+// record above that would be a second round.  A record has at least two steps, or one where there are few: more
+// split results cost as much as they save.
 int64_t plan_prefill(const oxy_pool* p, const std::vector<PrefillItem>& items, std::vector<int32_t>* work,
                      std::vector<int32_t>* merges, int32_t* n_long) {
   constexpr int32_t kStepKeys = 32, kFewSteps = 8, kTwoSteps = 32;   // steps a CU; steps from which on a record has two

@@ -9,14 +9,16 @@
 // are taken turned round, keys by rows and dims by rows: a lane then has one row's logits, and with the cache's order of keys
 // its probabilities are the next product's operand as they are.
 //
-// What bounds it: large calls, the clock under this load (1.6 GHz of 2.4), at which the matrix pipes are busy 60 % of the time; the
-// rest of a wavefront's instructions overlap with the other workgroup's on the CU.  2048 new tokens behind 32781 reach
-// 1120 TFLOP/s and a causal prompt of 16391 tokens 1040, where an 8192^3 product reaches 1247 on this card.  Middle ones,
-// the split results and the way to the first tile (record - page - rows: 4 us); small ones, that and the launches.
+// What bounds it: large calls, the products, of which two halves of each weight make half as many again as the formula has: 2048
+// new tokens behind 32781 take 680 to 710 us (802 to 837 TFLOP/s of the formula's, 1200 to 1255 of what runs), a causal prompt
+// of 16391 tokens 1380 to 1410 (784 to 801, 1180 to 1200), where an 8192^3 product reaches 1247 on this card; the matrix pipes
+// are busy 69 % of the cycles.  Middle ones (19 to 29 %), that a workgroup with a CU to itself does a tile's softmax and
+// products one after the other, the split results, and the way to the first tile (record - page - rows - the queries' two
+// halves: 4 us); small ones, that way and the launches.
 //
 // A workgroup that has a CU to itself was also built, with tiles requested three and four ahead and a tile's softmax among the
-// products of its neighbours: 64 records of 30 tiles 32.2 us instead of 35.6, 208 to 256 records of 6 to 10 as here, more of them
-// 1.2 to 1.3 times as slow.
+// products of its neighbours (then of weights rounded once): 64 records of 30 tiles 32.2 us instead of 35.6, 208 to 256 records
+// of 6 to 10 as here, more of them 1.2 to 1.3 times as slow.
 #include "oxy_merge.h"
 #include "oxy_prefill.h"
 #include "oxy_kv8_device.h"
@@ -450,9 +452,9 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const int32_t* work, co
       // kernels of a step.  Rounded once (2^-8 of each), they were up to 1.5 times a step's tolerance off where few keys, or a few
       // large weights among thousands, carry a row, and off by as much in all dims where weights round the same way.  Half as
       // many products of the values again, behind the same reads (rounded once / so, us a layer: all of a prompt of 832 22.3 /
-      // 23.8, 4 prefixes' 256 tokens behind 576 23.3 / 24.5, a causal prompt of 16391 1085 / 1410, 2048 tokens behind 32781
-      // 518 / 692, 48 behind 131071 in 8 bits 76 / 88).  The second product only in tiles with a weight above an eighth
-      // of its row's sum so far: 1200 of the 1410, and roundings that agree still add up.
+      // 23.8, 4 prefixes' 256 tokens behind 576 23.3 / 24.5, a causal prompt of 16391 1085 / 1380 to 1410, 2048 tokens behind
+      // 32781 518 / 680 to 710, 48 behind 131071 in 8 bits 76 / 88).  The second product only in tiles with a weight above an eighth
+      // of its row's sum so far: 1200 for the long prompt, and roundings that agree still add up.
       const float ref = m == -__builtin_inff() ? 0.f : m;
       u32x4 p[2], rest[2];
 #pragma unroll
